@@ -33,7 +33,7 @@ def listed():
         # A batch of chats of different lengths through a 70B layer, some batch places idle.
         {"name": "cached_ragged_32", "kind": "cached", "sequences": 32, "queries": 1, "longest": 4099, "ragged": True, "heads": 64, "kv_heads": 8,
          "head_dim": 128, "page": 64},
-        # Four drafted tokens and one more of each of eight sequences, heads of 64.
+        # Up to four drafted tokens and one more of each of eight sequences, heads of 64.
         {"name": "cached_drafts_8x5", "kind": "cached", "sequences": 8, "queries": 5, "longest": 16001, "ragged": True, "heads": 16, "kv_heads": 4,
          "head_dim": 64, "page": 16},
         # Two long documents: few rows, a long axis.
@@ -104,7 +104,7 @@ def _lengths(case):
         out = []
         for i in range(n):
             length = longest if i == 0 or not case["ragged"] else 0 if rng.random() < 0.08 else rng.randint(1, longest)
-            out.append((case["queries"], length))
+            out.append((rng.randint(1, case["queries"]) if case["ragged"] else case["queries"], length))
         return out
     return [(longest if i == 0 or not case["ragged"] else rng.randint(0, longest), case["prefix"] and rng.randint(0, case["prefix"])) for i in range(n)]
 
@@ -258,7 +258,9 @@ def prepare(case, seed):
         lengths = _lengths(case)
         state.update(q=q, table=table.cuda(), scale=D ** -0.5, page=case["page"], counts=[a for a, _ in lengths], keys=[b for _, b in lengths])
         state["lengths"] = torch.tensor(state["keys"], dtype=torch.int32, device="cuda")
-        state["starts"] = torch.tensor(_starts(state["counts"]), dtype=torch.int32, device="cuda")
+        state["starts"] = None                   # as many query tokens in every sequence
+        if len(set(state["counts"])) > 1:
+            state["starts"] = torch.tensor(_starts(state["counts"]), dtype=torch.int32, device="cuda")
         state["longest"] = max(state["keys"])
         if own:
             state["cache"] = B.KVCache(pages, G, D, page_tokens=case["page"])
