@@ -27,6 +27,9 @@ EXPORTS = ["ap_packed_size", "ap_pack_host", "ap_unpack_host", "ap_blob_lut_entr
            "ap_gemm_workspace_size", "ap_gemm", "ap_gemm_static", "ap_quantize", "ap_probe_read", "ap_probe_issue", "ap_matrix_info",
            "ap_free", "ap_strerror"]
 
+DECODE_EXPORTS = ["ap_cache_size", "ap_cache_append", "ap_cache_read", "ap_attention_cached_size", "ap_attention_cached",
+                  "ap_attention_prompt", "ap_verify_size", "ap_verify"]   # include/apdecode.h
+
 
 OPTIONS = {"waves": 0, "row_groups": 1, "mfma_min_batch": 2, "variant": 3}
 VARIANT_AUTO, VARIANT_NO_EXCHANGE, VARIANT_EXCHANGE, VARIANT_BANK_PER_LANE = 0, 1, 3, 5
@@ -71,8 +74,18 @@ def _load():
                                  ctypes.POINTER(cu)]
     L.ap_free.argtypes = [vp]
     L.ap_free.restype = None
+    L.ap_cache_size.argtypes = [vp, psz]
+    L.ap_cache_append.argtypes = [vp, vp, vp]
+    L.ap_cache_read.argtypes = [vp, vp, ctypes.c_int64, vp, vp, vp]
+    L.ap_attention_cached_size.argtypes = [vp, vp, psz]
+    L.ap_attention_cached.argtypes = [vp, vp, vp]
+    L.ap_attention_prompt.argtypes = [vp, vp]
+    L.ap_verify_size.argtypes = [vp, psz]
+    L.ap_verify.argtypes = [vp, vp]
     L.ap_strerror.argtypes = [ci]
     L.ap_strerror.restype = ctypes.c_char_p
+    for name in DECODE_EXPORTS:
+        getattr(L, name).restype = ci
     for name in EXPORTS:
         if name not in ("ap_free", "ap_strerror"):
             getattr(L, name).restype = ci
@@ -333,3 +346,84 @@ def ap_quantize(w, sens=None, n_seed=3, n=8, iters=20):
 def ap_gemv_raw(handle, b, x_ptr, y_ptr, batch, stream_ptr):
     """Unchecked call for timing loops: returns the status code."""
     return lib.ap_gemv(handle, b, x_ptr, y_ptr, batch, stream_ptr)
+
+
+# ---------------------------------------------------------------------------------------------- decoder operators (include/apdecode.h)
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("pages", ctypes.c_int64), ("page_tokens", ctypes.c_int), ("kv_heads", ctypes.c_int),
+                ("head_dim", ctypes.c_int)]
+
+
+def ap_cache_size(pages, kv_heads, head_dim, page_tokens=64):
+    """Bytes of a 4-bit cache of `pages` pages of page_tokens tokens."""
+    out = ctypes.c_size_t(0)
+    _check(lib.ap_cache_size(ctypes.byref(_Cache(None, pages, page_tokens, kv_heads, head_dim)), ctypes.byref(out)), "ap_cache_size")
+    return out.value
+
+
+class KVCache:
+    """A paged cache of keys and values in 4 bits: owns the torch device buffer.  A token's slot is page * page_tokens + place."""
+
+    def __init__(self, pages, kv_heads, head_dim, page_tokens=64, device="cuda:0"):
+        size = ap_cache_size(pages, kv_heads, head_dim, page_tokens)
+        self.pages, self.page_tokens, self.kv_heads, self.head_dim = pages, page_tokens, kv_heads, head_dim
+        self.shape = (pages, page_tokens, kv_heads, head_dim)
+        self.buf = torch.empty(size, dtype=torch.uint8, device=device)
+
+
+def _named(stream):
+    return None if stream is None else stream.cuda_stream
+
+
+def _result(r, where):
+    if type(r) is int:
+        raise ApError(abs(r), where if r > 0 else where + "_size")
+    return r
+
+
+def rotary_table(rows, rot_dim, base=10000.0, device="cuda:0"):
+    """(rows, rot_dim) float32: the cosines, then the sines of position / base^(2 i / rot_dim), as ap_cache_append takes them."""
+    angle = torch.arange(rows, dtype=torch.float64)[:, None] * base ** (-torch.arange(0, rot_dim, 2, dtype=torch.float64) / rot_dim)
+    return torch.cat([angle.cos(), angle.sin()], dim=1).float().to(device)
+
+
+def ap_cache_append(cache, k, v, slots, q=None, positions=None, rotary=None, interleaved=False, q_out=None, k_out=None, stream=None):
+    """Rotates q and k (tokens, heads, head_dim) and appends k and v to the cache; returns the rotated (q, k), q None if none was given.
+
+    slots, positions: int64 (tokens,); rotary: a table like rotary_table's, None = no rotation.  A slot outside the cache (-1) keeps its
+    token out of it.  q_out and k_out may be q and k themselves.  `stream` as in ap_gemv."""
+    return _result(_torch_call.cache_append(cache.buf, cache.shape, k, v, slots, q, positions, rotary, interleaved, q_out, k_out,
+                                            _named(stream)), "ap_cache_append")
+
+
+def ap_cache_read(cache, slots, stream=None):
+    """The values that slots stand for: (k, v), float16 (slots, kv_heads, head_dim) each; zeros for a slot outside the cache."""
+    return _result(_torch_call.cache_read(cache.buf, cache.shape, slots, _named(stream)), "ap_cache_read")
+
+
+def ap_attention_cached(cache, q, tables, lengths, q_starts=None, scale=None, max_length=None, out=None, work=None, stream=None):
+    """Attention of new tokens q (tokens, heads, head_dim) over the cache; the last token of a sequence sees its lengths[s] keys.
+
+    tables: int32 (sequences, pages), lengths: int32 (sequences,), q_starts: int32 (sequences + 1,), None = tokens / sequences each;
+    max_length: a bound of lengths, None = what the tables hold; scale: head_dim ** -0.5 if None.  `stream` as in ap_gemv; a given work (uint8)
+    is in use until that stream is done with the call."""
+    return _result(_torch_call.attention_cached(cache.buf, cache.shape, q, tables, lengths, q_starts,
+                                                scale, max_length, out, work, _named(stream)),
+                   "ap_attention_cached")
+
+
+def ap_attention_prompt(q, k, v, q_starts, k_starts=None, scale=None, out=None, stream=None):
+    """Causal attention over packed sequences: q (tokens, heads, head_dim), k and v (keys, kv_heads, head_dim); q_starts, k_starts: int32
+    (sequences + 1,), k_starts = q_starts if None.  The last query of a sequence sees its last key.  `stream` as in ap_gemv."""
+    return _result(_torch_call.attention_prompt(q, k, v, q_starts, q_starts if k_starts is None else k_starts, scale, out,
+                                                _named(stream)), "ap_attention_prompt")
+
+
+def ap_verify(target, draft, drafted, uniform, noise, counts=None, work=None, stream=None):
+    """Verification of drafted (sequences, drafts) int64 tokens by target (sequences, drafts + 1, vocabulary) and draft (sequences, drafts,
+    vocabulary) probabilities, float32 or float16, with uniform (sequences, drafts) and exponential noise (sequences, vocabulary) float32.
+
+    Returns (tokens (sequences, drafts + 1) int64: the accepted drafts, the token after them, -1s; accepted (sequences,) int32)."""
+    return _result(_torch_call.verify(target, draft, drafted, uniform, noise, counts, work, _named(stream)), "ap_verify")

@@ -2,49 +2,13 @@
 // output and workspace tensors, the current stream and the call of the C-ABI entry point.  They hold no logic of the library.
 // A small product takes 3 to 5 us on the GPU; through ctypes and torch.empty its call took the host 6.1 us, of which the launch
 // is 2.9.  Here: 4.6 (512 x 512, calls in a row).
-#include <torch/csrc/Exceptions.h>
-#include <torch/csrc/autograd/python_variable.h>
-
-#include <ATen/hip/impl/HIPStreamMasqueradingAsCUDA.h>
-#include <ATen/ops/empty.h>
-
-#include <algorithm>
-#include <vector>
+#include "torch_args.h"
 
 #include "../../include/apgemv.h"
 
+using namespace apgemv_torch;
+
 namespace {
-
-// `o` as a tensor, or an error set
-const at::Tensor *tensor_of(PyObject *o, const char *what)
-{
-    if (THPVariable_Check(o)) return &THPVariable_Unpack(o);
-    PyErr_Format(PyExc_TypeError, "%s must be a torch.Tensor", what);
-    return nullptr;
-}
-
-// An address given as an int or None (0); false with an error set otherwise
-bool address_of(PyObject *o, void **out)
-{
-    *out = nullptr;
-    if (o == Py_None) return true;
-    *out = PyLong_AsVoidPtr(o);
-    return !PyErr_Occurred();
-}
-
-// The stream of a call: a named one, or (None) the current one
-struct CallStream {
-    void *address;
-    bool named;
-};
-
-bool stream_of(PyObject *o, CallStream *out)
-{
-    out->named = o != Py_None;
-    if (out->named) return address_of(o, &out->address);
-    out->address = c10::hip::getCurrentHIPStream().stream();
-    return true;
-}
 
 // x: `batch` rows of K activations or more
 bool activations_ok(const at::Tensor &x, int64_t K)
@@ -58,40 +22,11 @@ bool activations_ok(const at::Tensor &x, int64_t K)
     return false;
 }
 
-// Bytes of a given tensor's memory from its first element on; 0 for memory that the GPU cannot write
-int64_t room(const at::Tensor &t)
-{
-    if (!t.is_cuda() && !t.is_pinned()) return 0;
-    return (int64_t)t.storage().nbytes() - t.storage_offset() * (int64_t)t.element_size();
-}
-
 bool output_ok(const at::Tensor &y, int64_t batch, int64_t M)
 {
     if (room(y) >= batch * M * 2) return true;
     PyErr_SetString(PyExc_AssertionError, "y must hold batch x M float16 values on the GPU");
     return false;
-}
-
-// Memory that work on the call's stream writes.  The caching allocator hands a block out in the order of the stream that is current,
-// and again as soon as it is released there.  For a named stream it is therefore asked in that stream's order: from the current
-// stream's blocks, work still queued there could use a block that the call overwrites, or be given one that the call still
-// uses.  A tensor that is returned is read by the caller on the current stream, so its release waits for that one too.
-at::Tensor allocate(at::IntArrayRef sizes, at::ScalarType type, at::Device device, const CallStream &stream, bool returned)
-{
-    const auto options = at::TensorOptions().dtype(type).device(device);
-    if (!stream.named) return at::empty(sizes, options);
-    const auto current = c10::hip::getCurrentHIPStreamMasqueradingAsCUDA(device.index());
-    if (current.stream() == stream.address) return at::empty(sizes, options);
-    struct Restore {
-        decltype(current) &stream;
-        ~Restore() { c10::hip::setCurrentHIPStreamMasqueradingAsCUDA(stream); }
-    } restore{current};
-    c10::hip::setCurrentHIPStreamMasqueradingAsCUDA(
-        stream.address ? c10::hip::getStreamFromExternalMasqueradingAsCUDA(static_cast<hipStream_t>(stream.address), current.device_index())
-                       : c10::hip::getDefaultHIPStreamMasqueradingAsCUDA(current.device_index()));
-    at::Tensor t = at::empty(sizes, options);
-    if (returned) t.record_stream(current.unwrap());
-    return t;
 }
 
 // empty(sizes, half, device index, stream) -> a float16 (half != 0) or uint8 tensor that work on the named stream writes
@@ -192,6 +127,11 @@ PyMethodDef methods[] = {
     {"gemv", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(gemv)), METH_FASTCALL, nullptr},
     {"empty", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(empty)), METH_FASTCALL, nullptr},
     {"gemm", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(gemm)), METH_FASTCALL, nullptr},
+    {"cache_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(cache_append)), METH_FASTCALL, nullptr},
+    {"cache_read", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(cache_read)), METH_FASTCALL, nullptr},
+    {"attention_cached", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(attention_cached)), METH_FASTCALL, nullptr},
+    {"attention_prompt", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(attention_prompt)), METH_FASTCALL, nullptr},
+    {"verify", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(verify)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,461 @@
+"""GPU tests of the decoder operators against plain 64-bit forms: sizes, layouts, masks and values at which they can go wrong."""
+import numpy as np
+import pytest
+import torch
+
+import decode_util as U
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2402_10517_amd import binding
+    return binding
+
+
+def normal(seed, *shape, outlier=False):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    x = torch.randn(shape, generator=g, device="cuda", dtype=torch.float16)
+    if outlier:
+        x[..., shape[-1] // 3] *= 8
+    return x
+
+
+# ------------------------------------------------------------------------------------------------ append
+
+
+def full_cache(B, pages, G, D, page):
+    """A cache whose memory holds the bytes that hurt most: NaN scales, full codes."""
+    cache = B.KVCache(pages, G, D, page_tokens=page)
+    cache.buf.fill_(255)
+    return cache
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("tokens,H,G,rot,inter,page", [(1, 1, 1, 0, False, 16), (1, 32, 32, 1.0, False, 64), (17, 3, 1, 1.0, True, 16), (5, 40, 8, 0.5, False, 32),
+                                                       (33, 7, 7, 0.25, True, 128), (130, 64, 8, 1.0, False, 256), (3, 0, 5, 1.0, True, 16)])
+def test_append_rotates_and_rounds(B, D, tokens, H, G, rot, inter, page):
+    table, pages = U.page_table([tokens + 5], page, seed=tokens)
+    slots = U.slots_of(table, page, 0, 5, tokens + 5)
+    slots[tokens // 2] = -1                                     # a token that is not kept
+    q = normal(1, tokens, H, D) if H else None
+    k, v = normal(2, tokens, G, D, outlier=True), normal(3, tokens, G, D)
+    v[0, 0] = 1.5                                               # a row of one value: its step is 0
+    k[-1, -1] *= 2.0 ** -14                                     # subnormal values and steps
+    rotary = B.rotary_table(300, int(rot * D)) if rot else None
+    positions = torch.randint(0, 300, (tokens,), generator=torch.Generator().manual_seed(4))
+    cache = full_cache(B, pages, G, D, page)
+    before = cache.buf.clone()
+    q_out, k_out = B.ap_cache_append(cache, k, v, slots.cuda(), q=q, positions=positions.cuda() if rot else None, rotary=rotary, interleaved=inter)
+    for x, got in ((q, q_out), (k, k_out)):
+        if x is None:
+            assert got is None
+            continue
+        want = U.rotate(x, rotary, positions.cuda(), inter)
+        # two products and a sum in binary32 of values up to the larger of the pair, then one rounding
+        U.check(got, want, U.HALF_EPS16 * want.abs() + 4 * U.EPS32 * x.double().abs().amax(-1, keepdim=True) + U.SUBNORMAL16, "rotated")
+    k_got, v_got = B.ap_cache_read(cache, slots.cuda())
+    kept = (slots >= 0).cuda()[:, None, None]
+    for x, got in ((k_out, k_got), (v, v_got)):
+        codes, low, step = U.codes_of(x)
+        assert torch.equal(got, torch.where(kept, low + step * codes, torch.zeros_like(low)).half())
+    # only the bytes of the tokens that were kept have changed
+    changed = int((cache.buf != before).sum())
+    assert changed <= int(kept.sum()) * G * (D + 8)
+    assert changed >= int(kept.sum()) * G * (D + 8) // 2
+
+
+def test_append_strided_in_place_and_in_any_order(B):
+    T, H, G, D, page = 29, 6, 2, 128, 16
+    x = normal(5, T, H + 2 * G, D)
+    q, k, v = x[:, :H], x[:, H:H + G], x[:, H + G:]
+    rotary = B.rotary_table(64, D)
+    positions = torch.arange(T).cuda()
+    slots = torch.randperm(4 * page, generator=torch.Generator().manual_seed(1))[:T].cuda()
+    one, two = full_cache(B, 4, G, D, page), full_cache(B, 4, G, D, page)
+    q1, k1 = B.ap_cache_append(one, k.contiguous(), v.contiguous(), slots, q=q.contiguous(), positions=positions, rotary=rotary)
+    heads_first = q.transpose(0, 1).contiguous().transpose(0, 1)        # (heads, tokens, head_dim) in memory
+    back = torch.arange(T - 1, -1, -1).cuda()
+    q2, k2 = B.ap_cache_append(two, k[back], v[back], slots[back], q=heads_first[back], positions=positions[back], rotary=rotary)
+    assert torch.equal(q1, q2[back]) and torch.equal(k1, k2[back]) and torch.equal(one.buf, two.buf)
+    q3, k3 = B.ap_cache_append(two, k, v, slots, q=q, positions=positions, rotary=rotary, q_out=q, k_out=k)
+    assert q3 is not None and torch.equal(x[:, :H], q1) and torch.equal(x[:, H:H + G], k1) and torch.equal(one.buf, two.buf)
+
+
+def test_append_values_out_of_range(B):
+    G, D, page = 2, 64, 16
+    cache = full_cache(B, 2, G, D, page)
+    before = cache.buf.clone()
+    k, v = normal(1, 5, G, D), normal(2, 5, G, D)
+    far = torch.tensor([-1, 2 * page, -2 ** 63, 2 ** 62, 2 ** 40], device="cuda")
+    B.ap_cache_append(cache, k, v, far)
+    assert torch.equal(cache.buf, before)
+    kz, vz = B.ap_cache_read(cache, far)
+    assert not kz.any() and not vz.any()
+    # a position outside the table: its rotated channels are NaN, the others stay
+    rotary = B.rotary_table(8, 32)
+    _, k_out = B.ap_cache_append(cache, k, v, far, positions=torch.tensor([7, 8, -1, 2 ** 62, 0], device="cuda"), rotary=rotary)
+    lost = torch.tensor([False, True, True, True, False], device="cuda")
+    assert torch.equal(torch.isnan(k_out[..., :32]).all(-1).all(-1), lost) and not torch.isnan(k_out[~lost]).any()
+    assert torch.equal(k_out[..., 32:], k[..., 32:])
+    # rows with an infinity or NaN read back as NaN, and only they; extreme finite values do not overflow
+    k[1, 0, 5], v[2, 1, 63], v[3, 0, 0] = float("inf"), float("nan"), float("-inf")
+    k[4, 0, :2] = torch.tensor([65504.0, -65504.0])
+    slots = torch.arange(5, device="cuda") + 11                 # across the end of the first page
+    B.ap_cache_append(cache, k, v, slots)
+    kz, vz = B.ap_cache_read(cache, slots)
+    for x, got in ((k, kz), (v, vz)):
+        assert torch.equal(torch.isnan(got).all(-1), ~torch.isfinite(x).all(-1)) and torch.equal(torch.isnan(got).any(-1), torch.isnan(got).all(-1))
+    assert torch.isfinite(kz[4]).all()
+    empty = k[:0]
+    assert B.ap_cache_append(cache, empty, empty, slots[:0])[1].shape == (0, G, D) and B.ap_cache_read(cache, slots[:0])[0].shape == (0, G, D)
+
+
+# ------------------------------------------------------------------------------------------------ attention over the cache
+
+
+def cached_case(B, lengths, queries, H, G, D, page, seed=0, scale=None, uniform=False, max_length=None, spoil=None, view=False, width=None, base=0):
+    """Runs one call and checks every row.  base: pages in front of the case's own, for addresses far into the cache."""
+    table, pages = U.page_table(lengths, page, seed=seed, width=width)
+    table = torch.where(table >= 0, table + base, table)
+    cache = B.KVCache(pages + base, G, D, page_tokens=page)
+    first = base * (cache.buf.numel() // (pages + base))
+    cache.buf[first:].fill_(255)
+    slots = torch.cat([U.slots_of(table, page, i, 0, n) for i, n in enumerate(lengths)])
+    total = len(slots)
+    k, v = normal(seed + 1, total, G, D, outlier=True), normal(seed + 2, total, G, D)
+    if spoil:
+        spoil(k, v)
+    B.ap_cache_append(cache, k, v, slots.cuda())
+    T = sum(queries)
+    q = normal(seed + 3, T, H + 2, D)[:, 1:H + 1] if view else normal(seed + 3, T, H, D)
+    st = U.starts(queries)
+    scale = D ** -0.5 if scale is None else scale
+    args = dict(q_starts=None if uniform else st.cuda(), scale=scale, max_length=max_length)
+    lens = torch.tensor(lengths, dtype=torch.int32).cuda()
+    out = B.ap_attention_cached(cache, q, table.cuda(), lens, **args)
+    again = B.ap_attention_cached(cache, q, table.cuda(), lens, **args)
+    assert torch.equal(out.view(torch.int16), again.view(torch.int16))
+    at, worst = 0, 0.0
+    for i, (n, m) in enumerate(zip(queries, lengths)):
+        m = m if max_length is None else min(m, max_length)
+        rows = slice(int(st[i]), int(st[i]) + n)
+        kk, vv = k[at:at + m], v[at:at + m]
+        _, kl, ks = U.codes_of(kk)
+        _, vl, vs = U.codes_of(vv)
+        sees = m - n + 1 + torch.arange(n)
+        # values enter the sums as low + step (offset + code) with an offset up to 128: the magnitudes that bound the rounding of the sums
+        want, bound = U.attention(q[rows].double(), U.cache_values(kk), U.cache_values(vv), scale, sees,
+                                  (kl.abs() + 143 * ks).double().expand(-1, -1, D), (vl.abs() + vs * 15).double().expand(-1, -1, D))
+        worst = max(worst, U.check(out[rows], want, bound, "sequence %d of %d keys" % (i, m)))
+        at += lengths[i]
+    return out, worst
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H,G", [(1, 1), (3, 3), (8, 1), (14, 2), (20, 1), (33, 1), (32, 32)])
+def test_cached_head_layouts(B, H, G, D):
+    cached_case(B, [1, 2, 15, 16, 17, 31, 32, 33, 130, 0, 257], [1] * 11, H, G, D, 16, seed=H, uniform=True)
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
+@pytest.mark.parametrize("D", [64, 128])
+def test_cached_pages_and_lengths(B, page, D):
+    cached_case(B, [page - 1, page, page + 1, 511, 512, 513, 1023, 1025, 2049, 1], [1, 2, 1, 5, 1, 3, 1, 0, 4, 1], 8, 2, D, page, seed=page)
+
+
+@pytest.mark.parametrize("queries", [2, 5, 8, 17, 40])
+def test_cached_many_queries(B, queries):
+    # some sequences are shorter than their queries: the first ones see nothing
+    cached_case(B, [3, 100, 0, 700, queries, 1, 1500], [queries] * 7, 16, 4, 128, 64, seed=queries, uniform=True, view=True)
+    cached_case(B, [3, 100, 0, 700, queries, 1], [queries, 1, 2, 0, queries, 3], 6, 2, 64, 16, seed=queries)
+
+
+def test_cached_long(B):
+    cached_case(B, [70001, 3], [1, 1], 8, 1, 128, 64, uniform=True)
+    cached_case(B, [33000], [3], 4, 2, 64, 16, uniform=True)
+
+
+def test_cached_scales_and_bounds(B):
+    for scale in (0.0, -0.3, 1.0, 1e-6):
+        cached_case(B, [100, 40], [1, 2], 4, 2, 128, 32, scale=scale)
+    cached_case(B, [300, 40, 128], [1, 2, 1], 4, 2, 128, 32, max_length=128)     # longer sequences are cut at max_length
+    cached_case(B, [300, 40], [1, 2], 4, 2, 64, 16, width=400)                   # a table much wider than what it holds
+    cached_case(B, [0, 0], [1, 2], 4, 2, 64, 16)
+
+
+def test_cached_nan_reaches_only_rows_that_see_it(B):
+    def spoil(k, v):
+        v[90, 0, 3] = float("inf")        # token 90 of 96: of 8 queries the last 6 see it
+        k[95, 1, 0] = float("nan")        # the last token: only the last query sees it
+    out, _ = cached_case(B, [96], [8], 4, 2, 128, 32, spoil=spoil)
+    bad = torch.isnan(out).all(-1)
+    assert bad[:, :2].any(1).tolist() == [False] * 2 + [True] * 6 and bad[:, 2:].any(1).tolist() == [False] * 7 + [True]
+
+
+def test_cached_pages_outside_the_cache_hold_nothing(B):
+    G, D, page = 2, 128, 16
+    cache = full_cache(B, 4, G, D, page)
+    k, v = normal(1, 32, G, D), normal(2, 32, G, D)
+    B.ap_cache_append(cache, k, v, torch.arange(32).cuda())
+    q = normal(3, 1, 4, D)
+    table = torch.tensor([[0, -1, 1, 4, 2 ** 31 - 1]], dtype=torch.int32).cuda()
+    out = B.ap_attention_cached(cache, q, table, torch.tensor([80], dtype=torch.int32).cuda())
+    want = B.ap_attention_cached(cache, q, torch.tensor([[0, 1]], dtype=torch.int32).cuda(), torch.tensor([32], dtype=torch.int32).cuda())
+    assert (out.float() - want.float()).abs().max() <= 2.0 ** -9 * want.float().abs().max()
+    gone = B.ap_attention_cached(cache, q, torch.full_like(table, -7), torch.tensor([80], dtype=torch.int32).cuda())
+    assert not gone.any()
+    # lengths and starts that make no sense: no fault, and rows of no sequence stay as they were
+    q = normal(4, 6, 4, D)
+    out = torch.full_like(q, 7.0)
+    bad = torch.tensor([0, 2, 2, -5, 4], dtype=torch.int32).cuda()
+    B.ap_attention_cached(cache, q, table.expand(4, -1).contiguous(), torch.tensor([-3, 2 ** 31 - 1, 1, 16], dtype=torch.int32).cuda(), q_starts=bad, out=out)
+    assert not out[:2].any() and (out[4:] == 7).all()
+
+
+def test_cached_offsets_beyond_32_bits(B):
+    # 2.2 million tokens in front: the case's pages lie beyond 4 GiB
+    cached_case(B, [200, 77], [1, 2], 32, 16, 128, 64, base=35000)
+
+
+def test_cached_on_a_named_stream(B):
+    table, pages = U.page_table([600], 64)
+    cache = full_cache(B, pages, 2, 128, 64)
+    k, v = normal(1, 600, 2, 128), normal(2, 600, 2, 128)
+    slots = U.slots_of(table, 64, 0, 0, 600).cuda()
+    q, tables, lens = normal(3, 1, 8, 128), table.cuda(), torch.tensor([600], dtype=torch.int32).cuda()
+    B.ap_cache_append(cache, k, v, slots)
+    want = B.ap_attention_cached(cache, q, tables, lens)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        cache.buf.fill_(255)
+        side.wait_stream(torch.cuda.current_stream())
+        B.ap_cache_append(cache, k, v, slots, stream=side)
+        out = B.ap_attention_cached(cache, q, tables, lens, stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(out, want)
+
+
+# ------------------------------------------------------------------------------------------------ attention over prompts
+
+
+def prompt_case(B, q_counts, k_counts, H, G, D, seed=0, scale=None, fused=False, spoil=None, tensors=None):
+    T, M = sum(q_counts), sum(k_counts)
+    if tensors:
+        q, k, v = tensors
+    elif fused:
+        x = normal(seed, T, H + 2 * G, D)
+        q, k, v = x[:, :H], x[:, H:H + G], x[:, H + G:]
+    else:
+        q, k, v = normal(seed, T, H, D), normal(seed + 1, M, G, D), normal(seed + 2, M, G, D)
+    if spoil:
+        spoil(k, v)
+    qs, ks = U.starts(q_counts), U.starts(k_counts)
+    scale = D ** -0.5 if scale is None else scale
+    out = B.ap_attention_prompt(q, k, v, qs.cuda(), ks.cuda(), scale=scale)
+    again = B.ap_attention_prompt(q, k, v, qs.cuda(), ks.cuda(), scale=scale)
+    assert torch.equal(out.view(torch.int16), again.view(torch.int16))
+    worst = 0.0
+    for i, (n, m) in enumerate(zip(q_counts, k_counts)):
+        rows, keys = slice(int(qs[i]), int(qs[i]) + n), slice(int(ks[i]), int(ks[i]) + m)
+        want, bound = U.attention(q[rows].double(), k[keys].double(), v[keys].double(), scale, m - n + 1 + torch.arange(n))
+        worst = max(worst, U.check(out[rows], want, bound, "sequence %d, %d of %d" % (i, n, m)))
+    return out, worst
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H,G", [(1, 1), (4, 4), (8, 1), (14, 2), (20, 1)])
+def test_prompt_lengths(B, H, G, D):
+    n = [1, 2, 15, 16, 17, 0, 31, 32, 33, 63, 64, 65, 127, 128, 129, 200]
+    prompt_case(B, n, n, H, G, D, seed=H, fused=True)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_prompt_pieces(B, D):
+    prompt_case(B, [1, 5, 64, 130, 1, 0, 33], [300, 77, 1000, 131, 1, 40, 2000], 6, 2, D)
+    # more queries than keys: the first ones see nothing; none at all
+    prompt_case(B, [70, 200, 3, 1], [64, 3, 0, 0], 6, 2, D)
+
+
+def test_prompt_long(B):
+    prompt_case(B, [2500], [2500], 2, 1, 128)
+    prompt_case(B, [1100, 900], [5000, 901], 5, 1, 64)
+
+
+def test_prompt_scales(B):
+    for scale in (0.0, -0.2, 1.0, 30.0):
+        prompt_case(B, [100, 40], [100, 40], 2, 1, 128, scale=scale)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("at", [0, 5, 63, 64, 70, 149])
+def test_prompt_values_that_are_not_seen_do_not_matter(B, D, at):
+    def spoil(k, v):
+        v[at, 0, 3], v[at, 0, 9], v[at, 0, 17] = float("inf"), float("-inf"), float("nan")
+        k[150 + 20, 1, 5] = float("nan")                        # the second sequence's token 20
+        v[150 + 30, 1] = 65504.0
+    out, _ = prompt_case(B, [150, 60, 1], [150, 60, 1], 4, 2, D, spoil=spoil)
+    bad = ~torch.isfinite(out[:, :2]).all(-1).all(-1)
+    assert bad.tolist() == [at <= i < 150 for i in range(211)]
+    assert (~torch.isfinite(out[:, 2:]).all(-1).all(-1)).tolist() == [170 <= i < 210 for i in range(211)]
+
+
+def test_prompt_strides_and_offsets(B):
+    T, H, G, D = 90, 4, 2, 128
+    q, k, v = normal(1, H, T, D).transpose(0, 1), normal(2, G, T, D).transpose(0, 1), normal(3, T, G, D)
+    prompt_case(B, [50, 40], [50, 40], H, G, D, tensors=(q, k, v.flip(0).contiguous()))
+    # rows of the keys 2^24 elements apart: offsets beyond 2^32 bytes
+    far = torch.zeros(T << 24, dtype=torch.float16, device="cuda").as_strided((T, G, D), (1 << 24, D, 1))
+    far.copy_(k)
+    prompt_case(B, [50, 40], [50, 40], H, G, D, tensors=(q, far, v))
+
+
+def test_prompt_starts_that_make_no_sense(B):
+    q, k, v = normal(1, 40, 2, 64), normal(2, 40, 2, 64), normal(3, 40, 2, 64)
+    out = torch.full_like(q, 7.0)
+    B.ap_attention_prompt(q, k, v, torch.tensor([0, 10, 5, 2 ** 31 - 1, -4], dtype=torch.int32).cuda(),
+                          torch.tensor([-9, 10, 2 ** 31 - 1, 3, 50], dtype=torch.int32).cuda(), out=out)
+    torch.cuda.synchronize()
+    empty = q[:0]
+    assert B.ap_attention_prompt(empty, k, v, torch.zeros(2, dtype=torch.int32).cuda(), torch.tensor([0, 40], dtype=torch.int32).cuda()).shape == (0, 2, 64)
+
+
+# ------------------------------------------------------------------------------------------------ verification
+
+
+def verify_plain(target, draft, drafted, uniform, noise, counts):
+    """Token by token, on the host."""
+    S, N, V = draft.shape
+    tokens, accepted = np.full((S, N + 1), -1, dtype=np.int64), np.zeros(S, dtype=np.int32)
+    target, draft = target.astype(np.float32), draft.astype(np.float32)
+    for s in range(S):
+        count = min(max(int(counts[s]), 0), N)
+        n = 0
+        while n < count and 0 <= drafted[s, n] < V and uniform[s, n] * draft[s, n, drafted[s, n]] < target[s, n, drafted[s, n]]:
+            n += 1
+        def race(w):
+            with np.errstate(all="ignore"):
+                ratio = w / noise[s]
+            ok = (w > 0) & (ratio >= 0)
+            return int(np.argmax(np.where(ok, ratio, -1))) if ok.any() else -1
+        won = race(target[s, n] - draft[s, n]) if n < count else -1
+        if won < 0:
+            won = race(target[s, n])
+        tokens[s, :n], tokens[s, n], accepted[s] = drafted[s, :n], won, n
+    return tokens, accepted
+
+
+def verify_inputs(S, N, V, half, seed):
+    rng = np.random.default_rng(seed)
+    logits = rng.normal(size=(S, N + 1, V)) * 2
+    def softmax(x):
+        e = np.exp(x - x.max(-1, keepdims=True))
+        return e / e.sum(-1, keepdims=True)
+    target = softmax(logits).astype(np.float16 if half else np.float32)
+    draft = softmax(logits[:, :N] + rng.normal(size=(S, N, V)) * 0.5).astype(target.dtype)
+    drafted = rng.integers(0, V, size=(S, N))
+    for s in range(S):
+        for i in range(N):
+            if rng.random() < 0.8:
+                drafted[s, i] = draft[s, i].argmax()
+    return target, draft, drafted, rng.random((S, N)).astype(np.float32), rng.exponential(size=(S, V)).astype(np.float32)
+
+
+def check_verify(B, target, draft, drafted, uniform, noise, counts=None):
+    S, N, _ = draft.shape
+    d = [torch.from_numpy(np.ascontiguousarray(x)).cuda() for x in (target, draft, drafted, uniform, noise)]
+    tokens, accepted = B.ap_verify(*d, counts=None if counts is None else torch.tensor(counts, dtype=torch.int32).cuda())
+    want = verify_plain(target, draft, drafted, uniform, noise, [N] * S if counts is None else counts)
+    assert np.array_equal(tokens.cpu().numpy(), want[0]) and np.array_equal(accepted.cpu().numpy(), want[1])
+    return want
+
+
+@pytest.mark.parametrize("half", [False, True])
+@pytest.mark.parametrize("S,N,V", [(1, 1, 1), (1, 4, 32000), (3, 2, 7), (5, 7, 255), (7, 3, 257), (64, 4, 1001), (2, 8, 50257), (300, 1, 33), (1, 1, 131071)])
+def test_verify(B, half, S, N, V):
+    inputs = verify_inputs(S, N, V, half, seed=S * 1000 + V)
+    check_verify(B, *inputs)
+    counts = np.random.default_rng(V).integers(-1, N + 2, size=S)
+    check_verify(B, *inputs, counts=counts)
+
+
+@pytest.mark.parametrize("half", [False, True])
+def test_verify_edges(B, half):
+    target, draft, drafted, uniform, noise = verify_inputs(8, 3, 1003, half, seed=5)
+    uniform[0] = 0.0                                            # accepts whatever the target can produce
+    drafted[1, 0], drafted[2, 1] = -1, 1003                     # tokens outside the vocabulary
+    draft[3] = target[3, :3]
+    uniform[3] = 0.999                                          # equal probabilities: all are accepted
+    draft[4, 0] = target[4, 0]
+    uniform[4, 0] = 1.0                                         # refused where no token has more than its draft: from the target itself
+    target[5] = 0
+    target[5, :, 77] = 1                                        # one token only, refused until it comes
+    noise[6, 10:20] = 0.0                                       # infinite ratios: the lowest of equals
+    noise[6, 20] = float("nan")
+    target[7], draft[7] = 0, 0                                  # nothing to choose from
+    want = check_verify(B, target, draft, drafted, uniform, noise)
+    assert want[0][7, 0] == -1 and (want[0][5][want[1][5]] == 77)
+    target[:] = np.float32(1 / 1003)
+    noise[:] = 1.0                                              # all equal: the lowest index
+    draft[:] = 0
+    want = check_verify(B, target, draft, drafted, uniform, noise)
+    assert want[0][0, want[1][0]] == 0
+    check_verify(B, target, draft, drafted, uniform, noise, counts=[0] * 8)
+    check_verify(B, target[:, :1], draft[:, :0], drafted[:, :0], uniform[:, :0], noise)      # no drafts: a plain sample
+
+
+def test_verify_tokens_follow_the_target(B):
+    # a small vocabulary many times over: the first token's frequencies are the target's
+    S, V = 20000, 5
+    rng = np.random.default_rng(3)
+    p, q = np.array([0.5, 0.2, 0.2, 0.1, 0.0], np.float32), np.array([0.1, 0.4, 0.2, 0.1, 0.2], np.float32)
+    drafted = rng.choice(V, size=(S, 1), p=q / q.sum())
+    d = [np.broadcast_to(p, (S, 2, V)), np.broadcast_to(q, (S, 1, V)), drafted, rng.random((S, 1)).astype(np.float32),
+         rng.exponential(size=(S, V)).astype(np.float32)]
+    tokens, _ = B.ap_verify(*[torch.from_numpy(np.ascontiguousarray(x)).cuda() for x in d])
+    share = np.bincount(tokens[:, 0].cpu().numpy(), minlength=V) / S
+    assert np.abs(share - p).max() < 5 * 0.5 / S ** 0.5         # five standard deviations of a share
+
+
+# ------------------------------------------------------------------------------------------------ all of them
+
+
+def test_calls_in_a_graph(B):
+    G, D, page, H = 2, 128, 16, 8
+    table, pages = U.page_table([400, 300], page)
+    cache = full_cache(B, pages, G, D, page)
+    k, v = normal(1, 700, G, D), normal(2, 700, G, D)
+    old = torch.cat([U.slots_of(table, page, 0, 0, 400), U.slots_of(table, page, 1, 0, 300)]).cuda()
+    new = torch.cat([U.slots_of(table, page, 0, 399, 400), U.slots_of(table, page, 1, 299, 300)]).cuda()
+    rotary, positions = B.rotary_table(512, D), torch.tensor([399, 299]).cuda()
+    x = normal(3, 2, H + 2 * G, D)
+    lens, tables, starts = torch.tensor([400, 300], dtype=torch.int32).cuda(), table.cuda(), torch.tensor([0, 1, 2], dtype=torch.int32).cuda()
+    p = [torch.from_numpy(a).cuda() for a in verify_inputs(2, 3, 5000, False, 1)]
+
+    def step():
+        q, kk = B.ap_cache_append(cache, x[:, H:H + G], x[:, H + G:], new, q=x[:, :H], positions=positions, rotary=rotary)
+        return (q, kk, B.ap_attention_cached(cache, q, tables, lens), B.ap_attention_prompt(q, kk, x[:, H + G:], starts)) + B.ap_verify(*p)
+
+    B.ap_cache_append(cache, k, v, old)
+    step()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for seed in (7, 8, 9):
+        x.copy_(normal(seed, 2, H + 2 * G, D))
+        p[3].copy_(torch.rand_like(p[3]))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [o.clone() for o in outs]
+        cache.buf.fill_(255)
+        B.ap_cache_append(cache, k, v, old)
+        for a, b in zip(got, step()):
+            assert torch.equal(a, b)
