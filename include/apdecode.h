@@ -74,13 +74,14 @@ ap_status ap_cache_append(const ap_cache *c, const ap_append *a, void *stream);
 ap_status ap_cache_read(const ap_cache *c, const int64_t *slots, int64_t tokens, void *k_out, void *v_out, void *stream);
 
 /*
- * Attention of new tokens over the cache: out[i] = sum_j softmax_j(scale * q[i] . k[j]) v[j].
+ * Attention of new tokens (tokens * heads < 2^31 - 256) over the cache: out[i] = sum_j softmax_j(scale * q[i] . k[j]) v[j].
  *   q          tokens rows of heads heads; the tokens of a sequence are adjacent
- *   q_starts   device, sequences + 1: sequence s has the tokens q_starts[s] .. q_starts[s + 1] - 1; not descending.  NULL: tokens / sequences each
+ *   q_starts   device, sequences + 1: sequence s has the tokens q_starts[s] .. q_starts[s + 1] - 1; not descending (a sequence
+ *              whose two starts descend or leave 0 .. tokens has no tokens).  NULL: tokens / sequences each
  *   lengths    device, sequences: the keys of a sequence, its new tokens included (they have been appended): token i of n sees the first
  *              lengths[s] - n + 1 + i keys.  A token that sees none gets zeros.  Lengths above max_length are taken as max_length
  *   tables     device, sequences x table_width page numbers; a page outside the cache holds no keys
- *   max_length host's bound of the lengths, up to table_width * page_tokens: decides how the work is divided
+ *   max_length host's bound of the lengths, up to table_width * page_tokens and 2^30: decides how the work is divided
  *   out        device, tokens x heads x head_dim, contiguous, 16-byte aligned; only the tokens of q_starts are written
  *   work       device, ap_attention_cached_size bytes, 16-byte aligned; may be NULL where that is 0
  * Scores, softmax and sums are binary32.  Long sequences are divided among workgroups and joined by a second launch.
@@ -101,9 +102,9 @@ ap_status ap_attention_cached(const ap_cache *c, const ap_cached *a, void *strea
 
 /*
  * Causal attention over packed sequences: sequence s has the queries q_starts[s] .. q_starts[s + 1] - 1 and the keys k_starts[s] .. k_starts[s + 1] - 1
- * (device, sequences + 1 each, not descending); its last query sees its last key.  Query i of n sees the first m - n + 1 + i of m keys; one
+ * (device, sequences + 1 each, not descending; a sequence whose two starts descend or leave the rows has none); its last query sees its last key.  Query i of n sees the first m - n + 1 + i of m keys; one
  * that sees none gets zeros, as does one whose scores are all -inf.  What a query does not see does not reach it, NaN and infinities included.
- *   q; k, v    tokens rows of heads heads; keys rows of kv_heads heads
+ *   q; k, v    tokens rows of heads heads (tokens * heads < 2^31 - 256); keys rows of kv_heads heads
  *   out        device, tokens x heads x head_dim, contiguous, 16-byte aligned; only the tokens of q_starts are written
  * Scores, softmax and sums are binary32; the weights of the values are rounded to binary16.
  */

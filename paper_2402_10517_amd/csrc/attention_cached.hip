@@ -1,89 +1,410 @@
-// Attention of new tokens over the 4-bit paged cache.
+// Attention of new tokens over the 4-bit paged cache, on the matrix cores.
+//
+// A workgroup takes a tile of query rows (token, head of the group) of one sequence and key head and a range of its keys; a wave takes 32 keys at a time:
+//   S^T = C Q^T with C the key codes, v_mfma_f32_16x16x32_f16: codes 0..15 enter as binary16 64 + code (the nibble set into the mantissa of 64: a shift
+//         and one v_and_or for two), exact, and s = scale (step (S - 64 sum q) + low sum q) takes the offset back in binary32;
+//   O^T = V^T P^T, v_mfma_f32_16x16x32_bf16: codes enter as bfloat16 128 + code, the weights as p * step in two bfloat16 parts (high + rest:
+//         16 bits of mantissa, and the range of binary32 for any step); what is the same for all channels of a row, sum p low - 128 sum p step, is one number.
+// With keys as rows and queries as columns a lane holds scores of one query row throughout, the scores' registers are the weights' operand as
+// they stand (the order of the keys inside a product is free, and the cache's value layout follows it), and the statistics are one number per lane.
+// The running maximum moves only when a score exceeds it by 2^8: weights stay below 2^8 and the accumulators are seldom rescaled.
+//
+// Bound by HBM: a key of one head is D + 8 bytes, 4 (heads / kv_heads) D operations.  A wave has its next 32 keys' loads in flight while it works.
 #include "attention_rows.h"
 
 namespace apgemv {
 
 namespace {
 
+typedef __bf16 bf8_t __attribute__((ext_vector_type(8)));
+
 struct CachedArgs {
     CacheShape cache;
     const _Float16 *q;
-    int64_t q_token, q_head, tokens, table_width, max_length;
+    int64_t q_token, q_head, table_width;
     const int32_t *q_starts, *lengths, *tables;
-    int heads, sequences;
+    int tokens, heads, sequences, max_length;
+    int items, splits, chunk; // row tiles (at most), ranges of `chunk` keys
     float scale;
     _Float16 *out;
+    float *part;  // splits x rows x D: sums of range s
+    float2 *stat; // splits x rows: their maximum and sum of weights
 };
 
-template <int D> struct CachedRows {
-    typedef CacheLayout<D> L;
-    CacheShape cache;
-    const int32_t *table;
-    int head;
-    __device__ const uint8_t *block(int64_t j, int *t, bool *known) const
-    {
-        const int page = table[j >> cache.log_page];
-        *t = (int)(j & ((1 << cache.log_page) - 1));
-        *known = page >= 0 && page < cache.pages;
-        return L::block(cache, *known ? page : 0, head);
-    }
-    __device__ float score(int64_t j, const float *q) const
-    {
-        int t;
-        bool known;
-        const uint8_t *b = block(j, &t, &known);
-        const _Float16 *p = reinterpret_cast<const _Float16 *>(b + L::key_scale(cache.log_page, t));
-        float sum = 0;
-        for (int d = 0; d < D; ++d) sum += q[d] * ((float)p[0] + (float)p[1] * (b[L::key(t) + d / 2] >> (4 * (d & 1)) & 15));
-        return known ? sum : -INFINITY;
-    }
-    __device__ float value(int64_t j, int d) const
-    {
-        int t;
-        bool known;
-        const uint8_t *b = block(j, &t, &known);
-        const _Float16 *p = reinterpret_cast<const _Float16 *>(b + L::value_scale(cache.log_page, t));
-        const int c = d / (D / 16), i = d % (D / 16);
-        const int code = *reinterpret_cast<const uint16_t *>(b + L::value(cache.log_page, t, c, i / 4)) >> (4 * (i & 3)) & 15;
-        return known ? (float)p[0] + (float)p[1] * code : 0.0f;
-    }
-};
+constexpr int kThreads = 256;
+constexpr int kWaves = 4;
+constexpr int kTile = 32;                   // keys per wave and step
+constexpr int kStep = kTile * kWaves;       // keys per workgroup and step
+constexpr int kMaxChunk = 64 / 2 * kStep;   // a lane of a wave holds the page of one 16-key half: 32 steps
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kSlack = 8.0f;
 
-template <int D> __global__ __launch_bounds__(64) void attention_cached_kernel(const CachedArgs a)
+// Item -> sequence and row tile, where sequences have different numbers of tokens (64 lanes call together)
+__device__ __forceinline__ bool find_item(const CachedArgs &a, int rows_per_tile, int item, int *sequence, int *tile)
 {
-    const int64_t rows = a.tokens * a.heads;
-    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
-        const int64_t token = row / a.heads;
-        const int head = (int)(row - token * a.heads);
-        const int s = sequence_of(a.q_starts, token, a.tokens, a.sequences);
-        if (s < 0) continue;
-        int64_t begin, end;
-        token_range(a.q_starts, s, a.tokens, a.sequences, &begin, &end);
-        const int64_t length = a.lengths[s] < a.max_length ? a.lengths[s] : a.max_length;
-        const CachedRows<D> source{a.cache, a.tables + s * a.table_width, head / (a.heads / a.cache.kv_heads)};
-        attend_row<D>(source, length - (end - 1 - token), a.q + token * a.q_token + head * a.q_head, a.scale, a.out + row * D);
+    const int lane = threadIdx.x & 63, group = a.heads / a.cache.kv_heads;
+    int before = 0;
+    for (int first = 0; first < a.sequences; first += 64) {
+        int tiles = 0;
+        if (first + lane < a.sequences) {
+            int64_t begin, end;
+            token_range(a.q_starts, first + lane, a.tokens, a.sequences, &begin, &end);
+            tiles = (int)(((end - begin) * group + rows_per_tile - 1) / rows_per_tile);
+        }
+        int upto = tiles;
+        for (int d = 1; d < 64; d <<= 1) {
+            const int other = __shfl_up(upto, d);
+            if (lane >= d) upto += other;
+        }
+        const uint64_t found = __ballot(before + upto > item);
+        if (found) {
+            const int l = __builtin_ctzll(found);
+            *sequence = first + l;
+            *tile = item - before - (__shfl(upto, l) - __shfl(tiles, l));
+            return true;
+        }
+        before += __shfl(upto, 63);
     }
+    return false;
+}
+
+// Codes and (low, step) pairs of 16 keys as a lane (c = lane % 16, g = lane / 16) needs them: key c's channels g * D/4 .., the values of keys 4 g .. 4 g + 3
+// in channels c * D/16 .., the pairs of those four keys
+template <int D> struct Half {
+    typedef uint32_t words_t __attribute__((ext_vector_type(D / 32)));
+    words_t k, v;
+    uint4_t kp, vp;
+};
+
+template <int D> __device__ __forceinline__ Half<D> load_half(const uint8_t *block, int log_page, int t, int c, int g)
+{
+    typedef CacheLayout<D> L;
+    typedef typename Half<D>::words_t words_t;
+    Half<D> h;
+    h.k = *reinterpret_cast<const words_t *>(block + L::key(t) + c * L::kRow + g * (D / 8));
+    h.v = *reinterpret_cast<const words_t *>(block + L::value(log_page, t + 4 * g, c, 0));
+    h.kp = *reinterpret_cast<const uint4_t *>(block + L::key_scale(log_page, t + 4 * g));
+    h.vp = *reinterpret_cast<const uint4_t *>(block + L::value_scale(log_page, t + 4 * g));
+    return h;
+}
+
+__device__ __forceinline__ float low_of(uint32_t pair) { return (float)__builtin_bit_cast(_Float16, (uint16_t)pair); }
+__device__ __forceinline__ float step_of(uint32_t pair) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(pair >> 16)); }
+
+// 8 codes as binary16 64 + code, in the order 0 4 1 5 2 6 3 7
+__device__ __forceinline__ half8_t key_operand(uint32_t w)
+{
+    const uint4_t x = {(w << 4 & 0x00f000f0u) | 0x54005400u, (w & 0x00f000f0u) | 0x54005400u, (w >> 4 & 0x00f000f0u) | 0x54005400u,
+                       (w >> 8 & 0x00f000f0u) | 0x54005400u};
+    return __builtin_bit_cast(half8_t, x);
+}
+
+// Channel n of four keys of both halves as bfloat16 128 + code
+template <int D> __device__ __forceinline__ bf8_t value_operand(const Half<D> (&h)[2], int n)
+{
+    constexpr int kH = D / 64;
+    uint4_t x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = (h[i >> 1].v[(i & 1) * kH + n / 4] >> (4 * (n & 3)) & 0x000f000fu) | 0x43004300u;
+    return __builtin_bit_cast(bf8_t, x);
+}
+
+template <int D, int NR> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 64 ? 4 : 3 : 2) void attention_cached_kernel(const CachedArgs a)
+{
+    typedef CacheLayout<D> L;
+    constexpr int kSteps = D / 32;    // products of 32 channels per score
+    constexpr int kN = D / 16;        // channels of a lane's chunk
+    constexpr int kRows = 16 * NR;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
+    const int kv = a.cache.kv_heads, group = a.heads / kv;
+    const int head = blockIdx.x % kv, rest = blockIdx.x / kv;
+    const int item = rest % a.items, split = rest / a.items;
+    int sequence, tile;
+    if (!a.q_starts) {
+        const int tiles = a.items / a.sequences;
+        sequence = item / tiles;
+        tile = item - sequence * tiles;
+    } else if (!find_item(a, kRows, item, &sequence, &tile)) {
+        return;
+    }
+    sequence = __builtin_amdgcn_readfirstlane(sequence);
+    tile = __builtin_amdgcn_readfirstlane(tile);
+    int64_t begin64, end64;
+    token_range(a.q_starts, sequence, a.tokens, a.sequences, &begin64, &end64);
+    const int begin = (int)begin64, n = (int)(end64 - begin64);
+    int length = a.lengths[sequence];
+    length = length < 0 ? 0 : length > a.max_length ? a.max_length : length;
+    // keys that the tile's first and last row see
+    const int first_token = tile * kRows / group, last = (tile * kRows + kRows - 1) / group, last_token = last < n ? last : n - 1;
+    const int sees_least = length - n + 1 + first_token, sees_most = length - n + 1 + last_token;
+    const int c0 = split * a.chunk;
+    if (split > 0 && sees_most <= c0) return;
+    const int c1 = sees_most < c0 + a.chunk ? sees_most : c0 + a.chunk;
+
+    // pages of the wave's keys, one half of 16 per lane
+    int pages = -1;
+    {
+        const int t = c0 + kTile * (wave + kWaves * (lane >> 1)) + 16 * (lane & 1);
+        if (t < c1) pages = a.tables[(int64_t)sequence * a.table_width + (t >> a.cache.log_page)];
+        if ((int64_t)pages >= a.cache.pages) pages = -1;
+    }
+
+    half8_t q[NR][kSteps];
+    float q_sum[NR];
+    int sees[NR];
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+        const int row = tile * kRows + 16 * r + c, token = row / group, h = row - token * group;
+        const bool valid = token < n;
+        sees[r] = valid ? length - n + 1 + token : 0;
+        const _Float16 *p = a.q + (int64_t)(valid ? begin + token : begin) * a.q_token + (int64_t)(head * group + (valid ? h : 0)) * a.q_head + g * (D / 4);
+        float sum = 0;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const half8_t x = *reinterpret_cast<const half8_t *>(p + 8 * s);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += (float)x[i];
+            q[r][s] = half8_t{x[0], x[4], x[1], x[5], x[2], x[6], x[3], x[7]};
+        }
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        q_sum[r] = sum;
+    }
+
+    const float scale = a.scale * kLog2e;
+    float4_t o[NR][kN];
+    float m[NR], l[NR], bias[NR];
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+        m[r] = -INFINITY;
+        l[r] = bias[r] = 0;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) o[r][i] = float4_t{0, 0, 0, 0};
+    }
+
+    const int mine = c1 - c0 - kTile * wave, steps = mine > 0 ? (mine + kStep - 1) / kStep : 0;
+    const int page_mask = (1 << a.cache.log_page) - 1;
+    const auto load = [&](int step, int h) {
+        const int page = __builtin_amdgcn_readlane(pages, 2 * step + h);
+        const int t = (c0 + kTile * (wave + kWaves * step) + 16 * h) & page_mask;
+        return load_half<D>(L::block(a.cache, page < 0 ? 0 : page, head), a.cache.log_page, t, c, g);
+    };
+    Half<D> next[2];
+    if (steps > 0) next[0] = load(0, 0), next[1] = load(0, 1);
+#pragma unroll 1
+    for (int step = 0; step < steps; ++step) {
+        Half<D> h[2] = {next[0], next[1]};
+        if (step + 1 < steps) next[0] = load(step + 1, 0), next[1] = load(step + 1, 1);
+        const int t0 = c0 + kTile * (wave + kWaves * step);
+        const bool known0 = __builtin_amdgcn_readlane(pages, 2 * step) >= 0, known1 = __builtin_amdgcn_readlane(pages, 2 * step + 1) >= 0;
+        const bool whole = known0 && known1 && t0 + kTile <= sees_least && t0 + kTile <= c1;
+
+        float4_t s[NR][2];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+#pragma unroll
+            for (int r = 0; r < NR; ++r) s[r][half] = float4_t{0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) {
+                const half8_t x = key_operand(h[half].k[k]);
+#pragma unroll
+                for (int r = 0; r < NR; ++r) s[r][half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, q[r][k], s[r][half], 0, 0, 0);
+            }
+        }
+        bf8_t high[NR], low[NR];
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float step_k = step_of(h[half].kp[i]) * scale, low_k = low_of(h[half].kp[i]) * scale - 64.0f * step_k;
+                    float x = s[r][half][i] * step_k + low_k * q_sum[r];
+                    if (!whole) {
+                        const int t = t0 + 16 * half + 4 * g + i;
+                        x = (half ? known1 : known0) && t < sees[r] && t < c1 ? x : -INFINITY;
+                    }
+                    s[r][half][i] = x;
+                    top = fmaxf(top, x);
+                }
+            if (__any(top > m[r] + kSlack)) {
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float next_m = fmaxf(m[r], top), keep = next_m == -INFINITY ? 1.0f : exp2f(m[r] - next_m);
+                m[r] = next_m;
+                l[r] *= keep;
+                bias[r] *= keep;
+#pragma unroll
+                for (int i = 0; i < kN; ++i) o[r][i] *= keep;
+            }
+            const float base = m[r] == -INFINITY ? 0.0f : m[r];
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float p = __builtin_amdgcn_exp2f(s[r][half][i] - base);
+                    const bool seen = whole || s[r][half][i] != -INFINITY;
+                    const float ps = seen ? p * step_of(h[half].vp[i]) : 0.0f; // keys that are not seen may hold anything
+                    const __bf16 hi = (__bf16)ps, lo = (__bf16)(ps - (float)hi);
+                    high[r][4 * half + i] = hi;
+                    low[r][4 * half + i] = lo;
+                    l[r] += p;
+                    bias[r] += (seen ? p * low_of(h[half].vp[i]) : 0.0f) - 128.0f * ((float)hi + (float)lo);
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            const bf8_t v = value_operand<D>(h, i);
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                o[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, high[r], o[r][i], 0, 0, 0);
+                o[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, low[r], o[r][i], 0, 0, 0);
+            }
+        }
+    }
+
+    // join the waves: all sums to the common maximum, then every thread takes D / 16 channels of a row
+    __shared__ float sums[kWaves][16][D + 4];
+    __shared__ float4_t stats[kWaves][16];
+    const int row_of = threadIdx.x >> 4, chunk_of = threadIdx.x & 15;
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+        l[r] += __shfl_xor(l[r], 16);
+        l[r] += __shfl_xor(l[r], 32);
+        bias[r] += __shfl_xor(bias[r], 16);
+        bias[r] += __shfl_xor(bias[r], 32);
+        if (r > 0) __syncthreads();
+        if (g == 0) stats[wave][c] = float4_t{m[r], l[r], bias[r], 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < kN; ++k) sums[wave][c][(4 * g + i) * kN + k] = o[r][k][i];
+        __syncthreads();
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, stats[w][row_of][0]);
+        float total = 0, x[kN] = {};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float4_t st = stats[w][row_of];
+            // a wave without a finite maximum has seen no key, or only NaN: its sums are 0 or NaN and go in as they are
+            const float keep = st[0] == -INFINITY ? 1.0f : exp2f(st[0] - top);
+            total += keep * st[1];
+#pragma unroll
+            for (int k = 0; k < kN; ++k) x[k] += keep * (sums[w][row_of][chunk_of * kN + k] + st[2]);
+        }
+        const int row = tile * kRows + 16 * r + row_of, token = row / group, h = row - token * group;
+        if (token < n) {
+            const int64_t at = (int64_t)(begin + token) * a.heads + head * group + h;
+            if (length - n + 1 + token <= a.chunk) {
+                typedef _Float16 vec __attribute__((ext_vector_type(kN)));
+                vec y;
+#pragma unroll
+                for (int k = 0; k < kN; ++k) y[k] = (_Float16)(total == 0.0f ? 0.0f : x[k] / total);
+                if (split == 0) *reinterpret_cast<vec *>(a.out + at * D + chunk_of * kN) = y;
+            } else {
+                const int64_t place = (int64_t)split * a.tokens * a.heads + at;
+#pragma unroll
+                for (int k = 0; k < kN; k += 4) *reinterpret_cast<float4_t *>(a.part + place * D + chunk_of * kN + k) = float4_t{x[k], x[k + 1], x[k + 2], x[k + 3]};
+                if (chunk_of == 0) a.stat[place] = make_float2(top, total);
+            }
+        }
+    }
+}
+
+// Joins the ranges of rows that see more than one: D / 4 lanes per row
+template <int D> __global__ __launch_bounds__(kThreads) void attention_join_kernel(const CachedArgs a)
+{
+    constexpr int kLanes = D / 4, kRows = kThreads / kLanes;
+    const int groups = (a.heads + kRows - 1) / kRows;
+    const int token = blockIdx.x / groups, head = (blockIdx.x - token * groups) * kRows + threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+    const int s = sequence_of(a.q_starts, token, a.tokens, a.sequences);
+    if (s < 0 || head >= a.heads) return;
+    int64_t begin, end;
+    token_range(a.q_starts, s, a.tokens, a.sequences, &begin, &end);
+    const int length = a.lengths[s] < a.max_length ? a.lengths[s] : a.max_length, sees = (length < 0 ? 0 : length) - (int)(end - 1 - token);
+    if (sees <= a.chunk) return;
+    const int ranges = (sees + a.chunk - 1) / a.chunk;
+    const int64_t row = (int64_t)token * a.heads + head, rows = (int64_t)a.tokens * a.heads;
+    float top = -INFINITY;
+    for (int i = 0; i < ranges; ++i) top = fmaxf(top, a.stat[i * rows + row].x);
+    float total = 0;
+    float4_t x = {0, 0, 0, 0};
+#pragma unroll 4
+    for (int i = 0; i < ranges; ++i) {
+        const float2 st = a.stat[i * rows + row];
+        const float keep = st.x == -INFINITY ? 1.0f : exp2f(st.x - top);
+        total += keep * st.y;
+        x += keep * *reinterpret_cast<const float4_t *>(a.part + (i * rows + row) * D + lane * 4);
+    }
+    half4_t y;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) y[k] = (_Float16)(total == 0.0f ? 0.0f : x[k] / total);
+    *reinterpret_cast<half4_t *>(a.out + row * D + lane * 4) = y;
+}
+
+struct Plan {
+    int rows; // 16-row tiles per workgroup
+    int64_t items;
+    int chunk, splits;
+};
+
+Plan plan_of(const ap_cache &c, const ap_cached &a)
+{
+    Plan p;
+    const int64_t group = a.heads / c.kv_heads, each = (a.tokens + a.sequences - 1) / a.sequences;
+    p.rows = each * group <= 16 ? 1 : 2;
+    const int64_t tile = 16 * p.rows;
+    p.items = a.q_starts ? a.tokens * group / tile + a.sequences : (each * group + tile - 1) / tile * a.sequences;
+    // As many ranges as give the card four workgroups per CU, of 256 keys at least
+    const int64_t units = p.items * c.kv_heads, longest = a.max_length > 0 ? a.max_length : 1;
+    int64_t chunk = (longest * units + 1023) / 1024;
+    chunk = (chunk + kStep - 1) / kStep * kStep;
+    p.chunk = (int)(chunk < 2 * kStep ? 2 * kStep : chunk > kMaxChunk ? kMaxChunk : chunk);
+    p.splits = (int)((longest + p.chunk - 1) / p.chunk);
+    return p;
 }
 
 } // namespace
 
-size_t attention_cached_work(const ap_cache &, const ap_cached &) { return 0; }
+size_t attention_cached_work(const ap_cache &c, const ap_cached &a)
+{
+    const Plan p = plan_of(c, a);
+    return p.splits == 1 ? 0 : (size_t)p.splits * a.tokens * a.heads * (c.head_dim * sizeof(float) + sizeof(float2));
+}
 
 hipError_t launch_attention_cached(const ap_cache &c, const ap_cached &a, hipStream_t stream)
 {
+    const Plan p = plan_of(c, a);
     CachedArgs k;
     k.cache = cache_shape(c);
     k.q = static_cast<const _Float16 *>(a.q.data);
     k.q_token = a.q.token_stride, k.q_head = a.q.head_stride;
-    k.tokens = a.tokens, k.table_width = a.table_width, k.max_length = a.max_length;
+    k.table_width = a.table_width;
     k.q_starts = a.q_starts, k.lengths = a.lengths, k.tables = a.tables;
-    k.heads = a.heads, k.sequences = a.sequences;
+    k.tokens = (int)a.tokens, k.heads = a.heads, k.sequences = a.sequences, k.max_length = (int)a.max_length;
+    k.items = (int)p.items, k.splits = p.splits, k.chunk = p.chunk;
     k.scale = a.scale;
     k.out = static_cast<_Float16 *>(a.out);
-    const int64_t rows = a.tokens * a.heads;
-    const dim3 grid((unsigned)(rows < (1 << 22) ? rows : 1 << 22));
-    if (c.head_dim == 64) attention_cached_kernel<64><<<grid, 64, 0, stream>>>(k);
-    else attention_cached_kernel<128><<<grid, 64, 0, stream>>>(k);
+    k.part = static_cast<float *>(a.work);
+    k.stat = reinterpret_cast<float2 *>(k.part + (size_t)p.splits * a.tokens * a.heads * c.head_dim);
+    const int64_t blocks = p.items * c.kv_heads * p.splits;
+    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)blocks);
+    if (c.head_dim == 64) {
+        if (p.rows == 1) attention_cached_kernel<64, 1><<<grid, kThreads, 0, stream>>>(k);
+        else attention_cached_kernel<64, 2><<<grid, kThreads, 0, stream>>>(k);
+    } else {
+        if (p.rows == 1) attention_cached_kernel<128, 1><<<grid, kThreads, 0, stream>>>(k);
+        else attention_cached_kernel<128, 2><<<grid, kThreads, 0, stream>>>(k);
+    }
+    if (p.splits > 1) {
+        const int rows = kThreads / (c.head_dim / 4);
+        const dim3 join((unsigned)(a.tokens * ((a.heads + rows - 1) / rows)));
+        if (c.head_dim == 64) attention_join_kernel<64><<<join, kThreads, 0, stream>>>(k);
+        else attention_join_kernel<128><<<join, kThreads, 0, stream>>>(k);
+    }
     return hipGetLastError();
 }
 

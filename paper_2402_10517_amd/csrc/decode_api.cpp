@@ -49,9 +49,9 @@ ap_status check_cached(const ap_cache *c, const ap_cached *a)
     s = check_heads(a->heads, c->kv_heads);
     if (s != AP_OK) return s;
     if (a->tokens < 0 || a->tokens > kMaxTokens || a->sequences < 0 || a->sequences > (1 << 20)) return AP_ERR_SHAPE;
-    if (a->tokens > 0 && a->sequences < 1) return AP_ERR_SHAPE;
+    if ((a->tokens > 0 && a->sequences < 1) || a->tokens * a->heads > kMaxTokens) return AP_ERR_SHAPE;
     if (!a->q_starts && a->sequences > 0 && a->tokens % a->sequences) return AP_ERR_SHAPE;
-    if (a->table_width < 0 || a->table_width >= (int64_t)1 << 31 || a->max_length < 0 || a->max_length > kMaxTokens ||
+    if (a->table_width < 0 || a->table_width >= (int64_t)1 << 31 || a->max_length < 0 || a->max_length > 1 << 30 ||
         a->max_length > a->table_width * c->page_tokens)
         return AP_ERR_SHAPE;
     return AP_OK;
@@ -128,7 +128,7 @@ extern "C" ap_status ap_attention_prompt(const ap_prompt *a, void *stream)
     const ap_status s = check_heads(a->heads, a->kv_heads);
     if (s != AP_OK) return s;
     if (a->tokens < 0 || a->tokens > kMaxTokens || a->keys < 0 || a->keys > kMaxTokens || a->sequences < 0 || a->sequences > (1 << 20) ||
-        (a->tokens > 0 && a->sequences < 1))
+        (a->tokens > 0 && a->sequences < 1) || a->tokens * a->heads > kMaxTokens)
         return AP_ERR_SHAPE;
     if (a->tokens == 0) return AP_OK;
     if (!rows_ok(a->q) || (a->keys > 0 && (!rows_ok(a->k) || !rows_ok(a->v))) || !a->q_starts || !a->k_starts || !aligned(a->q_starts, 4) ||

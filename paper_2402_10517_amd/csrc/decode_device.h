@@ -33,7 +33,7 @@ template <int D> struct CacheLayout {
     }
 };
 
-// Tokens [begin, end) of sequence s, whatever the array holds inside [0, tokens)
+// Tokens [begin, end) of sequence s; none where the two starts descend or leave [0, tokens]
 __device__ __forceinline__ void token_range(const int32_t *starts, int s, int64_t tokens, int sequences, int64_t *begin, int64_t *end)
 {
     if (!starts) {
@@ -43,8 +43,9 @@ __device__ __forceinline__ void token_range(const int32_t *starts, int s, int64_
         return;
     }
     const int64_t a = starts[s], b = starts[s + 1];
-    *begin = a < 0 ? 0 : a > tokens ? tokens : a;
-    *end = b < *begin ? *begin : b > tokens ? tokens : b;
+    const bool ok = a >= 0 && a <= b && b <= tokens;
+    *begin = ok ? a : 0;
+    *end = ok ? b : 0;
 }
 
 } // namespace apgemv
