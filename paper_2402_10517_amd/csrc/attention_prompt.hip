@@ -1,45 +1,294 @@
-// Causal attention over packed sequences of binary16 keys and values.
+// Causal attention over packed sequences of binary16 keys and values, on the matrix cores.
+//
+// A workgroup takes 128 query rows (token, head of the group) of one sequence and key head and walks the keys they see, 64 at a time; a wave has 32
+// of the rows.  v_mfma_f32_32x32x16_f16 twice, both transposed:  S^T = K Q^T,  O^T = V^T P^T,  P = e^(scale s - m).
+// With keys as rows and queries as columns a lane holds scores of one query row throughout, and the scores' registers, rounded to binary16, are the
+// weights' operand as they stand: the order of the keys inside a product is free, and the values are read in the same order from LDS, transposed by
+// ds_read_b64_tr_b16.  Row statistics are one number per lane; the running maximum moves only when a score exceeds it by 2^8, so weights
+// stay below 2^8 and the accumulators are seldom rescaled.
+// Keys and values go from memory into LDS without registers, 16 bytes a lane, one tile ahead.  Rows of LDS have their 16-byte chunks exchanged (the
+// lanes ask memory for the chunk that belongs at their place) so that the reads of both operands meet every bank once.
+//
+// Bound by the matrix cores and the exponentials beside them: 4 D operations and one exponential per pair of query and key.
 #include "attention_rows.h"
 
 namespace apgemv {
 
 namespace {
 
+typedef float float16_t __attribute__((ext_vector_type(16)));
+typedef __fp16 fp4_t __attribute__((ext_vector_type(4)));
+
 struct PromptArgs {
     const _Float16 *q, *k, *v;
-    int64_t q_token, q_head, k_token, k_head, v_token, v_head, tokens, keys;
+    int64_t q_token, q_head, k_token, k_head, v_token, v_head;
     const int32_t *q_starts, *k_starts;
-    int heads, kv_heads, sequences;
-    float scale;
+    int tokens, keys, heads, kv_heads, sequences, items;
+    float scale, slack;
     _Float16 *out;
 };
 
-template <int D> struct PromptRows {
-    const _Float16 *k, *v;
-    int64_t k_token, v_token;
-    __device__ float score(int64_t j, const float *q) const
-    {
-        float sum = 0;
-        for (int d = 0; d < D; ++d) sum += q[d] * (float)k[j * k_token + d];
-        return sum;
-    }
-    __device__ float value(int64_t j, int d) const { return (float)v[j * v_token + d]; }
+constexpr int kThreads = 256;
+constexpr int kWaveRows = 32;
+constexpr int kRows = kWaveRows * kThreads / 64;
+constexpr int kKeys = 64; // keys of a tile
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kSlack = 8.0f;
+
+// A tile of kKeys rows of D values in LDS.  chunk(row, i): where the 16-byte chunk i of a row is
+template <int D> struct Tile {
+    static constexpr int kChunks = D / 8;
+    static constexpr int kBytes = kKeys * D * 2;
+    static constexpr int kLoads = kBytes / (kThreads * 16); // of 16 bytes per lane
+    __device__ static int key_chunk(int row, int i) { return D == 128 ? i ^ (row & 15) : i ^ (row >> 1 & 7); }
+    __device__ static int value_chunk(int row, int i) { return D == 128 ? i ^ (row & 3) << 2 : i ^ (row >> 1 & 1) << 2; }
 };
 
-template <int D> __global__ __launch_bounds__(64) void attention_prompt_kernel(const PromptArgs a)
-{
-    const int64_t rows = a.tokens * a.heads;
-    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
-        const int64_t token = row / a.heads;
-        const int head = (int)(row - token * a.heads), kv = head / (a.heads / a.kv_heads);
-        const int s = sequence_of(a.q_starts, token, a.tokens, a.sequences);
-        if (s < 0) continue;
-        int64_t begin, end, k0, k1;
-        token_range(a.q_starts, s, a.tokens, a.sequences, &begin, &end);
-        token_range(a.k_starts, s, a.keys, a.sequences, &k0, &k1);
-        const PromptRows<D> source{a.k + k0 * a.k_token + kv * a.k_head, a.v + k0 * a.v_token + kv * a.v_head, a.k_token, a.v_token};
-        attend_row<D>(source, (k1 - k0) - (end - 1 - token), a.q + token * a.q_token + head * a.q_head, a.scale, a.out + row * D);
+typedef __attribute__((address_space(3))) uint8_t lds_byte;
+
+// Where a lane's 16-byte pieces of a tile come from in memory; the tiles are asked for in order
+template <int D, bool VALUES> struct Source {
+    typedef Tile<D> T;
+    const _Float16 *rows, *at[T::kLoads];
+    int64_t stride;
+    int first_row, last; // of the lane's first piece; of the sequence
+
+    __device__ static int row_of(int i, int wave, int lane) { return ((wave * T::kLoads + i) * 64 + lane) / T::kChunks; }
+    __device__ void place(int key, int wave, int lane)
+    {
+#pragma unroll
+        for (int i = 0; i < T::kLoads; ++i) {
+            const int row = row_of(i, wave, lane), chunk = VALUES ? T::value_chunk(row, lane % T::kChunks) : T::key_chunk(row, lane % T::kChunks);
+            at[i] = rows + (key + row < last ? key + row : last) * stride + chunk * 8;
+        }
     }
+    __device__ void start(const _Float16 *data, int64_t token_stride, int keys, int wave, int lane)
+    {
+        rows = data;
+        stride = token_stride;
+        last = keys - 1;
+        place(0, wave, lane);
+    }
+    // the tile of keys key ..; rows beyond the last are the last's (they are not seen)
+    __device__ void fetch(int key, lds_byte *tile, int wave, int lane)
+    {
+        if (key > 0 && key + kKeys > last + 1) place(key, wave, lane);
+#pragma unroll
+        for (int i = 0; i < T::kLoads; ++i) {
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)at[i],
+                                             (__attribute__((address_space(3))) void *)(tile + (wave * T::kLoads + i) * 1024), 16, 0, 0);
+            at[i] += kKeys * stride;
+        }
+    }
+};
+
+// Four keys (4 h .. of 8, from `key`) of channel 32 block + lane % 32, transposed on the way from LDS; at: value_base
+template <int D> __device__ __forceinline__ int value_base(int block, int lane)
+{
+    const int row = 4 * (lane >> 5) + (lane >> 2 & 3), d = block * 32 + (lane & 16) + 4 * (lane & 3);
+    return row * D * 2 + Tile<D>::value_chunk(row, d >> 3) * 16 + (d & 4) * 2;
+}
+template <int D> __device__ __forceinline__ half4_t read_values(const lds_byte *at, int key)
+{
+    return __builtin_bit_cast(half4_t, __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) fp4_t *)(at + key * D * 2)));
+}
+
+__device__ __forceinline__ bool finite16(_Float16 x) { return (__builtin_bit_cast(uint16_t, x) & 0x7c00) != 0x7c00; }
+
+// Item -> sequence and row tile (64 lanes call together); the items of a sequence come last tile first, its longest
+__device__ __forceinline__ bool find_tile(const PromptArgs &a, int item, int *sequence, int *tile)
+{
+    const int lane = threadIdx.x & 63, group = a.heads / a.kv_heads;
+    int before = 0;
+    for (int first = 0; first < a.sequences; first += 64) {
+        int tiles = 0;
+        if (first + lane < a.sequences) {
+            int64_t begin, end;
+            token_range(a.q_starts, first + lane, a.tokens, a.sequences, &begin, &end);
+            tiles = (int)(((end - begin) * group + kRows - 1) / kRows);
+        }
+        int upto = tiles;
+        for (int d = 1; d < 64; d <<= 1) {
+            const int other = __shfl_up(upto, d);
+            if (lane >= d) upto += other;
+        }
+        const uint64_t found = __ballot(before + upto > item);
+        if (found) {
+            const int l = __builtin_ctzll(found);
+            *sequence = first + l;
+            *tile = before + __shfl(upto, l) - 1 - item;
+            return true;
+        }
+        before += __shfl(upto, 63);
+    }
+    return false;
+}
+
+template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prompt_kernel(const PromptArgs a)
+{
+    typedef Tile<D> T;
+    constexpr int kParts = D / 16; // products of 16 channels per score
+    constexpr int kBlocks = D / 32; // blocks of 32 channels of the output
+    __shared__ __attribute__((aligned(16))) uint8_t tiles[2][2][T::kBytes];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
+    const int group = a.heads / a.kv_heads, head = blockIdx.x % a.kv_heads;
+    int sequence, tile;
+    if (!find_tile(a, blockIdx.x / a.kv_heads, &sequence, &tile)) return;
+    sequence = __builtin_amdgcn_readfirstlane(sequence);
+    tile = __builtin_amdgcn_readfirstlane(tile);
+    int64_t q0, q1, k0, k1;
+    token_range(a.q_starts, sequence, a.tokens, a.sequences, &q0, &q1);
+    token_range(a.k_starts, sequence, a.keys, a.sequences, &k0, &k1);
+    const int n = (int)(q1 - q0), keys = (int)(k1 - k0), ahead = keys - n + 1; // token i sees ahead + i keys
+
+    const int row = tile * kRows + wave * kWaveRows + c, token = row / group;
+    const bool valid = token < n;
+    const int sees = valid ? ahead + token : 0;
+    half8_t q[kParts];
+    {
+        const _Float16 *p = a.q + (q0 + (valid ? token : 0)) * a.q_token + (int64_t)(head * group + (valid ? row - token * group : 0)) * a.q_head + 8 * h;
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) {
+            q[i] = *reinterpret_cast<const half8_t *>(p + 16 * i);
+            if (a.scale < 0) q[i] = -q[i];
+        }
+    }
+    const float scale = fabsf(a.scale) * kLog2e;
+    // keys that the workgroup's last row, and the wave's first and last, see
+    const auto token_of = [&](int r) { return r / group < n ? r / group : n - 1; };
+    const int most = ahead + token_of(tile * kRows + kRows - 1), first_row = tile * kRows + wave * kWaveRows;
+    const int wave_least = ahead + token_of(first_row), wave_most = first_row / group < n ? ahead + token_of(first_row + kWaveRows - 1) : 0;
+
+    const _Float16 *k = a.k + k0 * a.k_token + head * a.k_head, *v = a.v + k0 * a.v_token + head * a.v_head;
+    float16_t o[kBlocks];
+#pragma unroll
+    for (int i = 0; i < kBlocks; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[i][j] = 0;
+    float m = -INFINITY, l = 0;
+
+    // places in a tile: of the lane's key in the chunks of the products, of its values in the blocks of channels
+    int key_at[kParts], value_at[kBlocks];
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) key_at[i] = c * D * 2 + T::key_chunk(c, 2 * i + h) * 16;
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) value_at[b] = value_base<D>(b, lane);
+    lds_byte *const lds = (lds_byte *)&tiles[0][0][0];
+    Source<D, false> k_source;
+    Source<D, true> v_source;
+    if (most > 0) {
+        k_source.start(k, a.k_token, keys, wave, lane);
+        v_source.start(v, a.v_token, keys, wave, lane);
+        k_source.fetch(0, lds, wave, lane);
+        v_source.fetch(0, lds + T::kBytes, wave, lane);
+    }
+#pragma unroll 1
+    for (int key = 0, turn = 0; key < most; key += kKeys, turn ^= 1) {
+        __syncthreads(); // this tile has arrived, the other one is free
+        if (key + kKeys < most) {
+            lds_byte *next = lds + (turn ^ 1) * 2 * T::kBytes;
+            k_source.fetch(key + kKeys, next, wave, lane);
+            v_source.fetch(key + kKeys, next + T::kBytes, wave, lane);
+        }
+        if (key >= wave_most) continue;
+        const lds_byte *kt = lds + turn * 2 * T::kBytes, *vt = kt + T::kBytes;
+        float16_t s[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) s[b][j] = 0;
+#pragma unroll
+            for (int i = 0; i < kParts; ++i) {
+                const half8_t x = *(const __attribute__((address_space(3))) half8_t *)(kt + key_at[i] + b * 32 * D * 2);
+                s[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, q[i], s[b], 0, 0, 0);
+            }
+        }
+        const bool masked = key + kKeys > wave_least;
+        bool odd = false; // a value that is not finite, in a tile that some row sees only in part
+        if (masked) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (key + b * 32 + 8 * (j >> 2) + 4 * h + (j & 3) >= sees) s[b][j] = -INFINITY;
+            for (int i = lane; i < T::kBytes / 16; i += 64) {
+                const half8_t x = *(const __attribute__((address_space(3))) half8_t *)(vt + i * 16);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) odd = odd || !finite16(x[j]);
+            }
+            odd = __any(odd);
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) top = fmaxf(top, s[b][j]);
+        if (__any(top > m + a.slack)) {
+            const float next = fmaxf(m, fmaxf(top, __shfl_xor(top, 32))), keep = next == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - next) * scale);
+            m = next;
+            l *= keep;
+#pragma unroll
+            for (int i = 0; i < kBlocks; ++i) o[i] *= keep;
+        }
+        const float base = m == -INFINITY ? 0.0f : m * scale;
+        half8_t p[4];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][j], scale, -base));
+                l += x;
+                p[2 * b + (j >> 3)][j & 7] = (_Float16)x;
+            }
+        if (!odd) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) {
+                    const half4_t lo = read_values<D>(vt + value_at[b], 16 * i), hi = read_values<D>(vt + value_at[b], 16 * i + 8);
+                    o[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), p[i], o[b], 0, 0, 0);
+                }
+        } else {
+            // 0 * infinity is NaN: such values stay out of the products and are added to the rows that see them
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) {
+                    const half4_t lo = read_values<D>(vt + value_at[b], 16 * i), hi = read_values<D>(vt + value_at[b], 16 * i + 8);
+                    half8_t x = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (!finite16(x[j])) x[j] = 0;
+                    o[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, p[i], o[b], 0, 0, 0);
+                }
+            for (int j = 0; j < kKeys; ++j) {
+                if (key + j >= sees) break;
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int d = 32 * b + 8 * i + 4 * h;
+                        const half4_t x = *(const __attribute__((address_space(3))) half4_t *)(vt + j * D * 2 + T::value_chunk(j, d >> 3) * 16 + (d & 4) * 2);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (!finite16(x[e])) o[b][4 * i + e] += (float)x[e];
+                    }
+            }
+        }
+    }
+    l += __shfl_xor(l, 32);
+    if (!valid) return;
+    _Float16 *out = a.out + ((q0 + token) * a.heads + head * group + (row - token * group)) * D + 4 * h;
+    const float scale_out = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            half4_t x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = (_Float16)(l == 0.0f ? 0.0f : o[b][4 * i + e] * scale_out);
+            *reinterpret_cast<half4_t *>(out + 32 * b + 8 * i) = x;
+        }
 }
 
 } // namespace
@@ -53,15 +302,18 @@ hipError_t launch_attention_prompt(const ap_prompt &a, hipStream_t stream)
     k.q_token = a.q.token_stride, k.q_head = a.q.head_stride;
     k.k_token = a.k.token_stride, k.k_head = a.k.head_stride;
     k.v_token = a.v.token_stride, k.v_head = a.v.head_stride;
-    k.tokens = a.tokens, k.keys = a.keys;
+    k.tokens = (int)a.tokens, k.keys = (int)a.keys;
     k.q_starts = a.q_starts, k.k_starts = a.k_starts;
     k.heads = a.heads, k.kv_heads = a.kv_heads, k.sequences = a.sequences;
-    k.scale = a.scale;
+    // a scale of 0 makes all weights equal, as this one does; scores of -inf (keys that are not seen) stay what they are
+    k.scale = fabsf(a.scale) < 1e-30f ? 1e-30f : a.scale;
+    k.slack = kSlack / (fabsf(k.scale) * kLog2e);
     k.out = static_cast<_Float16 *>(a.out);
-    const int64_t rows = a.tokens * a.heads;
-    const dim3 grid((unsigned)(rows < (1 << 22) ? rows : 1 << 22));
-    if (a.head_dim == 64) attention_prompt_kernel<64><<<grid, 64, 0, stream>>>(k);
-    else attention_prompt_kernel<128><<<grid, 64, 0, stream>>>(k);
+    const int64_t items = a.tokens * (a.heads / a.kv_heads) / kRows + a.sequences, blocks = items * a.kv_heads;
+    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+    k.items = (int)items;
+    if (a.head_dim == 64) attention_prompt_kernel<64><<<dim3((unsigned)blocks), kThreads, 0, stream>>>(k);
+    else attention_prompt_kernel<128><<<dim3((unsigned)blocks), kThreads, 0, stream>>>(k);
     return hipGetLastError();
 }
 
