@@ -122,7 +122,7 @@ ap_status ap_attention_prompt(const ap_prompt *a, void *stream);
 /*
  * Verification of drafted tokens.  Sequence s has counts[s] drafts (drafts each where counts is NULL; a count outside 0..drafts is taken as the nearest).  Draft i is
  * accepted while uniform[i] * draft[i][x] < target[i][x] for its token x (binary32).  accepted[s] = n is how many are; the token after them is the
- * one with the greatest w[v] / noise[v], the lowest of equals, among those with w[v] > 0 (-1 if there is none), where w = target[n] - draft[n] after a refusal
+ * one with the greatest w[v] / noise[v], the lowest of equals, among those with w[v] > 0 and noise[v] >= 0 (-1 if there is none), where w = target[n] - draft[n] after a refusal
  * (or target[n] where no token has more than its draft) and w = target[n] after all counts[s] drafts.  With uniform numbers in [0, 1) and
  * noise from the exponential distribution the tokens are distributed as the target's own.
  *   target     device, sequences x (drafts + 1) x vocabulary probabilities;  draft  device, sequences x drafts x vocabulary

@@ -1,4 +1,8 @@
 // Verification of drafted tokens: accepted prefix, and the token after it by an exponential race.
+//
+// The token is the argmax of w / noise with lowest index first: no sum is taken, so any division of the vocabulary gives the same token, bit for bit.
+// Bound by HBM: one row of target and draft probabilities and the noise per sequence.  Few sequences leave most of the card idle, so a vocabulary is
+// divided among workgroups (2048 tokens at least each) and joined by a second launch.
 #include "decode_device.h"
 
 namespace apgemv {
@@ -6,6 +10,8 @@ namespace apgemv {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kEach = 8; // consecutive tokens of a thread
+constexpr int kStep = kThreads * kEach;
 
 struct VerifyArgs {
     const void *target, *draft;
@@ -14,77 +20,162 @@ struct VerifyArgs {
     const int32_t *counts;
     int64_t *tokens;
     int32_t *accepted;
-    int64_t vocabulary;
-    int sequences, drafts;
+    uint64_t *best; // sequences x parts
+    int64_t vocabulary, slice;
+    int sequences, drafts, parts;
 };
 
-// A candidate as one number whose order is that of (ratio, lower index): ratios are not negative, so their bits order like they do.
-__device__ __forceinline__ uint64_t candidate(float w, float noise, int64_t v)
+// A candidate as one number whose order is that of (ratio, lower index): ratios are not negative, so their bits order like they do.  0 = none
+__device__ __forceinline__ uint64_t candidate(float ratio, int64_t v)
 {
-    const float ratio = w / noise;
-    if (!(w > 0.0f) || !(ratio >= 0.0f)) return 0;
-    return (uint64_t)__float_as_uint(ratio) << 32 | (uint32_t)~(uint32_t)v;
+    return ratio >= 0.0f ? (uint64_t)__float_as_uint(ratio) << 32 | (uint32_t)~(uint32_t)v : 0;
 }
 
-__device__ __forceinline__ uint64_t wave_max(uint64_t x)
+__device__ __forceinline__ uint64_t block_max(uint64_t x)
 {
+    __shared__ uint64_t best[kThreads / 64];
     for (int m = 1; m < 64; m <<= 1) {
         const uint64_t y = __shfl_xor((unsigned long long)x, m);
         x = y > x ? y : x;
     }
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) best[threadIdx.x >> 6] = x;
+    __syncthreads();
+    for (int w = 0; w < kThreads / 64; ++w) x = best[w] > x ? best[w] : x;
     return x;
+}
+
+// Rows of an odd vocabulary start at any element: 16-byte loads that ask for the element's alignment only
+template <class T> struct __attribute__((packed, aligned(sizeof(T)))) Eight {
+    T x[kEach];
+};
+
+// The best of tokens [from, to): w = p - q, or p where there is no q
+template <class T> __device__ __forceinline__ uint64_t race(const T *p, const T *q, const float *noise, int64_t from, int64_t to)
+{
+    float best = -1.0f;
+    int64_t at = 0;
+    const auto consider = [&](float pv, float qv, float e, int64_t v) {
+        const float w = pv - qv, ratio = w / e;
+        if (w > 0.0f && e >= 0.0f && ratio > best) { // in ascending order: the lowest of equals stays
+            best = ratio;
+            at = v;
+        }
+    };
+    int64_t v = from + (int64_t)threadIdx.x * kEach;
+    for (; v + kEach <= to; v += kStep) {
+        const Eight<T> a = *reinterpret_cast<const Eight<T> *>(p + v);
+        const Eight<float> e = *reinterpret_cast<const Eight<float> *>(noise + v);
+        Eight<T> b;
+        if (q) b = *reinterpret_cast<const Eight<T> *>(q + v);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) consider((float)a.x[i], q ? (float)b.x[i] : 0.0f, e.x[i], v + i);
+    }
+    for (int i = 0; i < kEach && v + i < to; ++i) consider((float)p[v + i], q ? (float)q[v + i] : 0.0f, noise[v + i], v + i);
+    return block_max(candidate(best, at));
+}
+
+struct Sequence {
+    int count, accepted;
+};
+
+template <class T> __device__ __forceinline__ Sequence accept(const VerifyArgs &a, int64_t s)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t V = a.vocabulary;
+    Sequence r;
+    r.count = a.counts ? a.counts[s] : a.drafts;
+    r.count = r.count < 0 ? 0 : r.count > a.drafts ? a.drafts : r.count;
+    r.accepted = r.count;
+    for (int first = 0; first < r.count; first += 64) {
+        const int i = first + lane;
+        bool refused = false;
+        if (i < r.count) {
+            const int64_t x = a.drafted[s * a.drafts + i];
+            refused = true;
+            if (x >= 0 && x < V) {
+                const float p = (float)static_cast<const T *>(a.target)[(s * (a.drafts + 1) + i) * V + x];
+                const float q = (float)static_cast<const T *>(a.draft)[(s * a.drafts + i) * V + x];
+                refused = !(a.uniform[s * a.drafts + i] * q < p);
+            }
+        }
+        const uint64_t out = __ballot(refused);
+        if (out) {
+            r.accepted = first + __builtin_ctzll(out);
+            break;
+        }
+    }
+    return r;
+}
+
+// The end of a sequence, once the best of the whole vocabulary is known (0: none with more than its draft, or none at all)
+template <class T> __device__ __forceinline__ void finish(const VerifyArgs &a, int64_t s, int accepted, bool refused, uint64_t won)
+{
+    if (!won && refused)
+        won = race<T>(static_cast<const T *>(a.target) + (s * (a.drafts + 1) + accepted) * a.vocabulary, nullptr, a.noise + s * a.vocabulary, 0, a.vocabulary);
+    const int64_t token = won ? (int64_t)(uint32_t)~(uint32_t)won : -1;
+    for (int i = threadIdx.x; i <= a.drafts; i += kThreads)
+        a.tokens[s * (a.drafts + 1) + i] = i < accepted ? a.drafted[s * a.drafts + i] : i == accepted ? token : -1;
 }
 
 template <class T> __global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyArgs a)
 {
-    const int64_t s = blockIdx.x, V = a.vocabulary;
-    const T *target = static_cast<const T *>(a.target) + s * (a.drafts + 1) * V;
-    const T *draft = static_cast<const T *>(a.draft) + s * a.drafts * V;
-    const int64_t *drafted = a.drafted + s * a.drafts;
-    const float *uniform = a.uniform + s * a.drafts, *noise = a.noise + s * V;
+    const int64_t s = blockIdx.x / a.parts, V = a.vocabulary;
+    const int part = blockIdx.x - (int)s * a.parts;
+    const Sequence r = accept<T>(a, s);
+    const bool refused = r.accepted < r.count;
+    const T *p = static_cast<const T *>(a.target) + (s * (a.drafts + 1) + r.accepted) * V;
+    const T *q = refused ? static_cast<const T *>(a.draft) + (s * a.drafts + r.accepted) * V : nullptr;
+    const int64_t from = part * a.slice, to = from + a.slice < V ? from + a.slice : V;
+    const uint64_t won = race<T>(p, q, a.noise + s * V, from, to);
+    if (a.parts == 1) finish<T>(a, s, r.accepted, refused, won);
+    else if (threadIdx.x == 0) a.best[blockIdx.x] = won;
+    if (part == 0 && threadIdx.x == 0) a.accepted[s] = r.accepted;
+}
+
+template <class T> __global__ __launch_bounds__(kThreads) void verify_join_kernel(const VerifyArgs a)
+{
+    const int64_t s = blockIdx.x;
+    uint64_t won = 0;
+    for (int i = threadIdx.x; i < a.parts; i += kThreads) {
+        const uint64_t x = a.best[s * a.parts + i];
+        won = x > won ? x : won;
+    }
+    won = block_max(won);
     int count = a.counts ? a.counts[s] : a.drafts;
-    count = count < 0 ? 0 : count > a.drafts ? a.drafts : count;
-    int n = 0;
-    while (n < count) {
-        const int64_t x = drafted[n];
-        if (x < 0 || x >= V || !(uniform[n] * (float)draft[n * V + x] < (float)target[n * V + x])) break;
-        ++n;
-    }
-    const bool refused = n < count;
-    uint64_t rest = 0, full = 0;
-    for (int64_t v = threadIdx.x; v < V; v += kThreads) {
-        const float p = (float)target[n * V + v], e = noise[v];
-        const uint64_t f = candidate(p, e, v);
-        full = f > full ? f : full;
-        if (refused) {
-            const uint64_t r = candidate(p - (float)draft[n * V + v], e, v);
-            rest = r > rest ? r : rest;
-        }
-    }
-    __shared__ uint64_t best[2][kThreads / 64];
-    rest = wave_max(rest);
-    full = wave_max(full);
-    if ((threadIdx.x & 63) == 0) best[0][threadIdx.x >> 6] = rest, best[1][threadIdx.x >> 6] = full;
-    __syncthreads();
-    for (int w = 0; w < kThreads / 64; ++w) {
-        rest = best[0][w] > rest ? best[0][w] : rest;
-        full = best[1][w] > full ? best[1][w] : full;
-    }
-    const uint64_t won = rest ? rest : full;
-    const int64_t token = won ? (int64_t)(uint32_t)~(uint32_t)won : -1;
-    for (int i = threadIdx.x; i <= a.drafts; i += kThreads) a.tokens[s * (a.drafts + 1) + i] = i < n ? drafted[i] : i == n ? token : -1;
-    if (threadIdx.x == 0) a.accepted[s] = n;
+    count = count > a.drafts ? a.drafts : count;
+    const int accepted = a.accepted[s];
+    finish<T>(a, s, accepted, accepted < count, won);
+}
+
+// Parts of a vocabulary: as many as give the card four workgroups per CU, of one step at least
+int parts_of(const ap_verification &a)
+{
+    const int64_t steps = (a.vocabulary + kStep - 1) / kStep, wanted = (1024 + a.sequences - 1) / a.sequences;
+    return (int)(wanted < steps ? wanted : steps);
 }
 
 } // namespace
 
-size_t verify_work(const ap_verification &) { return 0; }
+size_t verify_work(const ap_verification &a)
+{
+    const int parts = parts_of(a);
+    return parts == 1 ? 0 : (size_t)parts * a.sequences * sizeof(uint64_t);
+}
 
 hipError_t launch_verify(const ap_verification &a, hipStream_t stream)
 {
-    const VerifyArgs k{a.target, a.draft, a.drafted, a.uniform, a.noise, a.counts, a.tokens, a.accepted, a.vocabulary, a.sequences, a.drafts};
-    if (a.half) verify_kernel<_Float16><<<a.sequences, kThreads, 0, stream>>>(k);
-    else verify_kernel<float><<<a.sequences, kThreads, 0, stream>>>(k);
+    const int parts = parts_of(a);
+    const int64_t steps = (a.vocabulary + kStep - 1) / kStep, slice = (steps + parts - 1) / parts * kStep;
+    const VerifyArgs k{a.target, a.draft,    a.drafted,                      a.uniform,    a.noise, a.counts,    a.tokens,
+                       a.accepted, static_cast<uint64_t *>(a.work), a.vocabulary, slice,   a.sequences, a.drafts, parts};
+    const dim3 grid((unsigned)a.sequences * (unsigned)parts);
+    if (a.half) verify_kernel<_Float16><<<grid, kThreads, 0, stream>>>(k);
+    else verify_kernel<float><<<grid, kThreads, 0, stream>>>(k);
+    if (parts > 1) {
+        if (a.half) verify_join_kernel<_Float16><<<a.sequences, kThreads, 0, stream>>>(k);
+        else verify_join_kernel<float><<<a.sequences, kThreads, 0, stream>>>(k);
+    }
     return hipGetLastError();
 }
 
