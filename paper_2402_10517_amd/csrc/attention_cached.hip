@@ -25,7 +25,7 @@ struct CachedArgs {
     const int32_t *q_starts, *lengths, *tables;
     int tokens, heads, sequences, max_length;
     int items, splits, chunk; // row tiles (at most), ranges of `chunk` keys
-    float scale;
+    float scale, slack;
     _Float16 *out;
     float *part;  // splits x rows x D: sums of range s
     float2 *stat; // splits x rows: their maximum and sum of weights
@@ -39,15 +39,32 @@ constexpr int kMaxChunk = 64 / 2 * kStep;   // a lane of a wave holds the page o
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.0f;
 
-// Item -> sequence and row tile, where sequences have different numbers of tokens (64 lanes call together)
-__device__ __forceinline__ bool find_item(const CachedArgs &a, int rows_per_tile, int item, int *sequence, int *tile)
+struct Item {
+    int sequence, tile, begin, tokens, length;
+};
+
+__device__ __forceinline__ int length_of(const CachedArgs &a, int sequence)
+{
+    const int length = a.lengths[sequence];
+    return length < 0 ? 0 : length > a.max_length ? a.max_length : length;
+}
+
+// The sequence and row tile of an item (64 lanes call together); false: there are fewer.  Where sequences have different numbers of tokens a lane looks at one
+// sequence, its length with it.
+__device__ __forceinline__ bool find_item(const CachedArgs &a, int rows_per_tile, int item, Item *out)
 {
     const int lane = threadIdx.x & 63, group = a.heads / a.cache.kv_heads;
+    if (!a.q_starts) {
+        const int tiles = a.items / a.sequences, s = item / tiles;
+        *out = Item{s, item - s * tiles, s * (a.tokens / a.sequences), a.tokens / a.sequences, __builtin_amdgcn_readfirstlane(length_of(a, s))};
+        return true;
+    }
     int before = 0;
     for (int first = 0; first < a.sequences; first += 64) {
-        int tiles = 0;
+        int tiles = 0, length = 0;
+        int64_t begin = 0, end = 0;
         if (first + lane < a.sequences) {
-            int64_t begin, end;
+            length = length_of(a, first + lane);
             token_range(a.q_starts, first + lane, a.tokens, a.sequences, &begin, &end);
             tiles = (int)(((end - begin) * group + rows_per_tile - 1) / rows_per_tile);
         }
@@ -59,11 +76,11 @@ __device__ __forceinline__ bool find_item(const CachedArgs &a, int rows_per_tile
         const uint64_t found = __ballot(before + upto > item);
         if (found) {
             const int l = __builtin_ctzll(found);
-            *sequence = first + l;
-            *tile = item - before - (__shfl(upto, l) - __shfl(tiles, l));
+            *out = Item{first + l, item - before - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(tiles, l)),
+                        __builtin_amdgcn_readlane((int)begin, l), __builtin_amdgcn_readlane((int)(end - begin), l), __builtin_amdgcn_readlane(length, l)};
             return true;
         }
-        before += __shfl(upto, 63);
+        before += __builtin_amdgcn_readlane(upto, 63);
     }
     return false;
 }
@@ -76,36 +93,52 @@ template <int D> struct Half {
     uint4_t kp, vp;
 };
 
-template <int D> __device__ __forceinline__ Half<D> load_half(const uint8_t *block, int log_page, int t, int c, int g)
+// section: where the (page, key head) starts, in scalar registers; t: the first of the 16 keys in it
+template <int D> __device__ __forceinline__ Half<D> load_half(const uint8_t *section, int log_page, int t, int c, int g)
 {
     typedef CacheLayout<D> L;
     typedef typename Half<D>::words_t words_t;
+    const uint8_t *k = section + L::key(t), *v = section + L::value(log_page, t, 0, 0), *kp = section + L::key_scale(log_page, t), *vp = section + L::value_scale(log_page, t);
     Half<D> h;
-    h.k = *reinterpret_cast<const words_t *>(block + L::key(t) + c * L::kRow + g * (D / 8));
-    h.v = *reinterpret_cast<const words_t *>(block + L::value(log_page, t + 4 * g, c, 0));
-    h.kp = *reinterpret_cast<const uint4_t *>(block + L::key_scale(log_page, t + 4 * g));
-    h.vp = *reinterpret_cast<const uint4_t *>(block + L::value_scale(log_page, t + 4 * g));
+    h.k = *reinterpret_cast<const words_t *>(k + (uint32_t)(c * L::kRow + g * (D / 8)));
+    h.v = *reinterpret_cast<const words_t *>(v + (uint32_t)(g * 4 * L::kRow + c * 8 * L::kHalves));
+    h.kp = *reinterpret_cast<const uint4_t *>(kp + (uint32_t)(g * 16));
+    h.vp = *reinterpret_cast<const uint4_t *>(vp + (uint32_t)(g * 16));
     return h;
 }
 
-__device__ __forceinline__ float low_of(uint32_t pair) { return (float)__builtin_bit_cast(_Float16, (uint16_t)pair); }
-__device__ __forceinline__ float step_of(uint32_t pair) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(pair >> 16)); }
+__device__ __forceinline__ _Float16 low_of(uint32_t pair) { return __builtin_bit_cast(_Float16, (uint16_t)pair); }
+__device__ __forceinline__ _Float16 step_of(uint32_t pair) { return __builtin_bit_cast(_Float16, (uint16_t)(pair >> 16)); }
+
+// A constant in a vector register: (w & it) | another constant is then one v_and_or_b32, which takes one scalar operand.  The instruction itself is the compiler's, who
+// knows how far it has to stay from the matrix instruction that reads its result.
+__device__ __forceinline__ uint32_t in_vector(uint32_t x)
+{
+    asm("" : "+v"(x));
+    return x;
+}
 
 // 8 codes as binary16 64 + code, in the order 0 4 1 5 2 6 3 7
-__device__ __forceinline__ half8_t key_operand(uint32_t w)
+__device__ __forceinline__ half8_t key_operand(uint32_t w, uint32_t mask)
 {
-    const uint4_t x = {(w << 4 & 0x00f000f0u) | 0x54005400u, (w & 0x00f000f0u) | 0x54005400u, (w >> 4 & 0x00f000f0u) | 0x54005400u,
-                       (w >> 8 & 0x00f000f0u) | 0x54005400u};
+    const uint32_t bits = 0x54005400u;
+    const uint4_t x = {(w << 4 & mask) | bits, (w & mask) | bits, (w >> 4 & mask) | bits, (w >> 8 & mask) | bits};
     return __builtin_bit_cast(half8_t, x);
 }
 
+__device__ __forceinline__ uint32_t pack_bf16(float x, float y)
+{
+    typedef __bf16 bf2_t __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, bf2_t{(__bf16)x, (__bf16)y});
+}
+
 // Channel n of four keys of both halves as bfloat16 128 + code
-template <int D> __device__ __forceinline__ bf8_t value_operand(const Half<D> (&h)[2], int n)
+template <int D> __device__ __forceinline__ bf8_t value_operand(const Half<D> (&h)[2], int n, uint32_t mask)
 {
     constexpr int kH = D / 64;
     uint4_t x;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = (h[i >> 1].v[(i & 1) * kH + n / 4] >> (4 * (n & 3)) & 0x000f000fu) | 0x43004300u;
+    for (int i = 0; i < 4; ++i) x[i] = (h[i >> 1].v[(i & 1) * kH + n / 4] >> (4 * (n & 3)) & mask) | 0x43004300u;
     return __builtin_bit_cast(bf8_t, x);
 }
 
@@ -119,21 +152,9 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 6
     const int kv = a.cache.kv_heads, group = a.heads / kv;
     const int head = blockIdx.x % kv, rest = blockIdx.x / kv;
     const int item = rest % a.items, split = rest / a.items;
-    int sequence, tile;
-    if (!a.q_starts) {
-        const int tiles = a.items / a.sequences;
-        sequence = item / tiles;
-        tile = item - sequence * tiles;
-    } else if (!find_item(a, kRows, item, &sequence, &tile)) {
-        return;
-    }
-    sequence = __builtin_amdgcn_readfirstlane(sequence);
-    tile = __builtin_amdgcn_readfirstlane(tile);
-    int64_t begin64, end64;
-    token_range(a.q_starts, sequence, a.tokens, a.sequences, &begin64, &end64);
-    const int begin = (int)begin64, n = (int)(end64 - begin64);
-    int length = a.lengths[sequence];
-    length = length < 0 ? 0 : length > a.max_length ? a.max_length : length;
+    Item it;
+    if (!find_item(a, kRows, item, &it)) return;
+    const int sequence = it.sequence, tile = it.tile, begin = it.begin, n = it.tokens, length = it.length;
     // keys that the tile's first and last row see
     const int first_token = tile * kRows / group, last = (tile * kRows + kRows - 1) / group, last_token = last < n ? last : n - 1;
     const int sees_least = length - n + 1 + first_token, sees_most = length - n + 1 + last_token;
@@ -161,7 +182,8 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 6
         float sum = 0;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
-            const half8_t x = *reinterpret_cast<const half8_t *>(p + 8 * s);
+            half8_t x = *reinterpret_cast<const half8_t *>(p + 8 * s);
+            if (a.scale < 0) x = -x;
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum += (float)x[i];
             q[r][s] = half8_t{x[0], x[4], x[1], x[5], x[2], x[6], x[3], x[7]};
@@ -171,12 +193,18 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 6
         q_sum[r] = sum;
     }
 
-    const float scale = a.scale * kLog2e;
-    float4_t o[NR][kN];
+    const float scale = fabsf(a.scale) * kLog2e;
+    float4_t o[NR][kN], offset[NR], start[NR]; // offset: 128 sum p step, on every channel; start: what takes the keys' 64 out
     float m[NR], l[NR], bias[NR];
+    const uint32_t key_mask = in_vector(0x00f000f0u), value_mask = in_vector(0x000f000fu);
+    const uint32_t ones = 0x43004300u; // bfloat16 128
+    const bf8_t all = __builtin_bit_cast(bf8_t, uint4_t{ones, ones, ones, ones});
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
         m[r] = -INFINITY;
+        offset[r] = float4_t{0, 0, 0, 0};
+        const float x = -64.0f * q_sum[r];
+        start[r] = float4_t{x, x, x, x};
         l[r] = bias[r] = 0;
 #pragma unroll
         for (int i = 0; i < kN; ++i) o[r][i] = float4_t{0, 0, 0, 0};
@@ -203,59 +231,71 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 6
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
 #pragma unroll
-            for (int r = 0; r < NR; ++r) s[r][half] = float4_t{0, 0, 0, 0};
-#pragma unroll
             for (int k = 0; k < kSteps; ++k) {
-                const half8_t x = key_operand(h[half].k[k]);
+                const half8_t x = key_operand(h[half].k[k], key_mask);
 #pragma unroll
-                for (int r = 0; r < NR; ++r) s[r][half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, q[r][k], s[r][half], 0, 0, 0);
+                for (int r = 0; r < NR; ++r) s[r][half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, q[r][k], k == 0 ? start[r] : s[r][half], 0, 0, 0);
             }
         }
         bf8_t high[NR], low[NR];
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
-            float top = -INFINITY;
+            uint32_t pairs[8];
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t kp = h[i >> 2].kp[i & 3];
+                s[r][i >> 2][i & 3] = __builtin_fmaf((float)step_of(kp), s[r][i >> 2][i & 3], (float)low_of(kp) * q_sum[r]);
+                pairs[i] = h[i >> 2].vp[i & 3];
+            }
+            if (!whole) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float step_k = step_of(h[half].kp[i]) * scale, low_k = low_of(h[half].kp[i]) * scale - 64.0f * step_k;
-                    float x = s[r][half][i] * step_k + low_k * q_sum[r];
-                    if (!whole) {
-                        const int t = t0 + 16 * half + 4 * g + i;
-                        x = (half ? known1 : known0) && t < sees[r] && t < c1 ? x : -INFINITY;
-                    }
-                    s[r][half][i] = x;
-                    top = fmaxf(top, x);
+                for (int i = 0; i < 8; ++i) {
+                    const int t = t0 + 16 * (i >> 2) + 4 * g + (i & 3);
+                    const bool seen = (i < 4 ? known0 : known1) && t < sees[r] && t < c1;
+                    s[r][i >> 2][i & 3] = seen ? s[r][i >> 2][i & 3] : -INFINITY;
+                    pairs[i] = seen ? pairs[i] : 0; // keys that are not seen may hold anything
                 }
-            if (__any(top > m[r] + kSlack)) {
+            }
+            float top = s[r][0][0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) top = fmaxf(top, s[r][i >> 2][i & 3]);
+            if (__any(top > m[r] + a.slack)) {
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
-                const float next_m = fmaxf(m[r], top), keep = next_m == -INFINITY ? 1.0f : exp2f(m[r] - next_m);
+                const float next_m = fmaxf(m[r], top), keep = next_m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m[r] - next_m) * scale);
                 m[r] = next_m;
                 l[r] *= keep;
                 bias[r] *= keep;
+                offset[r] *= keep;
 #pragma unroll
                 for (int i = 0; i < kN; ++i) o[r][i] *= keep;
             }
-            const float base = m[r] == -INFINITY ? 0.0f : m[r];
+            const float base = m[r] == -INFINITY ? 0.0f : m[r] * scale;
+            uint4_t hi, lo;
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
+            for (int i = 0; i < 8; i += 2) {
+                float ps[2];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(s[r][half][i] - base);
-                    const bool seen = whole || s[r][half][i] != -INFINITY;
-                    const float ps = seen ? p * step_of(h[half].vp[i]) : 0.0f; // keys that are not seen may hold anything
-                    const __bf16 hi = (__bf16)ps, lo = (__bf16)(ps - (float)hi);
-                    high[r][4 * half + i] = hi;
-                    low[r][4 * half + i] = lo;
+                for (int j = 0; j < 2; ++j) {
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][(i + j) >> 2][(i + j) & 3], scale, -base));
                     l[r] += p;
-                    bias[r] += (seen ? p * low_of(h[half].vp[i]) : 0.0f) - 128.0f * ((float)hi + (float)lo);
+                    bias[r] = __builtin_fmaf(p, (float)low_of(pairs[i + j]), bias[r]);
+                    ps[j] = p * (float)step_of(pairs[i + j]);
                 }
+                hi[i / 2] = pack_bf16(ps[0], ps[1]);
+                lo[i / 2] = pack_bf16(ps[0] - __builtin_bit_cast(float, hi[i / 2] << 16), ps[1] - __builtin_bit_cast(float, hi[i / 2] & 0xffff0000u));
+            }
+            high[r] = __builtin_bit_cast(bf8_t, hi);
+            low[r] = __builtin_bit_cast(bf8_t, lo);
+        }
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            offset[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(all, high[r], offset[r], 0, 0, 0);
+            offset[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(all, low[r], offset[r], 0, 0, 0);
         }
 #pragma unroll
         for (int i = 0; i < kN; ++i) {
-            const bf8_t v = value_operand<D>(h, i);
+            const bf8_t v = value_operand<D>(h, i, value_mask);
 #pragma unroll
             for (int r = 0; r < NR; ++r) {
                 o[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, high[r], o[r][i], 0, 0, 0);
@@ -274,6 +314,7 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 6
         l[r] += __shfl_xor(l[r], 32);
         bias[r] += __shfl_xor(bias[r], 16);
         bias[r] += __shfl_xor(bias[r], 32);
+        bias[r] -= offset[r][0];
         if (r > 0) __syncthreads();
         if (g == 0) stats[wave][c] = float4_t{m[r], l[r], bias[r], 0};
 #pragma unroll
@@ -289,7 +330,7 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 6
         for (int w = 0; w < kWaves; ++w) {
             const float4_t st = stats[w][row_of];
             // a wave without a finite maximum has seen no key, or only NaN: its sums are 0 or NaN and go in as they are
-            const float keep = st[0] == -INFINITY ? 1.0f : exp2f(st[0] - top);
+            const float keep = st[0] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((st[0] - top) * scale);
             total += keep * st[1];
 #pragma unroll
             for (int k = 0; k < kN; ++k) x[k] += keep * (sums[w][row_of][chunk_of * kN + k] + st[2]);
@@ -313,31 +354,39 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 6
     }
 }
 
-// Joins the ranges of rows that see more than one: D / 4 lanes per row
+// Joins the ranges of a row that sees more than one: D / 4 lanes take every kParts-th range, and a quarter or an eighth of the workgroup does the rest
 template <int D> __global__ __launch_bounds__(kThreads) void attention_join_kernel(const CachedArgs a)
 {
-    constexpr int kLanes = D / 4, kRows = kThreads / kLanes;
-    const int groups = (a.heads + kRows - 1) / kRows;
-    const int token = blockIdx.x / groups, head = (blockIdx.x - token * groups) * kRows + threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+    constexpr int kLanes = D / 4, kParts = kThreads / kLanes;
+    const int token = blockIdx.x / a.heads, lane = threadIdx.x % kLanes, part = threadIdx.x / kLanes;
     const int s = sequence_of(a.q_starts, token, a.tokens, a.sequences);
-    if (s < 0 || head >= a.heads) return;
+    if (s < 0) return;
     int64_t begin, end;
     token_range(a.q_starts, s, a.tokens, a.sequences, &begin, &end);
-    const int length = a.lengths[s] < a.max_length ? a.lengths[s] : a.max_length, sees = (length < 0 ? 0 : length) - (int)(end - 1 - token);
+    const int sees = length_of(a, s) - (int)(end - 1 - token);
     if (sees <= a.chunk) return;
     const int ranges = (sees + a.chunk - 1) / a.chunk;
-    const int64_t row = (int64_t)token * a.heads + head, rows = (int64_t)a.tokens * a.heads;
+    const int64_t row = blockIdx.x, rows = (int64_t)a.tokens * a.heads;
+    const float scale = fabsf(a.scale) * kLog2e;
     float top = -INFINITY;
-    for (int i = 0; i < ranges; ++i) top = fmaxf(top, a.stat[i * rows + row].x);
+    for (int i = threadIdx.x & 63; i < ranges; i += 64) top = fmaxf(top, a.stat[i * rows + row].x);
+    for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
     float total = 0;
     float4_t x = {0, 0, 0, 0};
-#pragma unroll 4
-    for (int i = 0; i < ranges; ++i) {
+#pragma unroll 2
+    for (int i = part; i < ranges; i += kParts) {
         const float2 st = a.stat[i * rows + row];
-        const float keep = st.x == -INFINITY ? 1.0f : exp2f(st.x - top);
+        const float keep = st.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((st.x - top) * scale);
         total += keep * st.y;
         x += keep * *reinterpret_cast<const float4_t *>(a.part + (i * rows + row) * D + lane * 4);
     }
+    __shared__ float4_t sums[kParts][kLanes];
+    __shared__ float totals[kParts];
+    sums[part][lane] = x;
+    if (lane == 0) totals[part] = total;
+    __syncthreads();
+    if (part > 0) return;
+    for (int i = 1; i < kParts; ++i) x += sums[i][lane], total += totals[i];
     half4_t y;
 #pragma unroll
     for (int k = 0; k < 4; ++k) y[k] = (_Float16)(total == 0.0f ? 0.0f : x[k] / total);
@@ -385,7 +434,9 @@ hipError_t launch_attention_cached(const ap_cache &c, const ap_cached &a, hipStr
     k.q_starts = a.q_starts, k.lengths = a.lengths, k.tables = a.tables;
     k.tokens = (int)a.tokens, k.heads = a.heads, k.sequences = a.sequences, k.max_length = (int)a.max_length;
     k.items = (int)p.items, k.splits = p.splits, k.chunk = p.chunk;
-    k.scale = a.scale;
+    // a scale of 0 makes all weights equal, as this one does; scores of -inf (keys that are not seen) stay what they are
+    k.scale = fabsf(a.scale) < 1e-30f ? 1e-30f : a.scale;
+    k.slack = kSlack / (fabsf(k.scale) * kLog2e);
     k.out = static_cast<_Float16 *>(a.out);
     k.part = static_cast<float *>(a.work);
     k.stat = reinterpret_cast<float2 *>(k.part + (size_t)p.splits * a.tokens * a.heads * c.head_dim);
@@ -400,8 +451,7 @@ hipError_t launch_attention_cached(const ap_cache &c, const ap_cached &a, hipStr
         else attention_cached_kernel<128, 2><<<grid, kThreads, 0, stream>>>(k);
     }
     if (p.splits > 1) {
-        const int rows = kThreads / (c.head_dim / 4);
-        const dim3 join((unsigned)(a.tokens * ((a.heads + rows - 1) / rows)));
+        const dim3 join((unsigned)(a.tokens * a.heads));
         if (c.head_dim == 64) attention_join_kernel<64><<<join, kThreads, 0, stream>>>(k);
         else attention_join_kernel<128><<<join, kThreads, 0, stream>>>(k);
     }
