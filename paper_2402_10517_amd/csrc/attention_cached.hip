@@ -56,7 +56,7 @@ __device__ __forceinline__ bool find_item(const CachedArgs &a, int rows_per_tile
     const int lane = threadIdx.x & 63, group = a.heads / a.cache.kv_heads;
     if (!a.q_starts) {
         const int tiles = a.items / a.sequences, s = item / tiles;
-        *out = Item{s, item - s * tiles, s * (a.tokens / a.sequences), a.tokens / a.sequences, __builtin_amdgcn_readfirstlane(length_of(a, s))};
+        *out = Item{s, item - s * tiles, s * (a.tokens / a.sequences), a.tokens / a.sequences, length_of(a, s)};
         return true;
     }
     int before = 0;
@@ -93,17 +93,17 @@ template <int D> struct Half {
     uint4_t kp, vp;
 };
 
-// section: where the (page, key head) starts, in scalar registers; t: the first of the 16 keys in it
+// They are read once: past the caches' usual order.  section: where the (page, key head) starts, in scalar registers; t: the first of the 16 keys in it
 template <int D> __device__ __forceinline__ Half<D> load_half(const uint8_t *section, int log_page, int t, int c, int g)
 {
     typedef CacheLayout<D> L;
     typedef typename Half<D>::words_t words_t;
     const uint8_t *k = section + L::key(t), *v = section + L::value(log_page, t, 0, 0), *kp = section + L::key_scale(log_page, t), *vp = section + L::value_scale(log_page, t);
     Half<D> h;
-    h.k = *reinterpret_cast<const words_t *>(k + (uint32_t)(c * L::kRow + g * (D / 8)));
-    h.v = *reinterpret_cast<const words_t *>(v + (uint32_t)(g * 4 * L::kRow + c * 8 * L::kHalves));
-    h.kp = *reinterpret_cast<const uint4_t *>(kp + (uint32_t)(g * 16));
-    h.vp = *reinterpret_cast<const uint4_t *>(vp + (uint32_t)(g * 16));
+    h.k = __builtin_nontemporal_load(reinterpret_cast<const words_t *>(k + (uint32_t)(c * L::kRow + g * (D / 8))));
+    h.v = __builtin_nontemporal_load(reinterpret_cast<const words_t *>(v + (uint32_t)(g * 4 * L::kRow + c * 8 * L::kHalves)));
+    h.kp = __builtin_nontemporal_load(reinterpret_cast<const uint4_t *>(kp + (uint32_t)(g * 16)));
+    h.vp = __builtin_nontemporal_load(reinterpret_cast<const uint4_t *>(vp + (uint32_t)(g * 16)));
     return h;
 }
 
@@ -154,21 +154,20 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 6
     const int item = rest % a.items, split = rest / a.items;
     Item it;
     if (!find_item(a, kRows, item, &it)) return;
-    const int sequence = it.sequence, tile = it.tile, begin = it.begin, n = it.tokens, length = it.length;
-    // keys that the tile's first and last row see
-    const int first_token = tile * kRows / group, last = (tile * kRows + kRows - 1) / group, last_token = last < n ? last : n - 1;
-    const int sees_least = length - n + 1 + first_token, sees_most = length - n + 1 + last_token;
-    const int c0 = split * a.chunk;
-    if (split > 0 && sees_most <= c0) return;
-    const int c1 = sees_most < c0 + a.chunk ? sees_most : c0 + a.chunk;
-
-    // pages of the wave's keys, one half of 16 per lane
+    const int sequence = it.sequence, tile = it.tile, begin = it.begin, n = it.tokens, c0 = split * a.chunk;
+    // pages of the wave's keys, one half of 16 per lane; asked for before the length is known
     int pages = -1;
     {
         const int t = c0 + kTile * (wave + kWaves * (lane >> 1)) + 16 * (lane & 1);
-        if (t < c1) pages = a.tables[(int64_t)sequence * a.table_width + (t >> a.cache.log_page)];
-        if ((int64_t)pages >= a.cache.pages) pages = -1;
+        if (t < a.max_length) pages = a.tables[(int64_t)sequence * a.table_width + (t >> a.cache.log_page)];
     }
+    const int length = __builtin_amdgcn_readfirstlane(it.length);
+    if ((int64_t)pages >= a.cache.pages) pages = -1;
+    // keys that the tile's first and last row see
+    const int first_token = tile * kRows / group, last = (tile * kRows + kRows - 1) / group, last_token = last < n ? last : n - 1;
+    const int sees_least = length - n + 1 + first_token, sees_most = length - n + 1 + last_token;
+    if (split > 0 && sees_most <= c0) return;
+    const int c1 = sees_most < c0 + a.chunk ? sees_most : c0 + a.chunk;
 
     half8_t q[NR][kSteps];
     float q_sum[NR];
