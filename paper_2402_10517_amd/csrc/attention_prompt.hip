@@ -17,6 +17,8 @@ namespace apgemv {
 namespace {
 
 typedef float float16_t __attribute__((ext_vector_type(16)));
+typedef float float2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 typedef __fp16 fp4_t __attribute__((ext_vector_type(4)));
 
 struct PromptArgs {
@@ -46,39 +48,31 @@ template <int D> struct Tile {
 
 typedef __attribute__((address_space(3))) uint8_t lds_byte;
 
-// Where a lane's 16-byte pieces of a tile come from in memory; the tiles are asked for in order
+// Where a lane's 16-byte pieces of a tile come from in memory, as offsets from the tile's first row
 template <int D, bool VALUES> struct Source {
     typedef Tile<D> T;
-    const _Float16 *rows, *at[T::kLoads];
-    int64_t stride;
-    int first_row, last; // of the lane's first piece; of the sequence
+    const uint8_t *rows;
+    uint32_t stride; // bytes
+    uint32_t at[T::kLoads];
 
-    __device__ static int row_of(int i, int wave, int lane) { return ((wave * T::kLoads + i) * 64 + lane) / T::kChunks; }
-    __device__ void place(int key, int wave, int lane)
+    // rows beyond the last key are the last's (they are not seen); present: keys from the tile's first on
+    __device__ void place(int present, int wave, int lane)
     {
 #pragma unroll
         for (int i = 0; i < T::kLoads; ++i) {
-            const int row = row_of(i, wave, lane), chunk = VALUES ? T::value_chunk(row, lane % T::kChunks) : T::key_chunk(row, lane % T::kChunks);
-            at[i] = rows + (key + row < last ? key + row : last) * stride + chunk * 8;
+            const int row = ((wave * T::kLoads + i) * 64 + lane) / T::kChunks, chunk = VALUES ? T::value_chunk(row, lane % T::kChunks) : T::key_chunk(row, lane % T::kChunks);
+            at[i] = (uint32_t)(row < present ? row : present - 1) * stride + chunk * 16;
         }
     }
-    __device__ void start(const _Float16 *data, int64_t token_stride, int keys, int wave, int lane)
+    // the tile of keys key ..
+    __device__ void fetch(int key, int keys, lds_byte *tile, int wave, int lane)
     {
-        rows = data;
-        stride = token_stride;
-        last = keys - 1;
-        place(0, wave, lane);
-    }
-    // the tile of keys key ..; rows beyond the last are the last's (they are not seen)
-    __device__ void fetch(int key, lds_byte *tile, int wave, int lane)
-    {
-        if (key > 0 && key + kKeys > last + 1) place(key, wave, lane);
+        if (key + kKeys > keys) place(keys - key, wave, lane);
+        const uint8_t *from = rows + (int64_t)key * stride;
 #pragma unroll
-        for (int i = 0; i < T::kLoads; ++i) {
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)at[i],
+        for (int i = 0; i < T::kLoads; ++i)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(from + at[i]),
                                              (__attribute__((address_space(3))) void *)(tile + (wave * T::kLoads + i) * 1024), 16, 0, 0);
-            at[i] += kKeys * stride;
-        }
     }
 };
 
@@ -94,6 +88,12 @@ template <int D> __device__ __forceinline__ half4_t read_values(const lds_byte *
 }
 
 __device__ __forceinline__ bool finite16(_Float16 x) { return (__builtin_bit_cast(uint16_t, x) & 0x7c00) != 0x7c00; }
+
+__device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b)
+{
+    typedef uint16_t u2_t __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u2_t, a), __builtin_bit_cast(u2_t, b)));
+}
 
 // Item -> sequence and row tile (64 lanes call together); the items of a sequence come last tile first, its longest
 __device__ __forceinline__ bool find_tile(const PromptArgs &a, int item, int *sequence, int *tile)
@@ -130,6 +130,7 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prompt
     constexpr int kParts = D / 16; // products of 16 channels per score
     constexpr int kBlocks = D / 32; // blocks of 32 channels of the output
     __shared__ __attribute__((aligned(16))) uint8_t tiles[2][2][T::kBytes];
+    __shared__ int flags[kThreads / 64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
     const int group = a.heads / a.kv_heads, head = blockIdx.x % a.kv_heads;
     int sequence, tile;
@@ -174,49 +175,67 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prompt
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b) value_at[b] = value_base<D>(b, lane);
     lds_byte *const lds = (lds_byte *)&tiles[0][0][0];
-    Source<D, false> k_source;
-    Source<D, true> v_source;
+    Source<D, false> k_source{reinterpret_cast<const uint8_t *>(k), (uint32_t)a.k_token * 2, {}};
+    Source<D, true> v_source{reinterpret_cast<const uint8_t *>(v), (uint32_t)a.v_token * 2, {}};
+    k_source.place(kKeys, wave, lane);
+    v_source.place(kKeys, wave, lane);
     if (most > 0) {
-        k_source.start(k, a.k_token, keys, wave, lane);
-        v_source.start(v, a.v_token, keys, wave, lane);
-        k_source.fetch(0, lds, wave, lane);
-        v_source.fetch(0, lds + T::kBytes, wave, lane);
+        k_source.fetch(0, keys, lds, wave, lane);
+        v_source.fetch(0, keys, lds + T::kBytes, wave, lane);
     }
+    const int least = ahead + tile * kRows / group; // what the workgroup's first row sees
 #pragma unroll 1
     for (int key = 0, turn = 0; key < most; key += kKeys, turn ^= 1) {
         __syncthreads(); // this tile has arrived, the other one is free
         if (key + kKeys < most) {
             lds_byte *next = lds + (turn ^ 1) * 2 * T::kBytes;
-            k_source.fetch(key + kKeys, next, wave, lane);
-            v_source.fetch(key + kKeys, next + T::kBytes, wave, lane);
+            k_source.fetch(key + kKeys, keys, next, wave, lane);
+            v_source.fetch(key + kKeys, keys, next + T::kBytes, wave, lane);
+        }
+        lds_byte *const kt = lds + turn * 2 * T::kBytes, *const vt = kt + T::kBytes;
+        bool odd = false; // a value that is not finite, in a tile that some row does not see whole: 0 * infinity is NaN
+        if (key + kKeys > least) {
+            uint32_t worst = 0;
+#pragma unroll
+            for (int i = 0; i < T::kLoads; ++i) {
+                const uint4_t x = *(const __attribute__((address_space(3))) uint4_t *)(vt + (i * kThreads + threadIdx.x) * 16);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) worst = max_halves(worst, x[j] & 0x7fff7fffu);
+            }
+            const bool bad = __any((worst & 0xffff) >= 0x7c00 || worst >= 0x7c000000u);
+            if (lane == 0) flags[wave] = bad;
+            __syncthreads();
+            odd = flags[0] | flags[1] | flags[2] | flags[3];
+            if (odd) { // such values leave the tile and are added to the rows that see them
+#pragma unroll
+                for (int i = 0; i < T::kLoads; ++i) {
+                    __attribute__((address_space(3))) half8_t *x = (__attribute__((address_space(3))) half8_t *)(vt + (i * kThreads + threadIdx.x) * 16);
+                    half8_t y = *x;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (!finite16(y[j])) y[j] = 0;
+                    *x = y;
+                }
+                __syncthreads();
+            }
         }
         if (key >= wave_most) continue;
-        const lds_byte *kt = lds + turn * 2 * T::kBytes, *vt = kt + T::kBytes;
         float16_t s[2];
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) s[b][j] = 0;
-#pragma unroll
             for (int i = 0; i < kParts; ++i) {
                 const half8_t x = *(const __attribute__((address_space(3))) half8_t *)(kt + key_at[i] + b * 32 * D * 2);
-                s[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, q[i], s[b], 0, 0, 0);
+                s[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, q[i], i == 0 ? float16_t{} : s[b], 0, 0, 0);
             }
         }
-        const bool masked = key + kKeys > wave_least;
-        bool odd = false; // a value that is not finite, in a tile that some row sees only in part
-        if (masked) {
+        if (key + kKeys > wave_least) {
+            const int seen = sees - key - 4 * h;
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
-                    if (key + b * 32 + 8 * (j >> 2) + 4 * h + (j & 3) >= sees) s[b][j] = -INFINITY;
-            for (int i = lane; i < T::kBytes / 16; i += 64) {
-                const half8_t x = *(const __attribute__((address_space(3))) half8_t *)(vt + i * 16);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) odd = odd || !finite16(x[j]);
-            }
-            odd = __any(odd);
+                    if (b * 32 + 8 * (j >> 2) + (j & 3) >= seen) s[b][j] = -INFINITY;
         }
         float top = s[0][0];
 #pragma unroll
@@ -233,42 +252,31 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prompt
         const float base = m == -INFINITY ? 0.0f : m * scale;
         half8_t p[4];
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][j], scale, -base));
-                l += x;
-                p[2 * b + (j >> 3)][j & 7] = (_Float16)x;
+            for (int j = 0; j < 8; j += 2) {
+                const float2_t x = {__builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 1][8 * (i & 1) + j], scale, -base)),
+                                    __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 1][8 * (i & 1) + j + 1], scale, -base))};
+                const half2_t y = __builtin_convertvector(x, half2_t);
+                l = __builtin_amdgcn_fdot2(y, half2_t{1, 1}, l, false); // the weights as they are used
+                p[i][j] = y[0];
+                p[i][j + 1] = y[1];
             }
-        if (!odd) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int b = 0; b < kBlocks; ++b) {
-                    const half4_t lo = read_values<D>(vt + value_at[b], 16 * i), hi = read_values<D>(vt + value_at[b], 16 * i + 8);
-                    o[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), p[i], o[b], 0, 0, 0);
-                }
-        } else {
-            // 0 * infinity is NaN: such values stay out of the products and are added to the rows that see them
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int b = 0; b < kBlocks; ++b) {
-                    const half4_t lo = read_values<D>(vt + value_at[b], 16 * i), hi = read_values<D>(vt + value_at[b], 16 * i + 8);
-                    half8_t x = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (!finite16(x[j])) x[j] = 0;
-                    o[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, p[i], o[b], 0, 0, 0);
-                }
-            for (int j = 0; j < kKeys; ++j) {
-                if (key + j >= sees) break;
+            for (int b = 0; b < kBlocks; ++b) {
+                const half4_t lo = read_values<D>(vt + value_at[b], 16 * i), hi = read_values<D>(vt + value_at[b], 16 * i + 8);
+                o[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), p[i], o[b], 0, 0, 0);
+            }
+        if (odd) {
+            const _Float16 *row_of = v + key * a.v_token + 4 * h;
+            for (int j = 0; j < kKeys && key + j < sees; ++j, row_of += a.v_token) {
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int d = 32 * b + 8 * i + 4 * h;
-                        const half4_t x = *(const __attribute__((address_space(3))) half4_t *)(vt + j * D * 2 + T::value_chunk(j, d >> 3) * 16 + (d & 4) * 2);
+                        const half4_t x = *reinterpret_cast<const half4_t *>(row_of + 32 * b + 8 * i);
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
                             if (!finite16(x[e])) o[b][4 * i + e] += (float)x[e];

@@ -130,6 +130,8 @@ extern "C" ap_status ap_attention_prompt(const ap_prompt *a, void *stream)
     if (a->tokens < 0 || a->tokens > kMaxTokens || a->keys < 0 || a->keys > kMaxTokens || a->sequences < 0 || a->sequences > (1 << 20) ||
         (a->tokens > 0 && a->sequences < 1) || a->tokens * a->heads > kMaxTokens)
         return AP_ERR_SHAPE;
+    // a tile of 64 rows of k or v is addressed by 32 bits from its first
+    if (a->k.token_stride < 0 || a->k.token_stride > 1 << 25 || a->v.token_stride < 0 || a->v.token_stride > 1 << 25) return AP_ERR_SHAPE;
     if (a->tokens == 0) return AP_OK;
     if (!rows_ok(a->q) || (a->keys > 0 && (!rows_ok(a->k) || !rows_ok(a->v))) || !a->q_starts || !a->k_starts || !aligned(a->q_starts, 4) ||
         !aligned(a->k_starts, 4) || !a->out || !aligned(a->out, 16) || !std::isfinite(a->scale))
