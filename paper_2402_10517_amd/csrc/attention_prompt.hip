@@ -69,12 +69,23 @@ template <int D, bool VALUES> struct Source {
     {
         if (key + kKeys > keys) place(keys - key, wave, lane);
         const uint8_t *from = rows + (int64_t)key * stride;
-#pragma unroll
-        for (int i = 0; i < T::kLoads; ++i)
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(from + at[i]),
-                                             (__attribute__((address_space(3))) void *)(tile + (wave * T::kLoads + i) * 1024), 16, 0, 0);
+        const uint32_t to = (uint32_t)(uintptr_t)tile + wave * T::kLoads * 1024;
+        // In assembly, as the compiler would have every later read of LDS wait for these loads; the loop waits for them before its barrier.  The s_nop's are the
+        // distances from a vector instruction that may have written the scalar operands, and from m0 to its use.
+        if constexpr (T::kLoads == 4)
+            asm volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\ts_add_i32 m0, %0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %5\n\t"
+                         "s_add_i32 m0, %0, 0x800\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %5\n\ts_add_i32 m0, %0, 0xc00\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, %5"
+                         :
+                         : "s"(to), "v"(at[0]), "v"(at[1]), "v"(at[T::kLoads - 2]), "v"(at[T::kLoads - 1]), "s"(from)
+                         : "memory", "m0", "scc");
+        else
+            asm volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\ts_add_i32 m0, %0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3"
+                         :
+                         : "s"(to), "v"(at[0]), "v"(at[1]), "s"(from)
+                         : "memory", "m0", "scc");
     }
 };
+__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // Four keys (4 h .. of 8, from `key`) of channel 32 block + lane % 32, transposed on the way from LDS; at: value_base
 template <int D> __device__ __forceinline__ int value_base(int block, int lane)
@@ -186,6 +197,7 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prompt
     const int least = ahead + tile * kRows / group; // what the workgroup's first row sees
 #pragma unroll 1
     for (int key = 0, turn = 0; key < most; key += kKeys, turn ^= 1) {
+        arrived();
         __syncthreads(); // this tile has arrived, the other one is free
         if (key + kKeys < most) {
             lds_byte *next = lds + (turn ^ 1) * 2 * T::kBytes;
@@ -221,14 +233,15 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prompt
         }
         if (key >= wave_most) continue;
         float16_t s[2];
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        for (int i = 0; i < kParts; ++i)
 #pragma unroll
-            for (int i = 0; i < kParts; ++i) {
+            for (int b = 0; b < 2; ++b) {
                 const half8_t x = *(const __attribute__((address_space(3))) half8_t *)(kt + key_at[i] + b * 32 * D * 2);
                 s[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, q[i], i == 0 ? float16_t{} : s[b], 0, 0, 0);
             }
-        }
+        __builtin_amdgcn_s_setprio(0);
         if (key + kKeys > wave_least) {
             const int seen = sees - key - 4 * h;
 #pragma unroll
@@ -262,6 +275,7 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prompt
                 p[i][j] = y[0];
                 p[i][j + 1] = y[1];
             }
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -269,6 +283,7 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prompt
                 const half4_t lo = read_values<D>(vt + value_at[b], 16 * i), hi = read_values<D>(vt + value_at[b], 16 * i + 8);
                 o[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), p[i], o[b], 0, 0, 0);
             }
+        __builtin_amdgcn_s_setprio(0);
         if (odd) {
             const _Float16 *row_of = v + key * a.v_token + 4 * h;
             for (int j = 0; j < kKeys && key + j < sees; ++j, row_of += a.v_token) {
