@@ -36,6 +36,8 @@ constexpr int kRows = kWaveRows * kThreads / 64;
 constexpr int kKeys = 64; // keys of a tile
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.0f;
+// instruction classes of the scheduler's groups
+constexpr int kProducts = 0x8, kLdsReads = 0x100;
 
 // A tile of kKeys rows of D values in LDS.  chunk(row, i): where the 16-byte chunk i of a row is
 template <int D> struct Tile {
@@ -241,6 +243,15 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prompt
                 const half8_t x = *(const __attribute__((address_space(3))) half8_t *)(kt + key_at[i] + b * 32 * D * 2);
                 s[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, q[i], i == 0 ? float16_t{} : s[b], 0, 0, 0);
             }
+        if constexpr (D == 128) { // operands of the scores six reads ahead; at head_dim 64 four waves per SIMD do better without
+            __builtin_amdgcn_sched_group_barrier(kLdsReads, 6, 0);
+#pragma unroll
+            for (int i = 0; i < 2 * kParts - 6; ++i) {
+                __builtin_amdgcn_sched_group_barrier(kProducts, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kLdsReads, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(kProducts, 6, 0);
+        }
         __builtin_amdgcn_s_setprio(0);
         if (key + kKeys > wave_least) {
             const int seen = sees - key - 4 * h;
@@ -283,6 +294,14 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prompt
                 const half4_t lo = read_values<D>(vt + value_at[b], 16 * i), hi = read_values<D>(vt + value_at[b], 16 * i + 8);
                 o[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), p[i], o[b], 0, 0, 0);
             }
+        // operands of the values 32 keys ahead
+        __builtin_amdgcn_sched_group_barrier(kLdsReads, 4 * kBlocks, 0);
+#pragma unroll
+        for (int i = 0; i < 2 * kBlocks; ++i) {
+            __builtin_amdgcn_sched_group_barrier(kProducts, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(kLdsReads, 2, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(kProducts, 2 * kBlocks, 0);
         __builtin_amdgcn_s_setprio(0);
         if (odd) {
             const _Float16 *row_of = v + key * a.v_token + 4 * h;
