@@ -107,7 +107,9 @@ ap_status ap_attention_cached(const ap_cache *c, const ap_cached *a, void *strea
  *   q; k, v    tokens rows of heads heads (tokens * heads < 2^31 - 256); keys rows of kv_heads heads, their token strides in
  *              0 .. 2^25 (AP_ERR_SHAPE otherwise)
  *   out        device, tokens x heads x head_dim, contiguous, 16-byte aligned; only the tokens of q_starts are written
- * Scores, softmax and sums are binary32; the weights of the values are rounded to binary16.
+ *   work       device, ap_attention_prompt_size bytes, 16-byte aligned; may be NULL where that is 0
+ * Scores, softmax and sums are binary32; the weights of the values are rounded to binary16.  Where the rows are too few for the card the keys are divided
+ * among workgroups and joined by a second launch.
  */
 typedef struct {
     ap_heads q, k, v;
@@ -116,8 +118,10 @@ typedef struct {
     int sequences;
     const int32_t *q_starts, *k_starts;
     float scale;
-    void *out;
+    void *out, *work;
+    size_t work_bytes;
 } ap_prompt;
+ap_status ap_attention_prompt_size(const ap_prompt *a, size_t *bytes);
 ap_status ap_attention_prompt(const ap_prompt *a, void *stream);
 
 /*

@@ -28,7 +28,7 @@ EXPORTS = ["ap_packed_size", "ap_pack_host", "ap_unpack_host", "ap_blob_lut_entr
            "ap_free", "ap_strerror"]
 
 DECODE_EXPORTS = ["ap_cache_size", "ap_cache_append", "ap_cache_read", "ap_attention_cached_size", "ap_attention_cached",
-                  "ap_attention_prompt", "ap_verify_size", "ap_verify"]   # include/apdecode.h
+                  "ap_attention_prompt_size", "ap_attention_prompt", "ap_verify_size", "ap_verify"]   # include/apdecode.h
 
 
 OPTIONS = {"waves": 0, "row_groups": 1, "mfma_min_batch": 2, "variant": 3}
@@ -79,6 +79,7 @@ def _load():
     L.ap_cache_read.argtypes = [vp, vp, ctypes.c_int64, vp, vp, vp]
     L.ap_attention_cached_size.argtypes = [vp, vp, psz]
     L.ap_attention_cached.argtypes = [vp, vp, vp]
+    L.ap_attention_prompt_size.argtypes = [vp, psz]
     L.ap_attention_prompt.argtypes = [vp, vp]
     L.ap_verify_size.argtypes = [vp, psz]
     L.ap_verify.argtypes = [vp, vp]
@@ -414,11 +415,12 @@ def ap_attention_cached(cache, q, tables, lengths, q_starts=None, scale=None, ma
                    "ap_attention_cached")
 
 
-def ap_attention_prompt(q, k, v, q_starts, k_starts=None, scale=None, out=None, stream=None):
+def ap_attention_prompt(q, k, v, q_starts, k_starts=None, scale=None, out=None, work=None, stream=None):
     """Causal attention over packed sequences: q (tokens, heads, head_dim), k and v (keys, kv_heads, head_dim); q_starts, k_starts: int32
-    (sequences + 1,), k_starts = q_starts if None.  The last query of a sequence sees its last key.  `stream` as in ap_gemv."""
+    (sequences + 1,), k_starts = q_starts if None.  The last query of a sequence sees its last key.  `stream` and work as in
+    ap_attention_cached."""
     return _result(_torch_call.attention_prompt(q, k, v, q_starts, q_starts if k_starts is None else k_starts, scale, out,
-                                                _named(stream)), "ap_attention_prompt")
+                                                work, _named(stream)), "ap_attention_prompt")
 
 
 def ap_verify(target, draft, drafted, uniform, noise, counts=None, work=None, stream=None):

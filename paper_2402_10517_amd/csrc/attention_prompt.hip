@@ -25,9 +25,11 @@ struct PromptArgs {
     const _Float16 *q, *k, *v;
     int64_t q_token, q_head, k_token, k_head, v_token, v_head;
     const int32_t *q_starts, *k_starts;
-    int tokens, keys, heads, kv_heads, sequences, items;
+    int tokens, keys, heads, kv_heads, sequences, items, splits;
     float scale, slack;
     _Float16 *out;
+    float *part;  // splits x rows x D: sums of range s
+    float2 *stat; // splits x rows: their maximum and sum of weights
 };
 
 constexpr int kThreads = 256;
@@ -36,6 +38,10 @@ constexpr int kRows = kWaveRows * kThreads / 64;
 constexpr int kKeys = 64; // keys of a tile
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.0f;
+// Weights are 2^7 e^(..): up to 2^15, and above the subnormal numbers of binary16 down to 2^-21 of the greatest
+constexpr float kRaise = 7.0f;
+constexpr int kLeastTiles = 4;    // of a range of keys
+constexpr int kJoinThreads = 256;
 // instruction classes of the scheduler's groups
 constexpr int kProducts = 0x8, kLdsReads = 0x100;
 
@@ -108,6 +114,16 @@ __device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b)
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u2_t, a), __builtin_bit_cast(u2_t, b)));
 }
 
+// How the keys that a row tile's last row sees are divided among `splits` workgroups: ranges of whole tiles
+struct Range {
+    int count, keys;
+};
+__device__ __forceinline__ Range range_of(int most, int splits)
+{
+    const int tiles = most > 0 ? (most + kKeys - 1) / kKeys : 1, each = (tiles + splits - 1) / splits, of = each < kLeastTiles ? kLeastTiles : each;
+    return Range{(tiles + of - 1) / of, of * kKeys};
+}
+
 // Item -> sequence and row tile (64 lanes call together); the items of a sequence come last tile first, its longest
 __device__ __forceinline__ bool find_tile(const PromptArgs &a, int item, int *sequence, int *tile)
 {
@@ -137,7 +153,7 @@ __device__ __forceinline__ bool find_tile(const PromptArgs &a, int item, int *se
     return false;
 }
 
-template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prompt_kernel(const PromptArgs a)
+template <int D> __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void attention_prompt_kernel(const PromptArgs a)
 {
     typedef Tile<D> T;
     constexpr int kParts = D / 16; // products of 16 channels per score
@@ -147,7 +163,8 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prompt
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
     const int group = a.heads / a.kv_heads, head = blockIdx.x % a.kv_heads;
     int sequence, tile;
-    if (!find_tile(a, blockIdx.x / a.kv_heads, &sequence, &tile)) return;
+    const int rest = blockIdx.x / a.kv_heads, item = rest % a.items, split = rest / a.items;
+    if (!find_tile(a, item, &sequence, &tile)) return;
     sequence = __builtin_amdgcn_readfirstlane(sequence);
     tile = __builtin_amdgcn_readfirstlane(tile);
     int64_t q0, q1, k0, k1;
@@ -173,6 +190,10 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prompt
     const int most = ahead + token_of(tile * kRows + kRows - 1), first_row = tile * kRows + wave * kWaveRows;
     const int wave_least = ahead + token_of(first_row), wave_most = first_row / group < n ? ahead + token_of(first_row + kWaveRows - 1) : 0;
 
+    const Range range = range_of(most, a.splits);
+    const int from = split * range.keys, to = most < from + range.keys ? most : from + range.keys;
+    if (split >= range.count) return;
+
     const _Float16 *k = a.k + k0 * a.k_token + head * a.k_head, *v = a.v + k0 * a.v_token + head * a.v_head;
     float16_t o[kBlocks];
 #pragma unroll
@@ -192,16 +213,16 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prompt
     Source<D, true> v_source{reinterpret_cast<const uint8_t *>(v), (uint32_t)a.v_token * 2, {}};
     k_source.place(kKeys, wave, lane);
     v_source.place(kKeys, wave, lane);
-    if (most > 0) {
-        k_source.fetch(0, keys, lds, wave, lane);
-        v_source.fetch(0, keys, lds + T::kBytes, wave, lane);
+    if (to > from) {
+        k_source.fetch(from, keys, lds, wave, lane);
+        v_source.fetch(from, keys, lds + T::kBytes, wave, lane);
     }
     const int least = ahead + tile * kRows / group; // what the workgroup's first row sees
 #pragma unroll 1
-    for (int key = 0, turn = 0; key < most; key += kKeys, turn ^= 1) {
+    for (int key = from, turn = 0; key < to; key += kKeys, turn ^= 1) {
         arrived();
         __syncthreads(); // this tile has arrived, the other one is free
-        if (key + kKeys < most) {
+        if (key + kKeys < to) {
             lds_byte *next = lds + (turn ^ 1) * 2 * T::kBytes;
             k_source.fetch(key + kKeys, keys, next, wave, lane);
             v_source.fetch(key + kKeys, keys, next + T::kBytes, wave, lane);
@@ -273,7 +294,7 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prompt
 #pragma unroll
             for (int i = 0; i < kBlocks; ++i) o[i] *= keep;
         }
-        const float base = m == -INFINITY ? 0.0f : m * scale;
+        const float base = (m == -INFINITY ? 0.0f : m * scale) - kRaise;
         half8_t p[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -320,7 +341,18 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prompt
     }
     l += __shfl_xor(l, 32);
     if (!valid) return;
-    _Float16 *out = a.out + ((q0 + token) * a.heads + head * group + (row - token * group)) * D + 4 * h;
+    const int64_t place = (q0 + token) * a.heads + head * group + (row - token * group);
+    if (range.count > 1) {
+        float *part = a.part + ((int64_t)split * a.tokens * a.heads + place) * D + 4 * h;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<float4_t *>(part + 32 * b + 8 * i) = float4_t{o[b][4 * i], o[b][4 * i + 1], o[b][4 * i + 2], o[b][4 * i + 3]};
+        if (h == 0) a.stat[(int64_t)split * a.tokens * a.heads + place] = make_float2(m, l);
+        return;
+    }
+    _Float16 *out = a.out + place * D + 4 * h;
     const float scale_out = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)
@@ -333,7 +365,72 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prompt
         }
 }
 
+// Joins the ranges of rows whose tile has more than one: D / 4 lanes a row
+template <int D> __global__ __launch_bounds__(kJoinThreads) void attention_prompt_join_kernel(const PromptArgs a)
+{
+    constexpr int kLanes = D / 4, kEach = kJoinThreads / kLanes;
+    const int groups = (a.heads + kEach - 1) / kEach, token = blockIdx.x / groups, lane = threadIdx.x % kLanes, group = a.heads / a.kv_heads;
+    const int head = (blockIdx.x - token * groups) * kEach + threadIdx.x / kLanes;
+    const int s = sequence_of(a.q_starts, token, a.tokens, a.sequences);
+    if (s < 0 || head >= a.heads) return;
+    int64_t q0, q1, k0, k1;
+    token_range(a.q_starts, s, a.tokens, a.sequences, &q0, &q1);
+    token_range(a.k_starts, s, a.keys, a.sequences, &k0, &k1);
+    // what the last row of this row's tile sees, as in the kernel above
+    const int n = (int)(q1 - q0), row = (int)(token - q0) * group + head % group, last = (row / kRows * kRows + kRows - 1) / group;
+    const Range range = range_of((int)(k1 - k0) - n + 1 + (last < n ? last : n - 1), a.splits);
+    if (range.count == 1) return;
+    const int64_t place = (int64_t)token * a.heads + head, rows = (int64_t)a.tokens * a.heads;
+    const float scale = fabsf(a.scale) * kLog2e;
+    float top = -INFINITY;
+    for (int i = 0; i < range.count; ++i) top = fmaxf(top, a.stat[i * rows + place].x);
+    float total = 0;
+    float4_t x = {0, 0, 0, 0};
+#pragma unroll 4
+    for (int i = 0; i < range.count; ++i) {
+        const float2 st = a.stat[i * rows + place];
+        // a range without a finite maximum has no key that the row sees, or only NaN: its sums are 0 or NaN and go in as they are
+        const float keep = st.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((st.x - top) * scale);
+        total += keep * st.y;
+        x += keep * *reinterpret_cast<const float4_t *>(a.part + (i * rows + place) * D + lane * 4);
+    }
+    half4_t y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = (_Float16)(total == 0.0f ? 0.0f : x[e] / total);
+    *reinterpret_cast<half4_t *>(a.out + place * D + lane * 4) = y;
+}
+
+struct PromptPlan {
+    int64_t items;
+    int splits;
+};
+
+// Row tiles (at most), and the ranges of keys that they are divided into: as many as fill the places that the card has for workgroups (two per CU at head_dim
+// 128, four at 64), of four tiles at least, where that saves more than it costs: a workgroup takes about 0.9 us for a tile of 64 keys (0.6 at head_dim 64), the
+// second launch 5 us, and the sums go through memory, written and read, at 4 TB/s.  us without / with ranges: 1 query of 8 heads over 4000 keys 72 / 16,
+// 200 of 32 over 8000 141 / 48, 3 x 500 of 16 x 64 over 7500 109 / 74; where the rule keeps to one: 512 of 32 over 512 16 / 21, 2000 of 16 x 64 over 2000 32 / 34.
+PromptPlan plan_of(const ap_prompt &a)
+{
+    PromptPlan p;
+    p.items = a.tokens * (a.heads / a.kv_heads) / kRows + a.sequences;
+    const int64_t places = a.head_dim == 64 ? 1024 : 512, units = p.items * a.kv_heads, each = a.keys / a.sequences, room = each / (kKeys * kLeastTiles);
+    int64_t splits = places / units;
+    splits = splits > room ? room : splits > 64 ? 64 : splits;
+    if (splits > 1) {
+        const double alone = (double)each / kKeys * (a.head_dim == 64 ? 0.6 : 0.9), sums = 2.0 * splits * a.tokens * a.heads * a.head_dim * sizeof(float);
+        if (alone * (1.0 - 1.0 / splits) < 5.0 + sums / 4e6) splits = 1;
+    }
+    p.splits = (int)(splits < 1 ? 1 : splits);
+    return p;
+}
+
 } // namespace
+
+size_t attention_prompt_work(const ap_prompt &a)
+{
+    const PromptPlan p = plan_of(a);
+    return p.splits == 1 ? 0 : (size_t)p.splits * a.tokens * a.heads * (a.head_dim * sizeof(float) + sizeof(float2));
+}
 
 hipError_t launch_attention_prompt(const ap_prompt &a, hipStream_t stream)
 {
@@ -351,11 +448,20 @@ hipError_t launch_attention_prompt(const ap_prompt &a, hipStream_t stream)
     k.scale = fabsf(a.scale) < 1e-30f ? 1e-30f : a.scale;
     k.slack = kSlack / (fabsf(k.scale) * kLog2e);
     k.out = static_cast<_Float16 *>(a.out);
-    const int64_t items = a.tokens * (a.heads / a.kv_heads) / kRows + a.sequences, blocks = items * a.kv_heads;
+    const PromptPlan p = plan_of(a);
+    const int64_t blocks = p.items * a.kv_heads * p.splits;
     if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-    k.items = (int)items;
+    k.items = (int)p.items, k.splits = p.splits;
+    k.part = static_cast<float *>(a.work);
+    k.stat = reinterpret_cast<float2 *>(k.part + (size_t)p.splits * a.tokens * a.heads * a.head_dim);
     if (a.head_dim == 64) attention_prompt_kernel<64><<<dim3((unsigned)blocks), kThreads, 0, stream>>>(k);
     else attention_prompt_kernel<128><<<dim3((unsigned)blocks), kThreads, 0, stream>>>(k);
+    if (p.splits > 1) {
+        const int each = kJoinThreads / (a.head_dim / 4);
+        const dim3 join((unsigned)(a.tokens * ((a.heads + each - 1) / each)));
+        if (a.head_dim == 64) attention_prompt_join_kernel<64><<<join, kJoinThreads, 0, stream>>>(k);
+        else attention_prompt_join_kernel<128><<<join, kJoinThreads, 0, stream>>>(k);
+    }
     return hipGetLastError();
 }
 

@@ -35,6 +35,7 @@ hipError_t launch_cache_append(const ap_cache &c, const ap_append &a, hipStream_
 hipError_t launch_cache_read(const ap_cache &c, const int64_t *slots, int64_t tokens, void *k, void *v, hipStream_t stream);
 size_t attention_cached_work(const ap_cache &c, const ap_cached &a);
 hipError_t launch_attention_cached(const ap_cache &c, const ap_cached &a, hipStream_t stream);
+size_t attention_prompt_work(const ap_prompt &a);
 hipError_t launch_attention_prompt(const ap_prompt &a, hipStream_t stream);
 size_t verify_work(const ap_verification &a);
 hipError_t launch_verify(const ap_verification &a, hipStream_t stream);

@@ -121,7 +121,7 @@ extern "C" ap_status ap_attention_cached(const ap_cache *c, const ap_cached *a, 
     return done(launch_attention_cached(*c, *a, static_cast<hipStream_t>(stream)));
 }
 
-extern "C" ap_status ap_attention_prompt(const ap_prompt *a, void *stream)
+static ap_status check_prompt(const ap_prompt *a)
 {
     if (!a) return AP_ERR_INVALID_ARG;
     if (!head_dim_ok(a->head_dim)) return AP_ERR_SHAPE;
@@ -132,10 +132,29 @@ extern "C" ap_status ap_attention_prompt(const ap_prompt *a, void *stream)
         return AP_ERR_SHAPE;
     // a tile of 64 rows of k or v is addressed by 32 bits from its first
     if (a->k.token_stride < 0 || a->k.token_stride > 1 << 25 || a->v.token_stride < 0 || a->v.token_stride > 1 << 25) return AP_ERR_SHAPE;
+    return AP_OK;
+}
+
+extern "C" ap_status ap_attention_prompt_size(const ap_prompt *a, size_t *bytes)
+{
+    const ap_status s = check_prompt(a);
+    if (s != AP_OK) return s;
+    if (!bytes) return AP_ERR_INVALID_ARG;
+    *bytes = a->tokens == 0 ? 0 : attention_prompt_work(*a);
+    return AP_OK;
+}
+
+extern "C" ap_status ap_attention_prompt(const ap_prompt *a, void *stream)
+{
+    const ap_status s = check_prompt(a);
+    if (s != AP_OK) return s;
     if (a->tokens == 0) return AP_OK;
     if (!rows_ok(a->q) || (a->keys > 0 && (!rows_ok(a->k) || !rows_ok(a->v))) || !a->q_starts || !a->k_starts || !aligned(a->q_starts, 4) ||
         !aligned(a->k_starts, 4) || !a->out || !aligned(a->out, 16) || !std::isfinite(a->scale))
         return AP_ERR_INVALID_ARG;
+    const size_t need = attention_prompt_work(*a);
+    if (need && (!a->work || !aligned(a->work, 16))) return AP_ERR_INVALID_ARG;
+    if (a->work_bytes < need) return AP_ERR_BUFFER_TOO_SMALL;
     return done(launch_attention_prompt(*a, static_cast<hipStream_t>(stream)));
 }
 

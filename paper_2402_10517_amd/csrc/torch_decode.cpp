@@ -256,10 +256,10 @@ PyObject *attention_cached(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
-// attention_prompt(q, k, v, q_starts, k_starts, scale, out, stream) -> out, or a status
+// attention_prompt(q, k, v, q_starts, k_starts, scale, out, work, stream) -> out, or a status
 PyObject *attention_prompt(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
-    return guarded(args, n, 8, [&]() -> PyObject * {
+    return guarded(args, n, 9, [&]() -> PyObject * {
         Call c;
         const at::Tensor &q = c.tensor(args[0], "q"), &k = c.tensor(args[1], "k");
         if (!q.is_cuda() || q.dim() != 3 || k.dim() != 3) refuse("q and k", "must be float16 tensors (tokens, heads, head_dim) on the GPU");
@@ -280,10 +280,14 @@ PyObject *attention_prompt(PyObject *, PyObject *const *args, Py_ssize_t n)
         a.q_starts = static_cast<const int32_t *>(c.array(args[3], "q_starts", at::kInt, starts.size(0)));
         a.k_starts = static_cast<const int32_t *>(c.array(args[4], "k_starts", at::kInt, starts.size(0)));
         a.scale = c.scale(args[5], D);
-        c.start(args[7]);
+        size_t bytes = 0;
+        ap_status status = ap_attention_prompt_size(&a, &bytes);
+        if (status != AP_OK) return PyLong_FromLong(-(long)status);
+        c.start(args[8]);
         const at::Tensor out = c.output(args[6], "out", {a.tokens, a.heads, D}, at::kHalf);
+        const at::Tensor work = c.workspace(args[7], bytes, &a.work, &a.work_bytes);
         a.out = out.data_ptr();
-        const ap_status status = without_gil([&] { return ap_attention_prompt(&a, c.stream.address); });
+        status = without_gil([&] { return ap_attention_prompt(&a, c.stream.address); });
         return status == AP_OK ? THPVariable_Wrap(out) : PyLong_FromLong(status);
     });
 }

@@ -28,7 +28,7 @@ class Cached(ctypes.Structure):
 
 class Prompt(ctypes.Structure):
     _fields_ = [("q", Heads), ("k", Heads), ("v", Heads), ("heads", ci), ("kv_heads", ci), ("head_dim", ci), ("tokens", i64), ("keys", i64), ("sequences", ci),
-                ("q_starts", vp), ("k_starts", vp), ("scale", ctypes.c_float), ("out", vp)]
+                ("q_starts", vp), ("k_starts", vp), ("scale", ctypes.c_float), ("out", vp), ("work", vp), ("work_bytes", ctypes.c_size_t)]
 
 
 class Verification(ctypes.Structure):
@@ -59,7 +59,7 @@ def cached(**kw):
 
 def prompt(**kw):
     return Prompt(**dict(dict(q=rows(), k=rows(), v=rows(), heads=8, kv_heads=2, head_dim=128, tokens=3, keys=3, sequences=2, q_starts=P, k_starts=P, scale=0.1,
-                              out=P), **kw))
+                              out=P, work=P, work_bytes=1 << 40), **kw))
 
 
 def verification(**kw):
@@ -140,6 +140,17 @@ def test_prompt_refusals():
     for bad in (dict(heads=0), dict(heads=3), dict(kv_heads=0), dict(head_dim=96), dict(tokens=-1), dict(keys=-1), dict(sequences=0), dict(keys=1 << 40)):
         assert ask(prompt(**bad)) == SHAPE, bad
     assert ask(prompt(tokens=0, q=rows(data=None))) == 0
+    for bad in (dict(k=rows(token_stride=-128)), dict(v=rows(token_stride=(1 << 25) + 8))):
+        assert ask(prompt(**bad)) == SHAPE, bad
+    size = ctypes.c_size_t(7)
+    long = prompt(keys=1 << 18)
+    assert B.lib.ap_attention_prompt_size(ctypes.byref(long), ctypes.byref(size)) == 0 and size.value > 0
+    long.work_bytes = size.value - 1
+    assert ask(long) == SMALL
+    long.work, long.work_bytes = None, size.value
+    assert ask(long) == INVALID
+    assert B.lib.ap_attention_prompt_size(ctypes.byref(prompt(tokens=0)), ctypes.byref(size)) == 0 and size.value == 0
+    assert B.lib.ap_attention_prompt_size(ctypes.byref(prompt()), None) == INVALID
 
 
 def test_verify_refusals():

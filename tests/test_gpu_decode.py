@@ -285,6 +285,32 @@ def test_prompt_long(B):
     prompt_case(B, [1100, 900], [5000, 901], 5, 1, 64)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_prompt_keys_divided_among_workgroups(B, D):
+    # few rows and many keys; with sequences whose keys are one range, several, none, and queries that see only some of the ranges
+    prompt_case(B, [1], [5000], 8, 8, D)
+    prompt_case(B, [3, 40, 1, 5, 2], [6000, 41, 0, 9000, 1], 8, 2, D)
+    def spoil(k, v):
+        v[4100, 0, 3] = float("nan")
+        v[4201, 1, 5] = float("inf")                            # seen by the last query only
+    out, _ = prompt_case(B, [200], [4202], 2, 2, D, spoil=spoil)
+    bad = ~torch.isfinite(out).all(-1)
+    assert bad[:, 0].tolist() == [4002 + i >= 4100 for i in range(200)] and bad[:, 1].tolist() == [False] * 199 + [True]
+
+
+def test_weights_far_below_the_greatest(B):
+    # one key far above 8191 equal ones, whose weights are small numbers of binary16: they count by their sum
+    for low in (2.0 ** -14, 2.0 ** -18, 2.0 ** -21):
+        q, k, v = torch.zeros((1, 1, 128)), torch.zeros((8192, 1, 128)), torch.ones((8192, 1, 128))
+        q[0, 0, 0], k[0, 0, 0], v[0] = 1.0, 64.0, 0.0
+        q, k, v = q.half().cuda(), k.half().cuda(), v.half().cuda()
+        scale = -np.log(low) / 64
+        out = B.ap_attention_prompt(q, k, v, U.starts([1]).cuda(), U.starts([8192]).cuda(), scale=scale)
+        want = 8191 * low / (1 + 8191 * low)
+        # half a step of binary16 in the result, and the same in the weights down to 2^-21
+        assert (out.double() - want).abs().max().item() <= want * 2 * U.HALF_EPS16 + U.SUBNORMAL16, low
+
+
 def test_prompt_scales(B):
     for scale in (0.0, -0.2, 1.0, 30.0):
         prompt_case(B, [100, 40], [100, 40], 2, 1, 128, scale=scale)
