@@ -93,22 +93,32 @@ template <int D> struct Half {
     uint4_t kp, vp;
 };
 
-// They are read once: past the caches' usual order.  section: where the (page, key head) starts, in scalar registers; t: the first of the 16 keys in it
-template <int D> __device__ __forceinline__ Half<D> load_half(const uint8_t *section, int log_page, int t, int c, int g)
+// Byte offsets of a lane in them: from where the codes and where the pairs of the 16 keys start
+struct Lane {
+    uint32_t k, v, kp, vp;
+};
+
+// They are read once: past the caches' usual order.  section: where the (page, key head) starts; t: the first of the 16 keys in it.  Both starts are kept in scalar registers.
+template <int D> __device__ __forceinline__ Half<D> load_half(const uint8_t *section, int log_page, int t, const Lane &at)
 {
-    typedef CacheLayout<D> L;
     typedef typename Half<D>::words_t words_t;
-    const uint8_t *k = section + L::key(t), *v = section + L::value(log_page, t, 0, 0), *kp = section + L::key_scale(log_page, t), *vp = section + L::value_scale(log_page, t);
+    uintptr_t codes_at = reinterpret_cast<uintptr_t>(section + t * CacheLayout<D>::kRow), pairs_at = reinterpret_cast<uintptr_t>(section + (D << log_page) + 4 * t);
+    asm("" : "+s"(codes_at), "+s"(pairs_at));
+    typedef const __attribute__((address_space(1))) uint8_t *global_t; // memory, and not LDS
+    const global_t codes = (global_t)codes_at, pairs = (global_t)pairs_at;
     Half<D> h;
-    h.k = __builtin_nontemporal_load(reinterpret_cast<const words_t *>(k + (uint32_t)(c * L::kRow + g * (D / 8))));
-    h.v = __builtin_nontemporal_load(reinterpret_cast<const words_t *>(v + (uint32_t)(g * 4 * L::kRow + c * 8 * L::kHalves)));
-    h.kp = __builtin_nontemporal_load(reinterpret_cast<const uint4_t *>(kp + (uint32_t)(g * 16)));
-    h.vp = __builtin_nontemporal_load(reinterpret_cast<const uint4_t *>(vp + (uint32_t)(g * 16)));
+    h.k = __builtin_nontemporal_load((const __attribute__((address_space(1))) words_t *)(codes + at.k));
+    h.v = __builtin_nontemporal_load((const __attribute__((address_space(1))) words_t *)(codes + at.v));
+    h.kp = __builtin_nontemporal_load((const __attribute__((address_space(1))) uint4_t *)(pairs + at.kp));
+    h.vp = __builtin_nontemporal_load((const __attribute__((address_space(1))) uint4_t *)(pairs + at.vp));
     return h;
 }
 
 __device__ __forceinline__ _Float16 low_of(uint32_t pair) { return __builtin_bit_cast(_Float16, (uint16_t)pair); }
 __device__ __forceinline__ _Float16 step_of(uint32_t pair) { return __builtin_bit_cast(_Float16, (uint16_t)(pair >> 16)); }
+
+// A binary16 number times a binary32 one in one mixed-precision instruction
+__device__ __forceinline__ float times(_Float16 x, float y) { return __builtin_fmaf((float)x, y, 0.0f); }
 
 // A constant in a vector register: (w & it) | another constant is then one v_and_or_b32, which takes one scalar operand.  The instruction itself is the compiler's, who
 // knows how far it has to stay from the matrix instruction that reads its result.
@@ -210,18 +220,22 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 6
     }
 
     const int mine = c1 - c0 - kTile * wave, steps = mine > 0 ? (mine + kStep - 1) / kStep : 0;
-    const int page_mask = (1 << a.cache.log_page) - 1;
-    const auto load = [&](int step, int h) {
-        const int page = __builtin_amdgcn_readlane(pages, 2 * step + h);
-        const int t = (c0 + kTile * (wave + kWaves * step) + 16 * h) & page_mask;
-        return load_half<D>(L::block(a.cache, page < 0 ? 0 : page, head), a.cache.log_page, t, c, g);
+    const int lp = a.cache.log_page, page_mask = (1 << lp) - 1;
+    const Lane at{(uint32_t)(c * L::kRow + g * (D / 8)), (uint32_t)((L::kRow << lp) + g * 4 * L::kRow + c * 8 * L::kHalves), (uint32_t)g * 16, (uint32_t)((4 << lp) + g * 16)};
+    const auto load = [&](int step, Half<D> (&h)[2]) {
+        const int t = c0 + kTile * (wave + kWaves * step);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int page = __builtin_amdgcn_readlane(pages, 2 * step + half);
+            h[half] = load_half<D>(L::block(a.cache, page < 0 ? 0 : page, head), lp, (t + 16 * half) & page_mask, at);
+        }
     };
     Half<D> next[2];
-    if (steps > 0) next[0] = load(0, 0), next[1] = load(0, 1);
+    if (steps > 0) load(0, next);
 #pragma unroll 1
     for (int step = 0; step < steps; ++step) {
         Half<D> h[2] = {next[0], next[1]};
-        if (step + 1 < steps) next[0] = load(step + 1, 0), next[1] = load(step + 1, 1);
+        if (step + 1 < steps) load(step + 1, next);
         const int t0 = c0 + kTile * (wave + kWaves * step);
         const bool known0 = __builtin_amdgcn_readlane(pages, 2 * step) >= 0, known1 = __builtin_amdgcn_readlane(pages, 2 * step + 1) >= 0;
         const bool whole = known0 && known1 && t0 + kTile <= sees_least && t0 + kTile <= c1;
@@ -243,7 +257,7 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 6
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const uint32_t kp = h[i >> 2].kp[i & 3];
-                s[r][i >> 2][i & 3] = __builtin_fmaf((float)step_of(kp), s[r][i >> 2][i & 3], (float)low_of(kp) * q_sum[r]);
+                s[r][i >> 2][i & 3] = __builtin_fmaf((float)step_of(kp), s[r][i >> 2][i & 3], times(low_of(kp), q_sum[r]));
                 pairs[i] = h[i >> 2].vp[i & 3];
             }
             if (!whole) {
@@ -279,7 +293,7 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 6
                     const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][(i + j) >> 2][(i + j) & 3], scale, -base));
                     l[r] += p;
                     bias[r] = __builtin_fmaf(p, (float)low_of(pairs[i + j]), bias[r]);
-                    ps[j] = p * (float)step_of(pairs[i + j]);
+                    ps[j] = times(step_of(pairs[i + j]), p);
                 }
                 hi[i / 2] = pack_bf16(ps[0], ps[1]);
                 lo[i / 2] = pack_bf16(ps[0] - __builtin_bit_cast(float, hi[i / 2] << 16), ps[1] - __builtin_bit_cast(float, hi[i / 2] & 0xffff0000u));
