@@ -272,7 +272,7 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 6
             float top = s[r][0][0];
 #pragma unroll
             for (int i = 1; i < 8; ++i) top = fmaxf(top, s[r][i >> 2][i & 3]);
-            if (__any(top > m[r] + a.slack)) {
+            if (__any(top - m[r] > a.slack)) { // also from -inf; a sum could round a difference of large scores away
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
                 const float next_m = fmaxf(m[r], top), keep = next_m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m[r] - next_m) * scale);

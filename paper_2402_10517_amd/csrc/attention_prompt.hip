@@ -191,7 +191,7 @@ template <int D> __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void at
     const int wave_least = ahead + token_of(first_row), wave_most = first_row / group < n ? ahead + token_of(first_row + kWaveRows - 1) : 0;
 
     const Range range = range_of(most, a.splits);
-    const int from = split * range.keys, to = most < from + range.keys ? most : from + range.keys;
+    const int begin = split * range.keys, to = most < begin + range.keys ? most : begin + range.keys;
     if (split >= range.count) return;
 
     const _Float16 *k = a.k + k0 * a.k_token + head * a.k_head, *v = a.v + k0 * a.v_token + head * a.v_head;
@@ -213,13 +213,13 @@ template <int D> __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void at
     Source<D, true> v_source{reinterpret_cast<const uint8_t *>(v), (uint32_t)a.v_token * 2, {}};
     k_source.place(kKeys, wave, lane);
     v_source.place(kKeys, wave, lane);
-    if (to > from) {
-        k_source.fetch(from, keys, lds, wave, lane);
-        v_source.fetch(from, keys, lds + T::kBytes, wave, lane);
+    if (to > begin) {
+        k_source.fetch(begin, keys, lds, wave, lane);
+        v_source.fetch(begin, keys, lds + T::kBytes, wave, lane);
     }
     const int least = ahead + tile * kRows / group; // what the workgroup's first row sees
 #pragma unroll 1
-    for (int key = from, turn = 0; key < to; key += kKeys, turn ^= 1) {
+    for (int key = begin, turn = 0; key < to; key += kKeys, turn ^= 1) {
         arrived();
         __syncthreads(); // this tile has arrived, the other one is free
         if (key + kKeys < to) {
@@ -287,14 +287,22 @@ template <int D> __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void at
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int j = 0; j < 16; ++j) top = fmaxf(top, s[b][j]);
-        if (__any(top > m + a.slack)) {
+        if (__any(top - m > a.slack)) { // also from -inf; a sum could round a difference of large scores away
             const float next = fmaxf(m, fmaxf(top, __shfl_xor(top, 32))), keep = next == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - next) * scale);
             m = next;
             l *= keep;
 #pragma unroll
             for (int i = 0; i < kBlocks; ++i) o[i] *= keep;
         }
-        const float base = (m == -INFINITY ? 0.0f : m * scale) - kRaise;
+        const float from = m == -INFINITY ? 0.0f : m;
+        float base = from * scale - kRaise;
+        if (__any(fabsf(base) > 0x1p18f)) { // the rounding of the product would take weights past the end of binary16
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s[b][j] -= from;
+            base = -kRaise;
+        }
         half8_t p[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i)

@@ -280,6 +280,13 @@ def test_prompt_pieces(B, D):
     prompt_case(B, [70, 200, 3, 1], [64, 3, 0, 0], 6, 2, D)
 
 
+@pytest.mark.parametrize("S", [63, 64, 65, 130])
+def test_prompt_many_sequences(B, S):
+    # every sequence and tile is some workgroup's, whatever order they go in
+    n = [(i * 37) % 290 if i % 5 else 0 for i in range(S)]
+    prompt_case(B, n, [x + i % 3 for i, x in enumerate(n)], 4, 2, 64, seed=S)
+
+
 def test_prompt_long(B):
     prompt_case(B, [2500], [2500], 2, 1, 128)
     prompt_case(B, [1100, 900], [5000, 901], 5, 1, 64)
@@ -309,6 +316,19 @@ def test_weights_far_below_the_greatest(B):
         want = 8191 * low / (1 + 8191 * low)
         # half a step of binary16 in the result, and the same in the weights down to 2^-21
         assert (out.double() - want).abs().max().item() <= want * 2 * U.HALF_EPS16 + U.SUBNORMAL16, low
+
+
+@pytest.mark.parametrize("size", [8.0, 300.0, 20000.0])
+def test_large_scores(B, size):
+    # scores up to 10^10: their own binary32 rounding decides which key wins, but the weights stay weights
+    q, k, v = normal(1, 70, 2, 128) * size, normal(2, 300, 2, 128) * size, normal(3, 300, 2, 128)
+    prompt_case(B, [70], [300], 2, 2, 128, tensors=(q, k, v))
+    q, k = q.clamp(-60000, 60000), k.clamp(-60000, 60000)
+    k[1::2] = k[0::2]                                           # pairs of equal keys: the weights of a pair are equal whatever they are
+    v[1::2] = -v[0::2]
+    out = B.ap_attention_prompt(q[:2], k, v, U.starts([2]).cuda(), U.starts([299]).cuda())
+    assert out[1].abs().max().item() <= 2.0 and torch.isfinite(out).all()
+    cached_case(B, [300], [4], 2, 2, 128, 32, scale=size * size / 11)
 
 
 def test_prompt_scales(B):
