@@ -367,11 +367,18 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 6
     }
 }
 
-// Joins the ranges of a row that sees more than one: D / 4 lanes take every kParts-th range, and a quarter or an eighth of the workgroup does the rest
+// Joins the ranges of a row that sees more than one: D / 4 lanes take every kParts-th range with a running maximum, and one in kParts of the workgroup the rest.
+// The sums are asked for before it is known how many ranges the row has; what is beyond them is dropped.
 template <int D> __global__ __launch_bounds__(kThreads) void attention_join_kernel(const CachedArgs a)
 {
     constexpr int kLanes = D / 4, kParts = kThreads / kLanes;
     const int token = blockIdx.x / a.heads, lane = threadIdx.x % kLanes, part = threadIdx.x / kLanes;
+    const int64_t row = blockIdx.x, rows = (int64_t)a.tokens * a.heads;
+    const float scale = fabsf(a.scale) * kLog2e;
+    const auto stat_of = [&](int i) { return a.stat[(i < a.splits ? i : 0) * rows + row]; };
+    const auto part_of = [&](int i) { return *reinterpret_cast<const float4_t *>(a.part + ((i < a.splits ? i : 0) * rows + row) * D + lane * 4); };
+    float2 st = stat_of(part);
+    float4_t y = part_of(part);
     const int s = sequence_of(a.q_starts, token, a.tokens, a.sequences);
     if (s < 0) return;
     int64_t begin, end;
@@ -379,31 +386,38 @@ template <int D> __global__ __launch_bounds__(kThreads) void attention_join_kern
     const int sees = length_of(a, s) - (int)(end - 1 - token);
     if (sees <= a.chunk) return;
     const int ranges = (sees + a.chunk - 1) / a.chunk;
-    const int64_t row = blockIdx.x, rows = (int64_t)a.tokens * a.heads;
-    const float scale = fabsf(a.scale) * kLog2e;
-    float top = -INFINITY;
-    for (int i = threadIdx.x & 63; i < ranges; i += 64) top = fmaxf(top, a.stat[i * rows + row].x);
-    for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
-    float total = 0;
+    float top = -INFINITY, total = 0;
     float4_t x = {0, 0, 0, 0};
-#pragma unroll 2
+    // a range without a finite maximum has no key that the row sees, or only NaN: its sums are 0 or NaN and go in as they are
+    const auto keep_of = [&](float from, float to) { return from == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((from - to) * scale); };
     for (int i = part; i < ranges; i += kParts) {
-        const float2 st = a.stat[i * rows + row];
-        const float keep = st.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((st.x - top) * scale);
-        total += keep * st.y;
-        x += keep * *reinterpret_cast<const float4_t *>(a.part + (i * rows + row) * D + lane * 4);
+        const float2 next_st = stat_of(i + kParts);
+        const float4_t next_y = part_of(i + kParts);
+        const float next = fmaxf(top, st.x), old = keep_of(top, next), keep = keep_of(st.x, next);
+        total = total * old + st.y * keep;
+        x = x * old + y * keep;
+        top = next;
+        st = next_st;
+        y = next_y;
     }
     __shared__ float4_t sums[kParts][kLanes];
-    __shared__ float totals[kParts];
+    __shared__ float2 stats[kParts];
     sums[part][lane] = x;
-    if (lane == 0) totals[part] = total;
+    if (lane == 0) stats[part] = make_float2(top, total);
     __syncthreads();
     if (part > 0) return;
-    for (int i = 1; i < kParts; ++i) x += sums[i][lane], total += totals[i];
-    half4_t y;
+    for (int i = 0; i < kParts; ++i) top = fmaxf(top, stats[i].x);
+    x = float4_t{0, 0, 0, 0};
+    total = 0;
+    for (int i = 0; i < kParts; ++i) {
+        const float keep = keep_of(stats[i].x, top);
+        x += keep * sums[i][lane];
+        total += keep * stats[i].y;
+    }
+    half4_t out;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) y[k] = (_Float16)(total == 0.0f ? 0.0f : x[k] / total);
-    *reinterpret_cast<half4_t *>(a.out + row * D + lane * 4) = y;
+    for (int k = 0; k < 4; ++k) out[k] = (_Float16)(total == 0.0f ? 0.0f : x[k] / total);
+    *reinterpret_cast<half4_t *>(a.out + row * D + lane * 4) = out;
 }
 
 struct Plan {
