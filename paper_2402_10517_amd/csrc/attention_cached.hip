@@ -433,9 +433,14 @@ Plan plan_of(const ap_cache &c, const ap_cached &a)
     p.rows = each * group <= 16 ? 1 : 2;
     const int64_t tile = 16 * p.rows;
     p.items = a.q_starts ? a.tokens * group / tile + a.sequences : (each * group + tile - 1) / tile * a.sequences;
-    // As many ranges as give the card four workgroups per CU, of 256 keys at least
+    // Ranges of keys.  Two workgroups per CU in all, of 256 keys at least; four where two would have more than 1024 keys each, as longer ranges leave the card waiting for
+    // the last.  One, and no second launch, where every CU has a workgroup of up to 2048 keys.  us at 1 / 2 / 4 / 8 / 16 / 32 / 64 ranges, heads of 128: 32 sequences of 2000 keys
+    // and 8 key heads 18.4 / 20.7 / 24.0, up to 4099 keys (ragged) - / 29.0 / 25.8 / 27.6, 4 of 3000 and 32 - / 16.9 / 15.6 / 17.6, 16 up to 8000 and 8 - / - / 28.2 / 24.1,
+    // 1 of 1000 and 32 10.1 / 9.9 / 8.6 / 8.4, 2 of 131072 and 8 at 32 62.7, at 64 57.9; heads of 64: 8 of 8000 and 4 at 8 12.9, at 16 12.6, at 32 14.6.
     const int64_t units = p.items * c.kv_heads, longest = a.max_length > 0 ? a.max_length : 1;
-    int64_t chunk = (longest * units + 1023) / 1024;
+    const int64_t keys = longest * units, two = (keys + 511) / 512, four = (keys + 1023) / 1024;
+    int64_t chunk = two <= 1024 ? two : four > 1024 ? four : 1024;
+    if (units >= 256 && longest <= 2048) chunk = longest;
     chunk = (chunk + kStep - 1) / kStep * kStep;
     p.chunk = (int)(chunk < 2 * kStep ? 2 * kStep : chunk > kMaxChunk ? kMaxChunk : chunk);
     p.splits = (int)((longest + p.chunk - 1) / p.chunk);
