@@ -1,16 +1,21 @@
 // Attention of new tokens over the 4-bit paged cache, on the matrix cores.
 //
-// A workgroup takes a tile of query rows (token, head of the group) of one sequence and key head and a range of its keys; a wave takes 32 keys at a time:
+// A workgroup takes a tile of query rows (token, head of the group) of one sequence and key head and a range of its keys; a wave takes 32 keys at a
+// time:
 //   S^T = C Q^T with C the key codes, v_mfma_f32_16x16x32_f16: codes 0..15 enter as binary16 64 + code (the nibble set into the mantissa of 64: a shift
 //         and one v_and_or for two), exact, and s = scale (step (S - 64 sum q) + low sum q) takes the offset back in binary32;
 //   O^T = V^T P^T, v_mfma_f32_16x16x32_bf16: codes enter as bfloat16 128 + code, the weights as p * step in two bfloat16 parts (high + rest:
 //         16 bits of mantissa, and the range of binary32 for any step); what is the same for all channels of a row, sum p low - 128 sum p step, is one number.
-// With keys as rows and queries as columns a lane holds scores of one query row throughout, the scores' registers are the weights' operand as
-// they stand (the order of the keys inside a product is free, and the cache's value layout follows it), and the statistics are one number per lane.
-// The running maximum moves only when a score exceeds it by 2^8: weights stay below 2^8 and the accumulators are seldom rescaled.
+// With keys as rows and queries as columns a lane holds scores of one query row throughout, the scores' registers are the weights' operand as they
+// stand (the order of the keys inside a product is free, and the cache's value layout follows it), and the statistics are one number per lane. The
+// running maximum moves only when a score exceeds it by 2^8: weights stay below 2^8 and the accumulators are seldom rescaled.
 //
-// Bound by HBM: a key of one head is D + 8 bytes, 4 (heads / kv_heads) D operations.  A wave has its next 32 keys' loads in flight while it works.
-#include "attention_rows.h"
+// A key of one head is D + 8 bytes and 4 (heads / kv_heads) D operations: HBM bounds the work, and a wave has its next 32 keys' loads in flight while
+// it works. Long sequences reach it: two of 131072 keys and 8 key heads of 128 take 51 us (285 MB, 5.6 TB/s; ap_probe_read reads as much in 44) and
+// the join 5. Short ones are bound by what happens once per workgroup (start, length, page and first key one after the other, the join of the waves,
+// the second launch: some 10 us in all), and by the vector instructions per 32 keys, about 240: 4-bit codes to operands 112, softmax and weights 100.
+// Codes staged through LDS two to four tiles ahead, or two sets of registers without moves, came out the same within 5 % on all of them.
+#include "decode_device.h"
 
 namespace apgemv {
 
@@ -49,8 +54,8 @@ __device__ __forceinline__ int length_of(const CachedArgs &a, int sequence)
     return length < 0 ? 0 : length > a.max_length ? a.max_length : length;
 }
 
-// The sequence and row tile of an item (64 lanes call together); false: there are fewer.  Where sequences have different numbers of tokens a lane looks at one
-// sequence, its length with it.
+// The sequence and row tile of an item (64 lanes call together); false: there are fewer.  Where sequences have different numbers of tokens a lane
+// looks at one sequence, its length with it.
 __device__ __forceinline__ bool find_item(const CachedArgs &a, int rows_per_tile, int item, Item *out)
 {
     const int lane = threadIdx.x & 63, group = a.heads / a.cache.kv_heads;
@@ -85,8 +90,8 @@ __device__ __forceinline__ bool find_item(const CachedArgs &a, int rows_per_tile
     return false;
 }
 
-// Codes and (low, step) pairs of 16 keys as a lane (c = lane % 16, g = lane / 16) needs them: key c's channels g * D/4 .., the values of keys 4 g .. 4 g + 3
-// in channels c * D/16 .., the pairs of those four keys
+// Codes and (low, step) pairs of 16 keys as a lane (c = lane % 16, g = lane / 16) needs them: key c's channels g * D/4 .., the values of keys 4 g ..
+// 4 g + 3 in channels c * D/16 .., the pairs of those four keys
 template <int D> struct Half {
     typedef uint32_t words_t __attribute__((ext_vector_type(D / 32)));
     words_t k, v;
@@ -98,7 +103,8 @@ struct Lane {
     uint32_t k, v, kp, vp;
 };
 
-// They are read once: past the caches' usual order.  section: where the (page, key head) starts; t: the first of the 16 keys in it.  Both starts are kept in scalar registers.
+// They are read once: past the caches' usual order.  section: where the (page, key head) starts; t: the first of the 16 keys in it.  Both starts are
+// kept in scalar registers.
 template <int D> __device__ __forceinline__ Half<D> load_half(const uint8_t *section, int log_page, int t, const Lane &at)
 {
     typedef typename Half<D>::words_t words_t;
@@ -120,8 +126,8 @@ __device__ __forceinline__ _Float16 step_of(uint32_t pair) { return __builtin_bi
 // A binary16 number times a binary32 one in one mixed-precision instruction
 __device__ __forceinline__ float times(_Float16 x, float y) { return __builtin_fmaf((float)x, y, 0.0f); }
 
-// A constant in a vector register: (w & it) | another constant is then one v_and_or_b32, which takes one scalar operand.  The instruction itself is the compiler's, who
-// knows how far it has to stay from the matrix instruction that reads its result.
+// A constant in a vector register: (w & it) | another constant is then one v_and_or_b32, which takes one scalar operand.  The instruction itself is
+// the compiler's, who knows how far it has to stay from the matrix instruction that reads its result.
 __device__ __forceinline__ uint32_t in_vector(uint32_t x)
 {
     asm("" : "+v"(x));
@@ -367,8 +373,8 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 6
     }
 }
 
-// Joins the ranges of a row that sees more than one: D / 4 lanes take every kParts-th range with a running maximum, and one in kParts of the workgroup the rest.
-// The sums are asked for before it is known how many ranges the row has; what is beyond them is dropped.
+// Joins the ranges of a row that sees more than one: D / 4 lanes take every kParts-th range with a running maximum, and one in kParts of the
+// workgroup the rest. The sums are asked for before it is known how many ranges the row has; what is beyond them is dropped.
 template <int D> __global__ __launch_bounds__(kThreads) void attention_join_kernel(const CachedArgs a)
 {
     constexpr int kLanes = D / 4, kParts = kThreads / kLanes;
@@ -433,10 +439,11 @@ Plan plan_of(const ap_cache &c, const ap_cached &a)
     p.rows = each * group <= 16 ? 1 : 2;
     const int64_t tile = 16 * p.rows;
     p.items = a.q_starts ? a.tokens * group / tile + a.sequences : (each * group + tile - 1) / tile * a.sequences;
-    // Ranges of keys.  Two workgroups per CU in all, of 256 keys at least; four where two would have more than 1024 keys each, as longer ranges leave the card waiting for
-    // the last.  One, and no second launch, where every CU has a workgroup of up to 2048 keys.  us at 1 / 2 / 4 / 8 / 16 / 32 / 64 ranges, heads of 128: 32 sequences of 2000 keys
-    // and 8 key heads 18.4 / 20.7 / 24.0, up to 4099 keys (ragged) - / 29.0 / 25.8 / 27.6, 4 of 3000 and 32 - / 16.9 / 15.6 / 17.6, 16 up to 8000 and 8 - / - / 28.2 / 24.1,
-    // 1 of 1000 and 32 10.1 / 9.9 / 8.6 / 8.4, 2 of 131072 and 8 at 32 62.7, at 64 57.9; heads of 64: 8 of 8000 and 4 at 8 12.9, at 16 12.6, at 32 14.6.
+    // Ranges of keys.  Two workgroups per CU in all, of 256 keys at least; four where two would have more than 1024 keys each, as longer ranges leave
+    // the card waiting for the last.  One, and no second launch, where every CU has a workgroup of up to 2048 keys.  us at 1 / 2 / 4 / 8 / 16 / 32 /
+    // 64 ranges, heads of 128: 32 sequences of 2000 keys and 8 key heads 18.4 / 20.7 / 24.0, up to 4099 keys (ragged) - / 29.0 / 25.8 / 27.6, 4 of
+    // 3000 and 32 - / 16.9 / 15.6 / 17.6, 16 up to 8000 and 8 - / - / 28.2 / 24.1, 1 of 1000 and 32 10.1 / 9.9 / 8.6 / 8.4, 2 of 131072 and 8 at 32
+    // 62.7, at 64 57.9; heads of 64: 8 of 8000 and 4 at 8 12.9, at 16 12.6, at 32 14.6.
     const int64_t units = p.items * c.kv_heads, longest = a.max_length > 0 ? a.max_length : 1;
     const int64_t keys = longest * units, two = (keys + 511) / 512, four = (keys + 1023) / 1024;
     int64_t chunk = two <= 1024 ? two : four > 1024 ? four : 1024;

@@ -1,16 +1,19 @@
 // Causal attention over packed sequences of binary16 keys and values, on the matrix cores.
 //
 // A workgroup takes 128 query rows (token, head of the group) of one sequence and key head and walks the keys they see, 64 at a time; a wave has 32
-// of the rows.  v_mfma_f32_32x32x16_f16 twice, both transposed:  S^T = K Q^T,  O^T = V^T P^T,  P = e^(scale s - m).
-// With keys as rows and queries as columns a lane holds scores of one query row throughout, and the scores' registers, rounded to binary16, are the
-// weights' operand as they stand: the order of the keys inside a product is free, and the values are read in the same order from LDS, transposed by
-// ds_read_b64_tr_b16.  Row statistics are one number per lane; the running maximum moves only when a score exceeds it by 2^8, so weights
-// stay below 2^8 and the accumulators are seldom rescaled.
-// Keys and values go from memory into LDS without registers, 16 bytes a lane, one tile ahead.  Rows of LDS have their 16-byte chunks exchanged (the
-// lanes ask memory for the chunk that belongs at their place) so that the reads of both operands meet every bank once.
+// of the rows.  v_mfma_f32_32x32x16_f16 twice, both transposed:  S^T = K Q^T,  O^T = V^T P^T,  P = e^(scale s - m). With keys as rows and queries as
+// columns a lane holds scores of one query row throughout, and the scores' registers, rounded to binary16, are the weights' operand as they stand:
+// the order of the keys inside a product is free, and the values are read in the same order from LDS, transposed by ds_read_b64_tr_b16.  Row
+// statistics are one number per lane; the running maximum moves only when a score exceeds it by 2^8, so weights stay below 2^8 and the accumulators
+// are seldom rescaled. Keys and values go from memory into LDS without registers, 16 bytes a lane, one tile ahead.  Rows of LDS have their 16-byte
+// chunks exchanged (the lanes ask memory for the chunk that belongs at their place) so that the reads of both operands meet every bank once.
 //
-// Bound by the matrix cores and the exponentials beside them: 4 D operations and one exponential per pair of query and key.
-#include "attention_rows.h"
+// 4 D operations and one exponential per pair of query and key: bound by the matrix cores and the vector instructions beside them. 8192 tokens of 64
+// heads and 8 key heads of 128 take 1.08 to 1.13 ms, 970 to 1016 TFLOP/s, where a library product of 8192^3 reaches 1177: the matrix cores are busy
+// for 55 % of the time and the vector units for 38 %, and the two waves of a SIMD overlap them but little. Two workgroups per CU (212 registers, 64
+// KB of LDS); no bank conflicts. Shorter prompts lose to the tiles on the diagonal and to the start of a workgroup: six of up to 2047 tokens and 40
+// heads run at 690.
+#include "decode_device.h"
 
 namespace apgemv {
 
@@ -78,8 +81,8 @@ template <int D, bool VALUES> struct Source {
         if (key + kKeys > keys) place(keys - key, wave, lane);
         const uint8_t *from = rows + (int64_t)key * stride;
         const uint32_t to = (uint32_t)(uintptr_t)tile + wave * T::kLoads * 1024;
-        // In assembly, as the compiler would have every later read of LDS wait for these loads; the loop waits for them before its barrier.  The s_nop's are the
-        // distances from a vector instruction that may have written the scalar operands, and from m0 to its use.
+        // In assembly, as the compiler would have every later read of LDS wait for these loads; the loop waits for them before its barrier.  The
+        // s_nop's are the distances from a vector instruction that may have written the scalar operands, and from m0 to its use.
         if constexpr (T::kLoads == 4)
             asm volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\ts_add_i32 m0, %0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %5\n\t"
                          "s_add_i32 m0, %0, 0x800\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %5\n\ts_add_i32 m0, %0, 0xc00\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, %5"
@@ -413,10 +416,11 @@ struct PromptPlan {
     int splits;
 };
 
-// Row tiles (at most), and the ranges of keys that they are divided into: as many as fill the places that the card has for workgroups (two per CU at head_dim
-// 128, four at 64), of four tiles at least, where that saves more than it costs: a workgroup takes about 0.9 us for a tile of 64 keys (0.6 at head_dim 64), the
-// second launch 5 us, and the sums go through memory, written and read, at 4 TB/s.  us without / with ranges: 1 query of 8 heads over 4000 keys 72 / 16,
-// 200 of 32 over 8000 141 / 48, 3 x 500 of 16 x 64 over 7500 109 / 74; where the rule keeps to one: 512 of 32 over 512 16 / 21, 2000 of 16 x 64 over 2000 32 / 34.
+// Row tiles (at most), and the ranges of keys that they are divided into: as many as fill the places that the card has for workgroups (two per CU at
+// head_dim 128, four at 64), of four tiles at least, where that saves more than it costs: a workgroup takes about 0.9 us for a tile of 64 keys (0.6
+// at head_dim 64), the second launch 5 us, and the sums go through memory, written and read, at 4 TB/s.  us without / with ranges: 1 query of 8 heads
+// over 4000 keys 72 / 16, 200 of 32 over 8000 141 / 48, 3 x 500 of 16 x 64 over 7500 109 / 74; where the rule keeps to one: 512 of 32 over 512 16 /
+// 21, 2000 of 16 x 64 over 2000 32 / 34.
 PromptPlan plan_of(const ap_prompt &a)
 {
     PromptPlan p;

@@ -48,5 +48,23 @@ __device__ __forceinline__ void token_range(const int32_t *starts, int s, int64_
     *end = ok ? b : 0;
 }
 
+// The sequence of token i (all 64 lanes call together); -1 for a token of none
+__device__ __forceinline__ int sequence_of(const int32_t *starts, int64_t i, int64_t tokens, int sequences)
+{
+    if (!starts) return (int)(i / (tokens / sequences));
+    const int lane = threadIdx.x & 63;
+    for (int first = 0; first < sequences; first += 64) {
+        bool mine = false;
+        if (first + lane < sequences) {
+            int64_t a, b;
+            token_range(starts, first + lane, tokens, sequences, &a, &b);
+            mine = i >= a && i < b;
+        }
+        const uint64_t found = __ballot(mine);
+        if (found) return first + __builtin_ctzll(found);
+    }
+    return -1;
+}
+
 } // namespace apgemv
 #endif
