@@ -196,7 +196,7 @@ PyObject *cache_append(PyObject *, PyObject *const *args, Py_ssize_t n)
             a.rotary = static_cast<const float *>(c.array(args[7], "rotary", at::kFloat, r.numel()));
             a.rotary_rows = r.size(0);
             a.rot_dim = (int)std::min<int64_t>(r.size(1), INT_MAX);
-            if (a.rotary_rows > 0 && !a.rotary) refuse("rotary", "has no memory");
+            if (!a.rotary) refuse("rotary", "must have rows and columns");
             if (args[6] == Py_None) refuse("positions", "are needed with rotary");
             a.positions = static_cast<const int64_t *>(c.array(args[6], "positions", at::kLong, a.tokens));
             a.interleaved = PyObject_IsTrue(args[8]) == 1;

@@ -75,6 +75,21 @@ def test_library_exports_every_declared_decoder_symbol():
         assert hasattr(ctypes.CDLL(B.LIB_PATH), name), name
 
 
+def test_attention_kernels_keep_their_registers():
+    # waves per SIMD that the division of the work counts on, and nothing spilled
+    from test_kernel_resources import _kernels
+    waves = {r"attention_cached_kernelILi64ELi1E": 4, r"attention_cached_kernelILi128ELi1E": 3, r"attention_cached_kernelILi(64|128)ELi2E": 2,
+             r"attention_prompt_kernelILi64E": 4, r"attention_prompt_kernelILi128E": 2}
+    seen = set()
+    for name, k in _kernels().items():
+        for pattern, least in waves.items():
+            if re.search(pattern, name):
+                seen.add(pattern)
+                assert k[".vgpr_spill_count"] == 0 and k[".private_segment_fixed_size"] == 0, name
+                assert 512 // ((k[".vgpr_count"] + 7) // 8 * 8) >= least, "%s: %d registers" % (name, k[".vgpr_count"])
+    assert seen == set(waves)
+
+
 def test_cache_size():
     assert B.ap_cache_size(10, 2, 128, 64) == 10 * 64 * 2 * 136            # 4 bits a value and 4 bytes a row, keys and values
     assert B.ap_cache_size(1, 1, 64, 16) == 16 * 72

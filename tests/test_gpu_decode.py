@@ -113,6 +113,47 @@ def test_append_values_out_of_range(B):
     assert B.ap_cache_append(cache, empty, empty, slots[:0])[1].shape == (0, G, D) and B.ap_cache_read(cache, slots[:0])[0].shape == (0, G, D)
 
 
+def test_tensors_that_do_not_fit_are_refused(B):
+    G, D, page, T = 2, 64, 16, 4
+    cache = full_cache(B, 3, G, D, page)
+    k, v, q, slots = normal(1, T, G, D), normal(2, T, G, D), normal(3, T, 4, D), torch.arange(T).cuda()
+    rotary, positions = B.rotary_table(8, 32), torch.arange(T).cuda()
+    table, lens, starts = torch.zeros((T, 3), dtype=torch.int32).cuda(), torch.ones(T, dtype=torch.int32).cuda(), torch.arange(T + 1, dtype=torch.int32).cuda()
+    append = lambda **kw: B.ap_cache_append(cache, **dict(dict(k=k, v=v, slots=slots, q=q, positions=positions, rotary=rotary), **kw))
+    for bad in (dict(k=k[:3]), dict(v=v.float()), dict(k=k.cpu()), dict(v=normal(1, T, G + 1, D)), dict(k=normal(1, T, G, 2 * D)[..., ::2]), dict(slots=slots.int()),
+                dict(slots=slots[:2]), dict(positions=None), dict(positions=positions.cpu()), dict(rotary=rotary.half()), dict(rotary=rotary[:0]), dict(q=q[0]),
+                dict(q_out=torch.empty_like(k)), dict(k_out=k.float())):
+        with pytest.raises(AssertionError):
+            append(**bad)
+    for bad in (dict(rotary=B.rotary_table(8, 8)), dict(k=normal(1, T * G * D + 4)[4:].as_strided((T, G, D), (G * D, D, 1), 4))):
+        with pytest.raises(B.ApError):
+            append(**bad)
+    attend = lambda **kw: B.ap_attention_cached(cache, **dict(dict(q=q, tables=table, lengths=lens), **kw))
+    for bad in (dict(q=q.float()), dict(tables=table.long()), dict(tables=table[:, :2]), dict(lengths=lens[:2]), dict(q_starts=starts[:-1]), dict(out=q[:2]),
+                dict(out=q.float()), dict(work=torch.zeros(8)), dict(tables=table[0])):
+        with pytest.raises(AssertionError):
+            attend(**bad)
+    for bad in (dict(max_length=49), dict(max_length=-1), dict(scale=float("nan")), dict(q=normal(3, T, 3, D)), dict(q=normal(3, T + 1, 4, D))):
+        with pytest.raises(B.ApError):
+            attend(**bad)
+    prompt = lambda **kw: B.ap_attention_prompt(**dict(dict(q=q, k=k, v=v, q_starts=starts), **kw))
+    for bad in (dict(k=k.float()), dict(v=v[:2]), dict(q_starts=starts.long()), dict(k_starts=starts[:3]), dict(q=q[:, 0])):
+        with pytest.raises(AssertionError):
+            prompt(**bad)
+    for bad in (dict(q=normal(3, T, 3, D)), dict(scale=float("inf"))):
+        with pytest.raises(B.ApError):
+            prompt(**bad)
+    with pytest.raises(B.ApError):                              # a workspace that is too small
+        B.ap_attention_prompt(normal(1, 1, 4, D), normal(2, 5000, 4, D), normal(3, 5000, 4, D), U.starts([1]).cuda(), U.starts([5000]).cuda(),
+                              work=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    p = [torch.from_numpy(x).cuda() for x in verify_inputs(2, 3, 50, False, 1)]
+    for i, bad in ((0, p[0].double()), (0, p[0][:, :3].contiguous()), (1, p[1].half()), (2, p[2].int()), (3, p[3][:1]), (4, p[4].cpu())):
+        with pytest.raises(AssertionError):
+            B.ap_verify(*[bad if j == i else x for j, x in enumerate(p)])
+    with pytest.raises(AssertionError):
+        B.ap_verify(*p, counts=torch.zeros(3, dtype=torch.int32).cuda())
+
+
 # ------------------------------------------------------------------------------------------------ attention over the cache
 
 
