@@ -374,16 +374,6 @@ class KVCache:
         self.buf = torch.empty(size, dtype=torch.uint8, device=device)
 
 
-def _named(stream):
-    return None if stream is None else stream.cuda_stream
-
-
-def _result(r, where):
-    if type(r) is int:
-        raise ApError(abs(r), where if r > 0 else where + "_size")
-    return r
-
-
 def rotary_table(rows, rot_dim, base=10000.0, device="cuda:0"):
     """(rows, rot_dim) float32: the cosines, then the sines of position / base^(2 i / rot_dim), as ap_cache_append takes them."""
     angle = torch.arange(rows, dtype=torch.float64)[:, None] * base ** (-torch.arange(0, rot_dim, 2, dtype=torch.float64) / rot_dim)
@@ -395,13 +385,19 @@ def ap_cache_append(cache, k, v, slots, q=None, positions=None, rotary=None, int
 
     slots, positions: int64 (tokens,); rotary: a table like rotary_table's, None = no rotation.  A slot outside the cache (-1) keeps its
     token out of it.  q_out and k_out may be q and k themselves.  `stream` as in ap_gemv."""
-    return _result(_torch_call.cache_append(cache.buf, cache.shape, k, v, slots, q, positions, rotary, interleaved, q_out, k_out,
-                                            _named(stream)), "ap_cache_append")
+    r = _torch_call.cache_append(cache.buf, cache.shape, k, v, slots, q, positions, rotary, interleaved, q_out, k_out,
+                                 None if stream is None else stream.cuda_stream)
+    if type(r) is int:
+        raise ApError(r, "ap_cache_append")
+    return r
 
 
 def ap_cache_read(cache, slots, stream=None):
     """The values that slots stand for: (k, v), float16 (slots, kv_heads, head_dim) each; zeros for a slot outside the cache."""
-    return _result(_torch_call.cache_read(cache.buf, cache.shape, slots, _named(stream)), "ap_cache_read")
+    r = _torch_call.cache_read(cache.buf, cache.shape, slots, None if stream is None else stream.cuda_stream)
+    if type(r) is int:
+        raise ApError(r, "ap_cache_read")
+    return r
 
 
 def ap_attention_cached(cache, q, tables, lengths, q_starts=None, scale=None, max_length=None, out=None, work=None, stream=None):
@@ -410,17 +406,22 @@ def ap_attention_cached(cache, q, tables, lengths, q_starts=None, scale=None, ma
     tables: int32 (sequences, pages), lengths: int32 (sequences,), q_starts: int32 (sequences + 1,), None = tokens / sequences each;
     max_length: a bound of lengths, None = what the tables hold; scale: head_dim ** -0.5 if None.  `stream` as in ap_gemv; a given work (uint8)
     is in use until that stream is done with the call."""
-    return _result(_torch_call.attention_cached(cache.buf, cache.shape, q, tables, lengths, q_starts,
-                                                scale, max_length, out, work, _named(stream)),
-                   "ap_attention_cached")
+    r = _torch_call.attention_cached(cache.buf, cache.shape, q, tables, lengths, q_starts, scale, max_length, out, work,
+                                     None if stream is None else stream.cuda_stream)
+    if type(r) is int:
+        raise ApError(abs(r), "ap_attention_cached" if r > 0 else "ap_attention_cached_size")
+    return r
 
 
 def ap_attention_prompt(q, k, v, q_starts, k_starts=None, scale=None, out=None, work=None, stream=None):
     """Causal attention over packed sequences: q (tokens, heads, head_dim), k and v (keys, kv_heads, head_dim); q_starts, k_starts: int32
     (sequences + 1,), k_starts = q_starts if None.  The last query of a sequence sees its last key.  `stream` and work as in
     ap_attention_cached."""
-    return _result(_torch_call.attention_prompt(q, k, v, q_starts, q_starts if k_starts is None else k_starts, scale, out,
-                                                work, _named(stream)), "ap_attention_prompt")
+    r = _torch_call.attention_prompt(q, k, v, q_starts, q_starts if k_starts is None else k_starts, scale, out, work,
+                                     None if stream is None else stream.cuda_stream)
+    if type(r) is int:
+        raise ApError(abs(r), "ap_attention_prompt" if r > 0 else "ap_attention_prompt_size")
+    return r
 
 
 def ap_verify(target, draft, drafted, uniform, noise, counts=None, work=None, stream=None):
@@ -428,4 +429,7 @@ def ap_verify(target, draft, drafted, uniform, noise, counts=None, work=None, st
     vocabulary) probabilities, float32 or float16, with uniform (sequences, drafts) and exponential noise (sequences, vocabulary) float32.
 
     Returns (tokens (sequences, drafts + 1) int64: the accepted drafts, the token after them, -1s; accepted (sequences,) int32)."""
-    return _result(_torch_call.verify(target, draft, drafted, uniform, noise, counts, work, _named(stream)), "ap_verify")
+    r = _torch_call.verify(target, draft, drafted, uniform, noise, counts, work, None if stream is None else stream.cuda_stream)
+    if type(r) is int:
+        raise ApError(abs(r), "ap_verify" if r > 0 else "ap_verify_size")
+    return r

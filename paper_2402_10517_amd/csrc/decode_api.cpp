@@ -131,7 +131,7 @@ static ap_status check_prompt(const ap_prompt *a)
         (a->tokens > 0 && a->sequences < 1) || a->tokens * a->heads > kMaxTokens)
         return AP_ERR_SHAPE;
     // a tile of 64 rows of k or v is addressed by 32 bits from its first
-    if (a->k.token_stride < 0 || a->k.token_stride > 1 << 25 || a->v.token_stride < 0 || a->v.token_stride > 1 << 25) return AP_ERR_SHAPE;
+    if (a->k.token_stride < 0 || a->k.token_stride > 1 << 24 || a->v.token_stride < 0 || a->v.token_stride > 1 << 24) return AP_ERR_SHAPE;
     return AP_OK;
 }
 

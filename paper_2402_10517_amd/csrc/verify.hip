@@ -2,7 +2,7 @@
 //
 // The token is the argmax of w / noise with lowest index first: no sum is taken, so any division of the vocabulary gives the same token, bit for bit.
 // Bound by HBM: one row of target and draft probabilities and the noise per sequence.  Few sequences leave most of the card idle, so a vocabulary is
-// divided among workgroups (2048 tokens at least each) and joined by a second launch. 64 sequences over 131071 binary16 probabilities take 16 us (67
+// divided among workgroups (2048 tokens at least each) and joined by a second launch, small ones aside. 64 sequences over 131071 binary16 probabilities take 16 us (67
 // MB, 4.1 TB/s), 4 drafts over 32000 tokens 8.5, two launches.
 #include "decode_device.h"
 
@@ -10,8 +10,9 @@ namespace apgemv {
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kEach = 8; // consecutive tokens of a thread
+constexpr int kThreads = 256; // of a workgroup that shares a vocabulary, or has one among many
+constexpr int kWide = 1024;   // of one that has a small vocabulary for itself
+constexpr int kEach = 8;      // consecutive tokens of a thread
 constexpr int kStep = kThreads * kEach;
 
 struct VerifyArgs {
@@ -32,9 +33,9 @@ __device__ __forceinline__ uint64_t candidate(float ratio, int64_t v)
     return ratio >= 0.0f ? (uint64_t)__float_as_uint(ratio) << 32 | (uint32_t)~(uint32_t)v : 0;
 }
 
-__device__ __forceinline__ uint64_t block_max(uint64_t x)
+template <int THREADS> __device__ __forceinline__ uint64_t block_max(uint64_t x)
 {
-    __shared__ uint64_t best[kThreads / 64];
+    __shared__ uint64_t best[THREADS / 64];
     for (int m = 1; m < 64; m <<= 1) {
         const uint64_t y = __shfl_xor((unsigned long long)x, m);
         x = y > x ? y : x;
@@ -42,7 +43,7 @@ __device__ __forceinline__ uint64_t block_max(uint64_t x)
     __syncthreads();
     if ((threadIdx.x & 63) == 0) best[threadIdx.x >> 6] = x;
     __syncthreads();
-    for (int w = 0; w < kThreads / 64; ++w) x = best[w] > x ? best[w] : x;
+    for (int w = 0; w < THREADS / 64; ++w) x = best[w] > x ? best[w] : x;
     return x;
 }
 
@@ -52,7 +53,7 @@ template <class T> struct __attribute__((packed, aligned(sizeof(T)))) Eight {
 };
 
 // The best of tokens [from, to): w = p - q, or p where there is no q
-template <class T> __device__ __forceinline__ uint64_t race(const T *p, const T *q, const float *noise, int64_t from, int64_t to)
+template <class T, int THREADS> __device__ __forceinline__ uint64_t race(const T *p, const T *q, const float *noise, int64_t from, int64_t to)
 {
     float best = -1.0f;
     int64_t at = 0;
@@ -64,7 +65,7 @@ template <class T> __device__ __forceinline__ uint64_t race(const T *p, const T 
         }
     };
     int64_t v = from + (int64_t)threadIdx.x * kEach;
-    for (; v + kEach <= to; v += kStep) {
+    for (; v + kEach <= to; v += THREADS * kEach) {
         const Eight<T> a = *reinterpret_cast<const Eight<T> *>(p + v);
         const Eight<float> e = *reinterpret_cast<const Eight<float> *>(noise + v);
         Eight<T> b;
@@ -73,7 +74,7 @@ template <class T> __device__ __forceinline__ uint64_t race(const T *p, const T 
         for (int i = 0; i < kEach; ++i) consider((float)a.x[i], q ? (float)b.x[i] : 0.0f, e.x[i], v + i);
     }
     for (int i = 0; i < kEach && v + i < to; ++i) consider((float)p[v + i], q ? (float)q[v + i] : 0.0f, noise[v + i], v + i);
-    return block_max(candidate(best, at));
+    return block_max<THREADS>(candidate(best, at));
 }
 
 struct Sequence {
@@ -110,16 +111,16 @@ template <class T> __device__ __forceinline__ Sequence accept(const VerifyArgs &
 }
 
 // The end of a sequence, once the best of the whole vocabulary is known (0: none with more than its draft, or none at all)
-template <class T> __device__ __forceinline__ void finish(const VerifyArgs &a, int64_t s, int accepted, bool refused, uint64_t won)
+template <class T, int THREADS> __device__ __forceinline__ void finish(const VerifyArgs &a, int64_t s, int accepted, bool refused, uint64_t won)
 {
     if (!won && refused)
-        won = race<T>(static_cast<const T *>(a.target) + (s * (a.drafts + 1) + accepted) * a.vocabulary, nullptr, a.noise + s * a.vocabulary, 0, a.vocabulary);
+        won = race<T, THREADS>(static_cast<const T *>(a.target) + (s * (a.drafts + 1) + accepted) * a.vocabulary, nullptr, a.noise + s * a.vocabulary, 0, a.vocabulary);
     const int64_t token = won ? (int64_t)(uint32_t)~(uint32_t)won : -1;
-    for (int i = threadIdx.x; i <= a.drafts; i += kThreads)
+    for (int i = threadIdx.x; i <= a.drafts; i += THREADS)
         a.tokens[s * (a.drafts + 1) + i] = i < accepted ? a.drafted[s * a.drafts + i] : i == accepted ? token : -1;
 }
 
-template <class T> __global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyArgs a)
+template <class T, int THREADS> __global__ __launch_bounds__(THREADS) void verify_kernel(const VerifyArgs a)
 {
     const int64_t s = blockIdx.x / a.parts, V = a.vocabulary;
     const int part = blockIdx.x - (int)s * a.parts;
@@ -128,8 +129,8 @@ template <class T> __global__ __launch_bounds__(kThreads) void verify_kernel(con
     const T *p = static_cast<const T *>(a.target) + (s * (a.drafts + 1) + r.accepted) * V;
     const T *q = refused ? static_cast<const T *>(a.draft) + (s * a.drafts + r.accepted) * V : nullptr;
     const int64_t from = part * a.slice, to = from + a.slice < V ? from + a.slice : V;
-    const uint64_t won = race<T>(p, q, a.noise + s * V, from, to);
-    if (a.parts == 1) finish<T>(a, s, r.accepted, refused, won);
+    const uint64_t won = race<T, THREADS>(p, q, a.noise + s * V, from, to);
+    if (a.parts == 1) finish<T, THREADS>(a, s, r.accepted, refused, won);
     else if (threadIdx.x == 0) a.best[blockIdx.x] = won;
     if (part == 0 && threadIdx.x == 0) a.accepted[s] = r.accepted;
 }
@@ -142,41 +143,52 @@ template <class T> __global__ __launch_bounds__(kThreads) void verify_join_kerne
         const uint64_t x = a.best[s * a.parts + i];
         won = x > won ? x : won;
     }
-    won = block_max(won);
+    won = block_max<kThreads>(won);
     int count = a.counts ? a.counts[s] : a.drafts;
     count = count > a.drafts ? a.drafts : count;
     const int accepted = a.accepted[s];
-    finish<T>(a, s, accepted, accepted < count, won);
+    finish<T, kThreads>(a, s, accepted, accepted < count, won);
 }
 
-// Parts of a vocabulary: as many as give the card four workgroups per CU, of one step at least
-int parts_of(const ap_verification &a)
+struct Plan {
+    int parts, threads;
+};
+
+// Parts of a vocabulary: as many as give the card four workgroups per CU, of one step at least.  A vocabulary of up to two steps of a wide workgroup is
+// not divided, which saves the second launch.  us divided / not, 4 drafts: 1 sequence of 8000 tokens 8.7 / 5.4, 16000 9.2 / 6.7, 32000 8.8 / 8.6; 64
+// sequences of 32000 8.4 / 9.7, 300 of 20000 in binary16 14.0 / 16.2.
+Plan plan_of(const ap_verification &a)
 {
     const int64_t steps = (a.vocabulary + kStep - 1) / kStep, wanted = (1024 + a.sequences - 1) / a.sequences;
-    return (int)(wanted < steps ? wanted : steps);
+    const int parts = (int)(wanted < steps ? wanted : steps);
+    if (parts > 1 && a.vocabulary <= 2 * kWide * kEach) return Plan{1, kWide};
+    return Plan{parts, kThreads};
+}
+
+template <class T> void launch(const VerifyArgs &k, const Plan &p, hipStream_t stream)
+{
+    const dim3 grid((unsigned)k.sequences * (unsigned)p.parts);
+    if (p.threads == kWide) verify_kernel<T, kWide><<<grid, kWide, 0, stream>>>(k);
+    else verify_kernel<T, kThreads><<<grid, kThreads, 0, stream>>>(k);
+    if (p.parts > 1) verify_join_kernel<T><<<k.sequences, kThreads, 0, stream>>>(k);
 }
 
 } // namespace
 
 size_t verify_work(const ap_verification &a)
 {
-    const int parts = parts_of(a);
+    const int parts = plan_of(a).parts;
     return parts == 1 ? 0 : (size_t)parts * a.sequences * sizeof(uint64_t);
 }
 
 hipError_t launch_verify(const ap_verification &a, hipStream_t stream)
 {
-    const int parts = parts_of(a);
-    const int64_t steps = (a.vocabulary + kStep - 1) / kStep, slice = (steps + parts - 1) / parts * kStep;
-    const VerifyArgs k{a.target, a.draft,    a.drafted,                      a.uniform,    a.noise, a.counts,    a.tokens,
-                       a.accepted, static_cast<uint64_t *>(a.work), a.vocabulary, slice,   a.sequences, a.drafts, parts};
-    const dim3 grid((unsigned)a.sequences * (unsigned)parts);
-    if (a.half) verify_kernel<_Float16><<<grid, kThreads, 0, stream>>>(k);
-    else verify_kernel<float><<<grid, kThreads, 0, stream>>>(k);
-    if (parts > 1) {
-        if (a.half) verify_join_kernel<_Float16><<<a.sequences, kThreads, 0, stream>>>(k);
-        else verify_join_kernel<float><<<a.sequences, kThreads, 0, stream>>>(k);
-    }
+    const Plan p = plan_of(a);
+    const int64_t steps = (a.vocabulary + kStep - 1) / kStep, slice = (steps + p.parts - 1) / p.parts * kStep;
+    const VerifyArgs k{a.target,   a.draft,    a.drafted,                      a.uniform,    a.noise, a.counts,    a.tokens,
+                       a.accepted, static_cast<uint64_t *>(a.work), a.vocabulary, slice,   a.sequences, a.drafts, p.parts};
+    if (a.half) launch<_Float16>(k, p, stream);
+    else launch<float>(k, p, stream);
     return hipGetLastError();
 }
 

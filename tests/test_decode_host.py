@@ -155,7 +155,7 @@ def test_prompt_refusals():
     for bad in (dict(heads=0), dict(heads=3), dict(kv_heads=0), dict(head_dim=96), dict(tokens=-1), dict(keys=-1), dict(sequences=0), dict(keys=1 << 40)):
         assert ask(prompt(**bad)) == SHAPE, bad
     assert ask(prompt(tokens=0, q=rows(data=None))) == 0
-    for bad in (dict(k=rows(token_stride=-128)), dict(v=rows(token_stride=(1 << 25) + 8))):
+    for bad in (dict(k=rows(token_stride=-128)), dict(v=rows(token_stride=(1 << 24) + 8))):
         assert ask(prompt(**bad)) == SHAPE, bad
     size = ctypes.c_size_t(7)
     long = prompt(keys=1 << 18)

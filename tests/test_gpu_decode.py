@@ -461,7 +461,8 @@ def check_verify(B, target, draft, drafted, uniform, noise, counts=None):
 
 
 @pytest.mark.parametrize("half", [False, True])
-@pytest.mark.parametrize("S,N,V", [(1, 1, 1), (1, 4, 32000), (3, 2, 7), (5, 7, 255), (7, 3, 257), (64, 4, 1001), (2, 8, 50257), (300, 1, 33), (1, 1, 131071)])
+@pytest.mark.parametrize("S,N,V", [(1, 1, 1), (1, 4, 32000), (3, 2, 7), (5, 7, 255), (7, 3, 257), (64, 4, 1001), (2, 8, 50257), (300, 1, 33), (1, 1, 131071), (2, 3, 8191), (2, 3, 16384), (2, 3, 16385),
+                                   (1030, 2, 2049)])
 def test_verify(B, half, S, N, V):
     inputs = verify_inputs(S, N, V, half, seed=S * 1000 + V)
     check_verify(B, *inputs)
