@@ -43,6 +43,9 @@ constexpr int kStep = kTile * kWaves;       // keys per workgroup and step
 constexpr int kMaxChunk = 64 / 2 * kStep;   // a lane of a wave holds the page of one 16-key half: 32 steps
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.0f;
+// Exponents are fma(score, scale, -rounded product of maximum and scale): off by that rounding, up to 2^-11 of a weight at this size.  From there on the
+// maximum is taken from the scores first: at 2^31 the rounding alone would be an exponent of 128.
+constexpr float kFar = 0x1p14f;
 
 struct Item {
     int sequence, tile, begin, tokens, length;
@@ -211,6 +214,7 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 6
     const float scale = fabsf(a.scale) * kLog2e;
     float4_t o[NR][kN], offset[NR], start[NR]; // offset: 128 sum p step, on every channel; start: what takes the keys' 64 out
     float m[NR], l[NR], bias[NR];
+    bool far[NR]; // scores whose product with the scale is too large to be rounded by itself
     const uint32_t key_mask = in_vector(0x00f000f0u), value_mask = in_vector(0x000f000fu);
     const uint32_t ones = 0x43004300u; // bfloat16 128
     const bf8_t all = __builtin_bit_cast(bf8_t, uint4_t{ones, ones, ones, ones});
@@ -221,6 +225,7 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 6
         const float x = -64.0f * q_sum[r];
         start[r] = float4_t{x, x, x, x};
         l[r] = bias[r] = 0;
+        far[r] = false;
 #pragma unroll
         for (int i = 0; i < kN; ++i) o[r][i] = float4_t{0, 0, 0, 0};
     }
@@ -283,13 +288,20 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 6
                 top = fmaxf(top, __shfl_xor(top, 32));
                 const float next_m = fmaxf(m[r], top), keep = next_m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m[r] - next_m) * scale);
                 m[r] = next_m;
+                far[r] = __any(next_m != -INFINITY && fabsf(next_m) * scale > kFar);
                 l[r] *= keep;
                 bias[r] *= keep;
                 offset[r] *= keep;
 #pragma unroll
                 for (int i = 0; i < kN; ++i) o[r][i] *= keep;
             }
-            const float base = m[r] == -INFINITY ? 0.0f : m[r] * scale;
+            const float from = m[r] == -INFINITY ? 0.0f : m[r];
+            float base = from * scale;
+            if (far[r]) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[r][i >> 2][i & 3] -= from;
+                base = 0.0f;
+            }
             uint4_t hi, lo;
 #pragma unroll
             for (int i = 0; i < 8; i += 2) {

@@ -410,6 +410,55 @@ def test_prompt_starts_that_make_no_sense(B):
     assert B.ap_attention_prompt(empty, k, v, torch.zeros(2, dtype=torch.int32).cuda(), torch.tensor([0, 40], dtype=torch.int32).cuda()).shape == (0, 2, 64)
 
 
+# ------------------------------------------------------------------------------------------------ scores of any size
+
+
+def attend(B, kernel, q, k, v, scale=None):
+    """One sequence whose queries are its last tokens, by either kernel: (out, keys, values, bound): what stands for k and v there, and the error of
+    a weighted mean of values with exact weights."""
+    if kernel == "prompt":
+        out = B.ap_attention_prompt(q, k, v, U.starts([len(q)]).cuda(), U.starts([len(k)]).cuda(), scale=scale)
+        return out, k.double(), v.double(), 64 * U.EPS32 * v.double().abs().amax()
+    page = 32
+    table, pages = U.page_table([len(k)], page)
+    cache = full_cache(B, pages, k.shape[1], k.shape[2], page)
+    B.ap_cache_append(cache, k, v, U.slots_of(table, page, 0, 0, len(k)).cuda())
+    out = B.ap_attention_cached(cache, q, table.cuda(), torch.tensor([len(k)], dtype=torch.int32).cuda(), scale=scale)
+    _, low, step = U.codes_of(v)
+    # values enter the sums as low + step (offset + code), weights times steps as two bfloat16 numbers
+    return out, U.cache_values(k), U.cache_values(v), (64 * U.EPS32 * (low.abs() + 143 * step) + 2.0 ** -16 * 15 * step).double().amax()
+
+
+@pytest.mark.parametrize("kernel", ["cached", "prompt"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("size", [1.0, 300.0, 20000.0, 30000.0, 40000.0, 65504.0])
+def test_equal_keys_of_any_size_are_averaged(B, kernel, D, size):
+    # equal keys have equal scores, however these and their product with the scale round: in a tile, across waves and across ranges
+    for n, m in ((3, 20), (2, 130), (5, 700), (1, 5000)):
+        q, k, v = torch.full((n, 4, D), size, dtype=torch.float16, device="cuda"), torch.full((m, 2, D), size, dtype=torch.float16, device="cuda"), normal(m, m, 2, D)
+        for scale in (None, -0.2):
+            out, _, values, err = attend(B, kernel, q, k, v, scale)
+            for i in range(n):
+                want = values[:m - n + 1 + i].mean(0).repeat_interleave(2, 0)
+                U.check(out[i], want, U.HALF_EPS16 * want.abs() + err + U.SUBNORMAL16, "query %d of %d keys" % (i, m))
+
+
+@pytest.mark.parametrize("kernel", ["cached", "prompt"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("size,scale", [(30.0, None), (300.0, None), (20000.0, None), (20000.0, -1.0), (1.0, 3e4), (1.0, 1e30), (20000.0, 1e30)])
+def test_the_greatest_score_of_any_size_takes_all(B, kernel, D, size, scale):
+    n, m = 8, 700
+    k, v = (normal(1, m, 2, D).float() * size).clamp(-60000, 60000).half(), normal(2, m, 2, D)
+    of = torch.tensor([(i * 97 + 40) % (m - n) for i in range(n)]).cuda()
+    q = k[of].repeat_interleave(2, 1) * (-1 if scale and scale < 0 else 1)
+    out, keys, values, err = attend(B, kernel, q, k, v, scale)
+    s = torch.matmul(q.double().transpose(0, 1), keys.repeat_interleave(2, 1).permute(1, 2, 0).contiguous()) * (scale or D ** -0.5)   # (heads, n, m)
+    first, second = s.topk(2, dim=2).values.unbind(2)
+    assert (first - second > 60 + s.abs().amax() * 2.0 ** -16).all() and (s.argmax(2) == of).all()
+    want = values[of].repeat_interleave(2, 1)
+    U.check(out, want, U.HALF_EPS16 * want.abs() + err + U.SUBNORMAL16)
+
+
 # ------------------------------------------------------------------------------------------------ verification
 
 
