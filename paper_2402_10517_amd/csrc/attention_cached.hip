@@ -485,8 +485,7 @@ hipError_t launch_attention_cached(const ap_cache &c, const ap_cached &a, hipStr
     k.q_starts = a.q_starts, k.lengths = a.lengths, k.tables = a.tables;
     k.tokens = (int)a.tokens, k.heads = a.heads, k.sequences = a.sequences, k.max_length = (int)a.max_length;
     k.items = (int)p.items, k.splits = p.splits, k.chunk = p.chunk;
-    // a scale of 0 makes all weights equal, as this one does; scores of -inf (keys that are not seen) stay what they are
-    k.scale = fabsf(a.scale) < 1e-30f ? 1e-30f : a.scale;
+    k.scale = scale_in_range(a.scale);
     k.slack = kSlack / (fabsf(k.scale) * kLog2e);
     k.out = static_cast<_Float16 *>(a.out);
     k.part = static_cast<float *>(a.work);

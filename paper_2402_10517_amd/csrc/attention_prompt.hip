@@ -456,8 +456,7 @@ hipError_t launch_attention_prompt(const ap_prompt &a, hipStream_t stream)
     k.tokens = (int)a.tokens, k.keys = (int)a.keys;
     k.q_starts = a.q_starts, k.k_starts = a.k_starts;
     k.heads = a.heads, k.kv_heads = a.kv_heads, k.sequences = a.sequences;
-    // a scale of 0 makes all weights equal, as this one does; scores of -inf (keys that are not seen) stay what they are
-    k.scale = fabsf(a.scale) < 1e-30f ? 1e-30f : a.scale;
+    k.scale = scale_in_range(a.scale);
     k.slack = kSlack / (fabsf(k.scale) * kLog2e);
     k.out = static_cast<_Float16 *>(a.out);
     const PromptPlan p = plan_of(a);

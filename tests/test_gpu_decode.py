@@ -445,7 +445,7 @@ def test_equal_keys_of_any_size_are_averaged(B, kernel, D, size):
 
 @pytest.mark.parametrize("kernel", ["cached", "prompt"])
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("size,scale", [(30.0, None), (300.0, None), (20000.0, None), (20000.0, -1.0), (1.0, 3e4), (1.0, 1e30), (20000.0, 1e30)])
+@pytest.mark.parametrize("size,scale", [(30.0, None), (300.0, None), (20000.0, None), (20000.0, -1.0), (1.0, 3e4), (1.0, 1e30), (20000.0, 1e30), (1.0, 3e38), (300.0, -3e38)])
 def test_the_greatest_score_of_any_size_takes_all(B, kernel, D, size, scale):
     n, m = 8, 700
     k, v = (normal(1, m, 2, D).float() * size).clamp(-60000, 60000).half(), normal(2, m, 2, D)
