@@ -39,13 +39,15 @@ template <int V> __device__ __forceinline__ void store_row(_Float16 *p, const fl
 // or (interleaved) of channels 2 i, 2 i + 1
 template <int V> struct Turn {
     float cosine[V], sine[V];
+    bool stays; // channels beyond the rotation: not 1 x + 0 y, which is NaN for an infinity and +0 for -0
     __device__ void load(const AppendArgs &a, int c, int64_t token)
     {
         const int d = c * V, half = a.rot_dim / 2;
         const bool upper = d >= half;
+        stays = d >= a.rot_dim;
 #pragma unroll
-        for (int i = 0; i < V; ++i) cosine[i] = 1, sine[i] = 0; // channels that stay: 1 x + 0 y
-        if (d >= a.rot_dim) return;
+        for (int i = 0; i < V; ++i) cosine[i] = sine[i] = 0;
+        if (stays) return;
         const int64_t position = a.positions[token];
         if (position < 0 || position >= a.rotary_rows) {
 #pragma unroll
@@ -103,6 +105,10 @@ template <int V, int TURN> __device__ __forceinline__ void rotate(const Turn<V> 
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i) x[i] = TURN == kNoTurn ? (float)own[i] : (float)own[i] * turn.cosine[i] + (float)other[i] * turn.sine[i];
+    }
+    if constexpr (TURN == kPartTurn || TURN == kInterleaved) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = turn.stays ? (float)own[i] : x[i];
     }
 }
 

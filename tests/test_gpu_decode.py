@@ -154,6 +154,30 @@ def test_tensors_that_do_not_fit_are_refused(B):
         B.ap_verify(*p, counts=torch.zeros(3, dtype=torch.int32).cuda())
 
 
+@pytest.mark.parametrize("D,rot", [(64, 32), (128, 64), (128, 16), (128, 112), (128, 128)])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("tokens", [5, 300])
+def test_channels_beyond_the_rotation_stay(B, D, rot, inter, tokens):
+    H, G = 6, 2
+    q, k, v = normal(1, tokens, H, D), normal(2, tokens, G, D), normal(3, tokens, G, D)
+    if rot < D:
+        for x in (q, k):
+            x[..., rot], x[1::3, :, rot + 5], x[2::3, :, D - 2], x[::2, :, D - 3] = -0.0, float("inf"), float("nan"), float("-inf")
+    rotary = B.rotary_table(tokens + 3, rot)
+    positions = torch.arange(tokens).cuda() + 3
+    positions[tokens // 2] = 2 ** 40                            # no row of the table
+    cache = full_cache(B, -(-tokens // 16), G, D, 16)
+    q_out, k_out = B.ap_cache_append(cache, k, v, torch.arange(tokens).cuda(), q=q, positions=positions, rotary=rotary, interleaved=inter)
+    positions[tokens // 2] = 0
+    for x, got in ((q, q_out), (k, k_out)):
+        assert torch.equal(got[..., rot:].view(torch.int16), x[..., rot:].view(torch.int16))
+        want = U.rotate(x, rotary, positions, inter)[..., :rot]
+        want[tokens // 2] = float("nan")
+        U.check(got[..., :rot], want, U.HALF_EPS16 * want.abs() + 4 * U.EPS32 * x[..., :rot].double().abs().amax(-1, keepdim=True) + U.SUBNORMAL16)
+    k_got, _ = B.ap_cache_read(cache, torch.arange(tokens).cuda())
+    assert torch.equal(torch.isnan(k_got).all(-1), ~torch.isfinite(k_out).all(-1))
+
+
 # ------------------------------------------------------------------------------------------------ attention over the cache
 
 
