@@ -27,10 +27,12 @@ struct VerifyArgs {
     int sequences, drafts, parts;
 };
 
-// A candidate as one number whose order is that of (ratio, lower index): ratios are not negative, so their bits order like they do.  0 = none
-__device__ __forceinline__ uint64_t candidate(float ratio, int64_t v)
+// A candidate as one number whose order is that of (ratio, lower index): ratios are not negative, so their bits order like they do, and indexes are
+// below 2^31, so that every candidate is greater than kNoNoise: tokens with a weight, none with noise that counts.  0 = no token with a weight
+constexpr uint64_t kNoNoise = 1;
+__device__ __forceinline__ uint64_t candidate(float ratio, int64_t v, bool weight)
 {
-    return ratio >= 0.0f ? (uint64_t)__float_as_uint(ratio) << 32 | (uint32_t)~(uint32_t)v : 0;
+    return ratio >= 0.0f ? (uint64_t)__float_as_uint(ratio) << 32 | (uint32_t)~(uint32_t)v : weight ? kNoNoise : 0;
 }
 
 template <int THREADS> __device__ __forceinline__ uint64_t block_max(uint64_t x)
@@ -57,8 +59,10 @@ template <class T, int THREADS> __device__ __forceinline__ uint64_t race(const T
 {
     float best = -1.0f;
     int64_t at = 0;
+    bool weight = false;
     const auto consider = [&](float pv, float qv, float e, int64_t v) {
         const float w = pv - qv, ratio = w / e;
+        weight = weight || w > 0.0f;
         if (w > 0.0f && e >= 0.0f && ratio > best) { // in ascending order: the lowest of equals stays
             best = ratio;
             at = v;
@@ -74,7 +78,7 @@ template <class T, int THREADS> __device__ __forceinline__ uint64_t race(const T
         for (int i = 0; i < kEach; ++i) consider((float)a.x[i], q ? (float)b.x[i] : 0.0f, e.x[i], v + i);
     }
     for (int i = 0; i < kEach && v + i < to; ++i) consider((float)p[v + i], q ? (float)q[v + i] : 0.0f, noise[v + i], v + i);
-    return block_max<THREADS>(candidate(best, at));
+    return block_max<THREADS>(candidate(best, at, weight));
 }
 
 struct Sequence {
@@ -110,12 +114,12 @@ template <class T> __device__ __forceinline__ Sequence accept(const VerifyArgs &
     return r;
 }
 
-// The end of a sequence, once the best of the whole vocabulary is known (0: none with more than its draft, or none at all)
+// The end of a sequence, once the best of the whole vocabulary is known (0 after a refusal: no token has more than its draft)
 template <class T, int THREADS> __device__ __forceinline__ void finish(const VerifyArgs &a, int64_t s, int accepted, bool refused, uint64_t won)
 {
     if (!won && refused)
         won = race<T, THREADS>(static_cast<const T *>(a.target) + (s * (a.drafts + 1) + accepted) * a.vocabulary, nullptr, a.noise + s * a.vocabulary, 0, a.vocabulary);
-    const int64_t token = won ? (int64_t)(uint32_t)~(uint32_t)won : -1;
+    const int64_t token = won > kNoNoise ? (int64_t)(uint32_t)~(uint32_t)won : -1;
     for (int i = threadIdx.x; i <= a.drafts; i += THREADS)
         a.tokens[s * (a.drafts + 1) + i] = i < accepted ? a.drafted[s * a.drafts + i] : i == accepted ? token : -1;
 }

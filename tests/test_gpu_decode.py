@@ -581,6 +581,27 @@ def test_verify_tokens_follow_the_target(B):
     assert np.abs(share - p).max() < 5 * 0.5 / S ** 0.5         # five standard deviations of a share
 
 
+@pytest.mark.parametrize("half", [False, True])
+@pytest.mark.parametrize("V", [40, 5000, 40000])
+def test_verify_where_no_noise_of_the_rest_counts(B, half, V):
+    # refused drafts, and tokens with more than their draft: the token after them is one of these, or none where none of their noise is a number from 0 on
+    target, draft, drafted, uniform, noise = verify_inputs(6, 2, V, half, seed=V)
+    drafted[:, 0] = 3
+    draft[:, 0], target[:, 0] = 2.0 / V, 1.0 / V                # more in the draft, but for two tokens
+    target[:, 0, 3] = 0                                         # refused
+    for at in (7, V - 2):
+        target[:, 0, at] = 4.0 / V
+    noise[0, [7, V - 2]] = np.nan
+    noise[1, [7, V - 2]] = -1.0
+    noise[2, [7, V - 2]] = np.nan, 5.0
+    noise[3, [7, V - 2]] = 0.5, -np.inf
+    noise[4, [7, V - 2]] = np.inf, -1.0                         # a ratio of 0 counts
+    d = [torch.from_numpy(np.ascontiguousarray(x)).cuda() for x in (target, draft, drafted, uniform, noise)]
+    tokens, accepted = B.ap_verify(*d)
+    assert not accepted.any() and (tokens[:, 1:] == -1).all()
+    assert tokens[:5, 0].tolist() == [-1, -1, V - 2, 7, 7] and tokens[5, 0].item() == (7 if noise[5, 7] <= noise[5, V - 2] else V - 2)
+
+
 # ------------------------------------------------------------------------------------------------ all of them
 
 
