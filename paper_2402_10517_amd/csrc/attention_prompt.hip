@@ -44,6 +44,7 @@ constexpr float kSlack = 8.0f;
 // Weights are 2^7 e^(..): up to 2^15, and above the subnormal numbers of binary16 down to 2^-21 of the greatest
 constexpr float kRaise = 7.0f;
 constexpr int kLeastTiles = 4;    // of a range of keys
+constexpr int64_t kMostRanges = 64;
 constexpr int kJoinThreads = 256;
 // instruction classes of the scheduler's groups
 constexpr int kProducts = 0x8, kLdsReads = 0x100;
@@ -417,17 +418,20 @@ struct PromptPlan {
 };
 
 // Row tiles (at most), and the ranges of keys that they are divided into: as many as fill the places that the card has for workgroups (two per CU at
-// head_dim 128, four at 64), of four tiles at least, where that saves more than it costs: a workgroup takes about 0.9 us for a tile of 64 keys (0.6
+// head_dim 128, four at 64), of four tiles at least and 64 in number at most, where that saves more than it costs: a workgroup takes about 0.9 us for a tile of 64 keys (0.6
 // at head_dim 64), the second launch 5 us, and the sums go through memory, written and read, at 4 TB/s.  us without / with ranges: 1 query of 8 heads
 // over 4000 keys 72 / 16, 200 of 32 over 8000 141 / 48, 3 x 500 of 16 x 64 over 7500 109 / 74; where the rule keeps to one: 512 of 32 over 512 16 /
-// 21, 2000 of 16 x 64 over 2000 32 / 34.
+// 21, 2000 of 16 x 64 over 2000 32 / 34.  More ranges make the join longer than they make the ranges shorter; us of 1 query of 8 heads and one key head
+// with 32 / 64 / 128 / 256 / 512 ranges: 32768 keys 32 / 30 / 41, 65536 50 / 40 / 46 / 75, 131000 85 / 57 / 55 / 80 / 121; heads of 64, 131072 keys 64 / 46
+// / 46 / 72 / 128.
 PromptPlan plan_of(const ap_prompt &a)
 {
     PromptPlan p;
     p.items = a.tokens * (a.heads / a.kv_heads) / kRows + a.sequences;
     const int64_t places = a.head_dim == 64 ? 1024 : 512, units = p.items * a.kv_heads, each = a.keys / a.sequences, room = each / (kKeys * kLeastTiles);
     int64_t splits = places / units;
-    splits = splits > room ? room : splits > 64 ? 64 : splits;
+    splits = splits < room ? splits : room;
+    splits = splits < kMostRanges ? splits : kMostRanges;
     if (splits > 1) {
         const double alone = (double)each / kKeys * (a.head_dim == 64 ? 0.6 : 0.9), sums = 2.0 * splits * a.tokens * a.heads * a.head_dim * sizeof(float);
         if (alone * (1.0 - 1.0 / splits) < 5.0 + sums / 4e6) splits = 1;

@@ -168,6 +168,18 @@ def test_prompt_refusals():
     assert B.lib.ap_attention_prompt_size(ctypes.byref(prompt()), None) == INVALID
 
 
+@pytest.mark.parametrize("head_dim", [64, 128])
+def test_prompt_ranges_grow_with_the_keys_up_to_a_bound(head_dim):
+    # the workspace holds head_dim + 2 floats per row and range: 64 ranges at most, however many would fit
+    size = ctypes.c_size_t(0)
+    ranges = []
+    for keys in (1 << 14, 1 << 15, 100000, 131000, (1 << 17) - 1, 1 << 17, 1 << 20, 1 << 25):
+        a = prompt(tokens=1, heads=8, kv_heads=1, keys=keys, sequences=1, head_dim=head_dim)
+        assert B.lib.ap_attention_prompt_size(ctypes.byref(a), ctypes.byref(size)) == 0
+        ranges.append(size.value // (8 * (head_dim + 2) * 4))
+    assert ranges == sorted(ranges) and ranges[-1] == 64, ranges
+
+
 def test_verify_refusals():
     ask = lambda a: of(B.lib.ap_verify, a)
     assert ask(None) == INVALID
