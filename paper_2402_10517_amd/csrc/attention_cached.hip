@@ -40,7 +40,7 @@ constexpr int kThreads = 256;
 constexpr int kWaves = 4;
 constexpr int kTile = 32;                   // keys per wave and step
 constexpr int kStep = kTile * kWaves;       // keys per workgroup and step
-constexpr int kMaxChunk = 64 / 2 * kStep;   // a lane of a wave holds the page of one 16-key half: 32 steps
+constexpr int kPiece = 64 / 2 * kStep;      // keys whose pages a wave holds, those of one 16-key half per lane: 32 steps
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.0f;
 // Exponents are fma(score, scale, -rounded product of maximum and scale): off by that rounding, up to 2^-11 of a weight at this size.  From there on the
@@ -174,12 +174,12 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 6
     Item it;
     if (!find_item(a, kRows, item, &it)) return;
     const int sequence = it.sequence, tile = it.tile, begin = it.begin, n = it.tokens, c0 = split * a.chunk;
-    // pages of the wave's keys, one half of 16 per lane; asked for before the length is known
-    int pages = -1;
-    {
-        const int t = c0 + kTile * (wave + kWaves * (lane >> 1)) + 16 * (lane & 1);
-        if (t < a.max_length) pages = a.tables[(int64_t)sequence * a.table_width + (t >> a.cache.log_page)];
-    }
+    // pages of the wave's keys in a piece, one half of 16 per lane; the first ones are asked for before the length is known
+    const auto pages_of = [&](int piece) {
+        const int t = piece + kTile * (wave + kWaves * (lane >> 1)) + 16 * (lane & 1);
+        return t < a.max_length ? a.tables[(int64_t)sequence * a.table_width + (t >> a.cache.log_page)] : -1;
+    };
+    int pages = pages_of(c0);
     const int length = __builtin_amdgcn_readfirstlane(it.length);
     if ((int64_t)pages >= a.cache.pages) pages = -1;
     // keys that the tile's first and last row see
@@ -230,11 +230,11 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 6
         for (int i = 0; i < kN; ++i) o[r][i] = float4_t{0, 0, 0, 0};
     }
 
-    const int mine = c1 - c0 - kTile * wave, steps = mine > 0 ? (mine + kStep - 1) / kStep : 0;
     const int lp = a.cache.log_page, page_mask = (1 << lp) - 1;
     const Lane at{(uint32_t)(c * L::kRow + g * (D / 8)), (uint32_t)((L::kRow << lp) + g * 4 * L::kRow + c * 8 * L::kHalves), (uint32_t)g * 16, (uint32_t)((4 << lp) + g * 16)};
+    int piece = c0;
     const auto load = [&](int step, Half<D> (&h)[2]) {
-        const int t = c0 + kTile * (wave + kWaves * step);
+        const int t = piece + kTile * (wave + kWaves * step);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const int page = __builtin_amdgcn_readlane(pages, 2 * step + half);
@@ -242,97 +242,106 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 6
         }
     };
     Half<D> next[2];
-    if (steps > 0) load(0, next);
+    // A range of more than a piece starts anew in each, a wait for pages and keys in 32 steps.  Only with 32 rows: with 16 the loop around costs short
+    // ranges 3 to 5 %, and their sums are few.
+    for (;;) {
+        const int mine = (NR == 2 && c1 - piece > kPiece ? kPiece : c1 - piece) - kTile * wave, steps = mine > 0 ? (mine + kStep - 1) / kStep : 0;
+        if (steps > 0) load(0, next);
 #pragma unroll 1
-    for (int step = 0; step < steps; ++step) {
-        Half<D> h[2] = {next[0], next[1]};
-        if (step + 1 < steps) load(step + 1, next);
-        const int t0 = c0 + kTile * (wave + kWaves * step);
-        const bool known0 = __builtin_amdgcn_readlane(pages, 2 * step) >= 0, known1 = __builtin_amdgcn_readlane(pages, 2 * step + 1) >= 0;
-        const bool whole = known0 && known1 && t0 + kTile <= sees_least && t0 + kTile <= c1;
+        for (int step = 0; step < steps; ++step) {
+            Half<D> h[2] = {next[0], next[1]};
+            if (step + 1 < steps) load(step + 1, next);
+            const int t0 = piece + kTile * (wave + kWaves * step);
+            const bool known0 = __builtin_amdgcn_readlane(pages, 2 * step) >= 0, known1 = __builtin_amdgcn_readlane(pages, 2 * step + 1) >= 0;
+            const bool whole = known0 && known1 && t0 + kTile <= sees_least && t0 + kTile <= c1;
 
-        float4_t s[NR][2];
+            float4_t s[NR][2];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
+            for (int half = 0; half < 2; ++half) {
 #pragma unroll
-            for (int k = 0; k < kSteps; ++k) {
-                const half8_t x = key_operand(h[half].k[k], key_mask);
+                for (int k = 0; k < kSteps; ++k) {
+                    const half8_t x = key_operand(h[half].k[k], key_mask);
 #pragma unroll
-                for (int r = 0; r < NR; ++r) s[r][half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, q[r][k], k == 0 ? start[r] : s[r][half], 0, 0, 0);
-            }
-        }
-        bf8_t high[NR], low[NR];
-#pragma unroll
-        for (int r = 0; r < NR; ++r) {
-            uint32_t pairs[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t kp = h[i >> 2].kp[i & 3];
-                s[r][i >> 2][i & 3] = __builtin_fmaf((float)step_of(kp), s[r][i >> 2][i & 3], times(low_of(kp), q_sum[r]));
-                pairs[i] = h[i >> 2].vp[i & 3];
-            }
-            if (!whole) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int t = t0 + 16 * (i >> 2) + 4 * g + (i & 3);
-                    const bool seen = (i < 4 ? known0 : known1) && t < sees[r] && t < c1;
-                    s[r][i >> 2][i & 3] = seen ? s[r][i >> 2][i & 3] : -INFINITY;
-                    pairs[i] = seen ? pairs[i] : 0; // keys that are not seen may hold anything
+                    for (int r = 0; r < NR; ++r) s[r][half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, q[r][k], k == 0 ? start[r] : s[r][half], 0, 0, 0);
                 }
             }
-            float top = s[r][0][0];
-#pragma unroll
-            for (int i = 1; i < 8; ++i) top = fmaxf(top, s[r][i >> 2][i & 3]);
-            if (__any(top - m[r] > a.slack)) { // also from -inf; a sum could round a difference of large scores away
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(top, __shfl_xor(top, 32));
-                const float next_m = fmaxf(m[r], top), keep = next_m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m[r] - next_m) * scale);
-                m[r] = next_m;
-                far[r] = __any(next_m != -INFINITY && fabsf(next_m) * scale > kFar);
-                l[r] *= keep;
-                bias[r] *= keep;
-                offset[r] *= keep;
-#pragma unroll
-                for (int i = 0; i < kN; ++i) o[r][i] *= keep;
-            }
-            const float from = m[r] == -INFINITY ? 0.0f : m[r];
-            float base = from * scale;
-            if (far[r]) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) s[r][i >> 2][i & 3] -= from;
-                base = 0.0f;
-            }
-            uint4_t hi, lo;
-#pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                float ps[2];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][(i + j) >> 2][(i + j) & 3], scale, -base));
-                    l[r] += p;
-                    bias[r] = __builtin_fmaf(p, (float)low_of(pairs[i + j]), bias[r]);
-                    ps[j] = times(step_of(pairs[i + j]), p);
-                }
-                hi[i / 2] = pack_bf16(ps[0], ps[1]);
-                lo[i / 2] = pack_bf16(ps[0] - __builtin_bit_cast(float, hi[i / 2] << 16), ps[1] - __builtin_bit_cast(float, hi[i / 2] & 0xffff0000u));
-            }
-            high[r] = __builtin_bit_cast(bf8_t, hi);
-            low[r] = __builtin_bit_cast(bf8_t, lo);
-        }
-#pragma unroll
-        for (int r = 0; r < NR; ++r) {
-            offset[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(all, high[r], offset[r], 0, 0, 0);
-            offset[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(all, low[r], offset[r], 0, 0, 0);
-        }
-#pragma unroll
-        for (int i = 0; i < kN; ++i) {
-            const bf8_t v = value_operand<D>(h, i, value_mask);
+            bf8_t high[NR], low[NR];
 #pragma unroll
             for (int r = 0; r < NR; ++r) {
-                o[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, high[r], o[r][i], 0, 0, 0);
-                o[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, low[r], o[r][i], 0, 0, 0);
+                uint32_t pairs[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t kp = h[i >> 2].kp[i & 3];
+                    s[r][i >> 2][i & 3] = __builtin_fmaf((float)step_of(kp), s[r][i >> 2][i & 3], times(low_of(kp), q_sum[r]));
+                    pairs[i] = h[i >> 2].vp[i & 3];
+                }
+                if (!whole) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int t = t0 + 16 * (i >> 2) + 4 * g + (i & 3);
+                        const bool seen = (i < 4 ? known0 : known1) && t < sees[r] && t < c1;
+                        s[r][i >> 2][i & 3] = seen ? s[r][i >> 2][i & 3] : -INFINITY;
+                        pairs[i] = seen ? pairs[i] : 0; // keys that are not seen may hold anything
+                    }
+                }
+                float top = s[r][0][0];
+#pragma unroll
+                for (int i = 1; i < 8; ++i) top = fmaxf(top, s[r][i >> 2][i & 3]);
+                if (__any(top - m[r] > a.slack)) { // also from -inf; a sum could round a difference of large scores away
+                    top = fmaxf(top, __shfl_xor(top, 16));
+                    top = fmaxf(top, __shfl_xor(top, 32));
+                    const float next_m = fmaxf(m[r], top), keep = next_m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m[r] - next_m) * scale);
+                    m[r] = next_m;
+                    far[r] = __any(next_m != -INFINITY && fabsf(next_m) * scale > kFar);
+                    l[r] *= keep;
+                    bias[r] *= keep;
+                    offset[r] *= keep;
+#pragma unroll
+                    for (int i = 0; i < kN; ++i) o[r][i] *= keep;
+                }
+                const float from = m[r] == -INFINITY ? 0.0f : m[r];
+                float base = from * scale;
+                if (far[r]) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s[r][i >> 2][i & 3] -= from;
+                    base = 0.0f;
+                }
+                uint4_t hi, lo;
+#pragma unroll
+                for (int i = 0; i < 8; i += 2) {
+                    float ps[2];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][(i + j) >> 2][(i + j) & 3], scale, -base));
+                        l[r] += p;
+                        bias[r] = __builtin_fmaf(p, (float)low_of(pairs[i + j]), bias[r]);
+                        ps[j] = times(step_of(pairs[i + j]), p);
+                    }
+                    hi[i / 2] = pack_bf16(ps[0], ps[1]);
+                    lo[i / 2] = pack_bf16(ps[0] - __builtin_bit_cast(float, hi[i / 2] << 16), ps[1] - __builtin_bit_cast(float, hi[i / 2] & 0xffff0000u));
+                }
+                high[r] = __builtin_bit_cast(bf8_t, hi);
+                low[r] = __builtin_bit_cast(bf8_t, lo);
+            }
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                offset[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(all, high[r], offset[r], 0, 0, 0);
+                offset[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(all, low[r], offset[r], 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < kN; ++i) {
+                const bf8_t v = value_operand<D>(h, i, value_mask);
+#pragma unroll
+                for (int r = 0; r < NR; ++r) {
+                    o[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, high[r], o[r][i], 0, 0, 0);
+                    o[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, low[r], o[r][i], 0, 0, 0);
+                }
             }
         }
+        if (NR == 1 || c1 - piece <= kPiece) break;
+        piece += kPiece;
+        pages = pages_of(piece);
+        if ((int64_t)pages >= a.cache.pages) pages = -1;
     }
 
     // join the waves: all sums to the common maximum, then every thread takes D / 16 channels of a row
@@ -447,21 +456,28 @@ struct Plan {
 Plan plan_of(const ap_cache &c, const ap_cached &a)
 {
     Plan p;
-    const int64_t group = a.heads / c.kv_heads, each = (a.tokens + a.sequences - 1) / a.sequences;
-    p.rows = each * group <= 16 ? 1 : 2;
-    const int64_t tile = 16 * p.rows;
-    p.items = a.q_starts ? a.tokens * group / tile + a.sequences : (each * group + tile - 1) / tile * a.sequences;
+    const int64_t group = a.heads / c.kv_heads, each = (a.tokens + a.sequences - 1) / a.sequences, longest = a.max_length > 0 ? a.max_length : 1;
+    const auto items_of = [&](int64_t tile) { return a.q_starts ? a.tokens * group / tile + a.sequences : (each * group + tile - 1) / tile * a.sequences; };
+    // 16 rows where that is enough for a sequence's queries, in ranges of one piece at most.  2^20 such ranges are more keys than the card's memory can
+    // hold: max_length is then far above the lengths, and the other kernel's ranges of any length keep the workgroups few.
+    p.rows = each * group <= 16 && longest / kPiece * items_of(16) * c.kv_heads <= 1 << 20 ? 1 : 2;
+    p.items = items_of(16 * p.rows);
     // Ranges of keys.  Two workgroups per CU in all, of 256 keys at least; four where two would have more than 1024 keys each, as longer ranges leave
     // the card waiting for the last.  One, and no second launch, where every CU has a workgroup of up to 2048 keys.  us at 1 / 2 / 4 / 8 / 16 / 32 /
     // 64 ranges, heads of 128: 32 sequences of 2000 keys and 8 key heads 18.4 / 20.7 / 24.0, up to 4099 keys (ragged) - / 29.0 / 25.8 / 27.6, 4 of
     // 3000 and 32 - / 16.9 / 15.6 / 17.6, 16 up to 8000 and 8 - / - / 28.2 / 24.1, 1 of 1000 and 32 10.1 / 9.9 / 8.6 / 8.4, 2 of 131072 and 8 at 32
     // 62.7, at 64 57.9; heads of 64: 8 of 8000 and 4 at 8 12.9, at 16 12.6, at 32 14.6.
-    const int64_t units = p.items * c.kv_heads, longest = a.max_length > 0 ? a.max_length : 1;
-    const int64_t keys = longest * units, two = (keys + 511) / 512, four = (keys + 1023) / 1024;
+    const int64_t units = p.items * c.kv_heads, keys = longest * units, two = (keys + 511) / 512, four = (keys + 1023) / 1024;
     int64_t chunk = two <= 1024 ? two : four > 1024 ? four : 1024;
     if (units >= 256 && longest <= 2048) chunk = longest;
-    chunk = (chunk + kStep - 1) / kStep * kStep;
-    p.chunk = (int)(chunk < 2 * kStep ? 2 * kStep : chunk > kMaxChunk ? kMaxChunk : chunk);
+    // Longer ones are cut all the same, which fills the last round of workgroups; with 32 rows up to some 8192 workgroups, so that their sums are 280 MB
+    // at most.  ms with ranges of 4096 keys / longer ones, 64 heads and 8 key heads of 128: 1 x 4096 queries over 32768 keys 7.78 / 7.13 (1.1 GB of
+    // sums / none), 8 x 512 over 16384 4.20 / 3.78, over up to 16384 2.72 / 2.40.
+    const int64_t cut = (keys + 8191) / 8192, most = p.rows == 2 && cut > kPiece ? cut : kPiece;
+    chunk = chunk > most ? most : chunk;
+    chunk = chunk > longest ? longest : chunk;
+    chunk = chunk < 2 * kStep ? 2 * kStep : chunk;
+    p.chunk = (int)((chunk + kStep - 1) / kStep * kStep);
     p.splits = (int)((longest + p.chunk - 1) / p.chunk);
     return p;
 }

@@ -180,6 +180,21 @@ def test_prompt_ranges_grow_with_the_keys_up_to_a_bound(head_dim):
     assert ranges == sorted(ranges) and ranges[-1] == 64, ranges
 
 
+def test_workspace_of_cached_attention_is_bounded():
+    # Sums of ranges are kept where row tiles are too few for the card; many rows over long caches need no more.  Few rows (16 of a key head at most, 2080 bytes per
+    # range of 4096 keys of 272 bytes, twice for row tiles that are not full) need a small part of what the cache holds.
+    size = ctypes.c_size_t(0)
+    for tokens in (1, 64, 511, 512, 1000, 2048, 4096, 1 << 14, 1 << 18, 1 << 20):
+        for length in (300, 4096, 5000, 32768, 131072, 1 << 20, 1 << 30):
+            for sequences in (1, 8, 64):
+                for head_dim in (64, 128):
+                    if tokens % sequences == 0:
+                        a = cached(tokens=tokens, heads=64, sequences=sequences, q_starts=None, table_width=1 << 24, max_length=length)
+                        assert B.lib.ap_attention_cached_size(ctypes.byref(cache(kv_heads=8, head_dim=head_dim)), ctypes.byref(a), ctypes.byref(size)) == 0
+                        few = tokens // sequences * 8 <= 16
+                        assert size.value <= (300 << 20) + few * sequences * length * 8 * (head_dim + 8) // 32, (tokens, length, sequences, size.value)
+
+
 def test_verify_refusals():
     ask = lambda a: of(B.lib.ap_verify, a)
     assert ask(None) == INVALID

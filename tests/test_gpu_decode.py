@@ -243,6 +243,33 @@ def test_cached_long(B):
     cached_case(B, [33000], [3], 4, 2, 64, 16, uniform=True)
 
 
+@pytest.mark.parametrize("D,H,G,S,longest,queries", [(128, 32, 32, 64, 20001, 1), (128, 32, 16, 256, 70000, 10), (128, 16, 16, 128, 30000, 17),
+                                                       (64, 16, 16, 256, 40001, 20)])
+def test_cached_ranges_longer_than_the_pages_that_a_wave_holds(B, D, H, G, S, longest, queries):
+    # with 32 rows a tile, and tiles enough for the card: ranges of more than 4096 keys; and calls of one query beside them
+    lengths = [longest, 1, 5003, 40] + [(i * 13) % 70 for i in range(S - 6)] + [longest - 3000, longest]
+    cached_case(B, lengths, [queries] * S, H, G, D, 64, uniform=True)
+
+
+def test_cached_few_rows_and_a_bound_far_above_the_lengths(B):
+    # as many ranges of 4096 keys as no launch can have
+    cached_case(B, [300], [1], 1024, 1024, 64, 16, max_length=2 ** 30, width=2 ** 26)
+
+
+def test_cached_pages_outside_the_cache_in_long_ranges(B):
+    S, n, G, D, page, longest, kept = 128, 17, 32, 64, 16, 70000, 5008
+    cache = full_cache(B, kept // page, G, D, page)
+    B.ap_cache_append(cache, normal(1, kept, G, D), normal(2, kept, G, D), torch.arange(kept).cuda())
+    q = normal(3, S * n, G, D)
+    table = torch.full((S, longest // page), 2 ** 30, dtype=torch.int32)
+    table[1::2] = -1
+    table[:, :kept // page] = torch.arange(kept // page)
+    at = lambda length: torch.full((S,), length, dtype=torch.int32).cuda()
+    # the last query alone: the others see fewer keys of the shorter length
+    outs = [B.ap_attention_cached(cache, q, table.cuda(), at(length)).view(S, n, G, D)[:, -1] for length in (longest, kept)]
+    assert torch.equal(*outs)
+
+
 def test_cached_scales_and_bounds(B):
     for scale in (0.0, -0.3, 1.0, 1e-6):
         cached_case(B, [100, 40], [1, 2], 4, 2, 128, 32, scale=scale)
