@@ -77,7 +77,7 @@ ap_status ap_cache_append(const ap_cache *c, const ap_append *a, void *stream);
 ap_status ap_cache_read(const ap_cache *c, const int64_t *slots, int64_t tokens, void *k_out, void *v_out, void *stream);
 
 /*
- * Attention of new tokens (tokens * heads < 2^31 - 256) over the cache: out[i] = sum_j softmax_j(scale * q[i] . k[j]) v[j].
+ * Attention of new tokens (tokens * heads / 16 + sequences * kv_heads < 2^24) over the cache: out[i] = sum_j softmax_j(scale * q[i] . k[j]) v[j].
  *   q          tokens rows of heads heads; the tokens of a sequence are adjacent
  *   q_starts   device, sequences + 1: sequence s has the tokens q_starts[s] .. q_starts[s + 1] - 1; not descending (a sequence
  *              whose two starts descend or leave 0 .. tokens has no tokens).  NULL: tokens / sequences each
@@ -109,7 +109,7 @@ ap_status ap_attention_cached(const ap_cache *c, const ap_cached *a, void *strea
  * k_starts[s + 1] - 1 (device, sequences + 1 each, not descending; a sequence whose two starts descend or leave the rows has none);
  * its last query sees its last key.  Query i of n sees the first m - n + 1 + i of m keys; one that sees none gets zeros, as does
  * one whose scores are all -inf.  What a query does not see does not reach it, NaN and infinities included.
- *   q; k, v    tokens rows of heads heads (tokens * heads < 2^31 - 256); keys rows of kv_heads heads, their token strides in 0 ..
+ *   q; k, v    tokens rows of heads heads (tokens * heads < 2^31 - 256, tokens * heads / 128 + sequences * kv_heads < 2^24); keys rows of kv_heads heads, their token strides in 0 ..
  *              2^24 (AP_ERR_SHAPE otherwise)
  *   out        device, tokens x heads x head_dim, contiguous, 16-byte aligned; only the tokens of q_starts are written
  *   work       device, ap_attention_prompt_size bytes, 16-byte aligned; may be NULL where that is 0

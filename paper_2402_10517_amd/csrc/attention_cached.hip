@@ -506,9 +506,7 @@ hipError_t launch_attention_cached(const ap_cache &c, const ap_cached &a, hipStr
     k.out = static_cast<_Float16 *>(a.out);
     k.part = static_cast<float *>(a.work);
     k.stat = reinterpret_cast<float2 *>(k.part + (size_t)p.splits * a.tokens * a.heads * c.head_dim);
-    const int64_t blocks = p.items * c.kv_heads * p.splits;
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)blocks);
+    const dim3 grid((unsigned)(p.items * c.kv_heads * p.splits)); // within kMostGroups: the caller has looked
     if (c.head_dim == 64) {
         if (p.rows == 1) attention_cached_kernel<64, 1><<<grid, kThreads, 0, stream>>>(k);
         else attention_cached_kernel<64, 2><<<grid, kThreads, 0, stream>>>(k);

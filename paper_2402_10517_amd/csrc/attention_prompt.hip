@@ -464,8 +464,7 @@ hipError_t launch_attention_prompt(const ap_prompt &a, hipStream_t stream)
     k.slack = kSlack / (fabsf(k.scale) * kLog2e);
     k.out = static_cast<_Float16 *>(a.out);
     const PromptPlan p = plan_of(a);
-    const int64_t blocks = p.items * a.kv_heads * p.splits;
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+    const int64_t blocks = p.items * a.kv_heads * p.splits; // within kMostGroups: the caller has looked
     k.items = (int)p.items, k.splits = p.splits;
     k.part = static_cast<float *>(a.work);
     k.stat = reinterpret_cast<float2 *>(k.part + (size_t)p.splits * a.tokens * a.heads * a.head_dim);

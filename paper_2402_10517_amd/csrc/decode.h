@@ -31,6 +31,11 @@ inline int cache_log_page(int page_tokens)
     return -1;
 }
 
+// Workgroups of a launch: a grid has fewer than 2^32 threads, and a workgroup 256.  An attention has one per row tile (16 rows of the cached one at
+// least, 128 of the prompts', one more per sequence) and key head; several per tile only where these are too few for the card.
+constexpr int64_t kMostGroups = ((int64_t)1 << 24) - 1;
+inline bool groups_ok(int64_t rows, int rows_per_tile, int64_t sequences, int kv_heads) { return rows / rows_per_tile + sequences * kv_heads <= kMostGroups; }
+
 hipError_t launch_cache_append(const ap_cache &c, const ap_append &a, hipStream_t stream);
 hipError_t launch_cache_read(const ap_cache &c, const int64_t *slots, int64_t tokens, void *k, void *v, hipStream_t stream);
 size_t attention_cached_work(const ap_cache &c, const ap_cached &a);

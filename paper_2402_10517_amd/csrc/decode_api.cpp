@@ -50,6 +50,7 @@ ap_status check_cached(const ap_cache *c, const ap_cached *a)
     if (s != AP_OK) return s;
     if (a->tokens < 0 || a->tokens > kMaxTokens || a->sequences < 0 || a->sequences > (1 << 20)) return AP_ERR_SHAPE;
     if ((a->tokens > 0 && a->sequences < 1) || a->tokens * a->heads > kMaxTokens) return AP_ERR_SHAPE;
+    if (!groups_ok(a->tokens * a->heads, 16, a->sequences, c->kv_heads)) return AP_ERR_SHAPE;
     if (!a->q_starts && a->sequences > 0 && a->tokens % a->sequences) return AP_ERR_SHAPE;
     if (a->table_width < 0 || a->table_width >= (int64_t)1 << 31 || a->max_length < 0 || a->max_length > 1 << 30 ||
         a->max_length > a->table_width * c->page_tokens)
@@ -128,7 +129,7 @@ static ap_status check_prompt(const ap_prompt *a)
     const ap_status s = check_heads(a->heads, a->kv_heads);
     if (s != AP_OK) return s;
     if (a->tokens < 0 || a->tokens > kMaxTokens || a->keys < 0 || a->keys > kMaxTokens || a->sequences < 0 || a->sequences > (1 << 20) ||
-        (a->tokens > 0 && a->sequences < 1) || a->tokens * a->heads > kMaxTokens)
+        (a->tokens > 0 && a->sequences < 1) || a->tokens * a->heads > kMaxTokens || !groups_ok(a->tokens * a->heads, 128, a->sequences, a->kv_heads))
         return AP_ERR_SHAPE;
     // a tile of 64 rows of k or v is addressed by 32 bits from its first
     if (a->k.token_stride < 0 || a->k.token_stride > 1 << 24 || a->v.token_stride < 0 || a->v.token_stride > 1 << 24) return AP_ERR_SHAPE;

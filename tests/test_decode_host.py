@@ -180,6 +180,23 @@ def test_prompt_ranges_grow_with_the_keys_up_to_a_bound(head_dim):
     assert ranges == sorted(ranges) and ranges[-1] == 64, ranges
 
 
+def test_sizes_that_no_launch_can_have_are_refused():
+    # a grid has fewer than 2^32 threads; workgroups have 256
+    size = ctypes.c_size_t(7)
+    cached_size = lambda kv, **kw: B.lib.ap_attention_cached_size(ctypes.byref(cache(kv_heads=kv)), ctypes.byref(cached(**kw)), ctypes.byref(size))
+    prompt_size = lambda **kw: B.lib.ap_attention_prompt_size(ctypes.byref(prompt(**kw)), ctypes.byref(size))
+    for kv, bad in ((2, dict(tokens=1 << 24, heads=16)), (8, dict(tokens=1 << 22, heads=64, sequences=1, q_starts=None)), (16, dict(tokens=3, heads=16, sequences=1 << 20)),
+                    (1024, dict(tokens=1 << 14, heads=1024, sequences=1 << 14))):
+        assert cached_size(kv, **bad) == SHAPE, (kv, bad)
+        assert of(B.lib.ap_attention_cached, cache(kv_heads=kv), cached(**bad)) == SHAPE, (kv, bad)
+    for bad in (dict(heads=16, kv_heads=16, sequences=1 << 20), dict(heads=1024, kv_heads=1024, sequences=1 << 14), dict(tokens=1 << 21, heads=1000, kv_heads=1000, sequences=1 << 10)):
+        assert prompt_size(**bad) == SHAPE, bad
+        assert of(B.lib.ap_attention_prompt, prompt(**bad)) == SHAPE, bad
+    # and what is just within them is not
+    assert cached_size(2, tokens=(1 << 24) - 64, heads=16, sequences=1) == 0 and cached_size(15, tokens=3, heads=15, sequences=1 << 20) == 0
+    assert prompt_size(heads=15, kv_heads=15, sequences=1 << 20) == 0 and prompt_size(tokens=(1 << 25) - (1 << 12), heads=63, kv_heads=9) == 0
+
+
 def test_workspace_of_cached_attention_is_bounded():
     # Sums of ranges are kept where row tiles are too few for the card; many rows over long caches need no more.  Few rows (16 of a key head at most, 2080 bytes per
     # range of 4096 keys of 272 bytes, twice for row tiles that are not full) need a small part of what the cache holds.
