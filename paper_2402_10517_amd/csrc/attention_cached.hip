@@ -459,8 +459,9 @@ Plan plan_of(const ap_cache &c, const ap_cached &a)
     const int64_t group = a.heads / c.kv_heads, each = (a.tokens + a.sequences - 1) / a.sequences, longest = a.max_length > 0 ? a.max_length : 1;
     const auto items_of = [&](int64_t tile) { return a.q_starts ? a.tokens * group / tile + a.sequences : (each * group + tile - 1) / tile * a.sequences; };
     // 16 rows where that is enough for a sequence's queries, in ranges of one piece at most.  2^20 such ranges are more keys than the card's memory can
-    // hold: max_length is then far above the lengths, and the other kernel's ranges of any length keep the workgroups few.
-    p.rows = each * group <= 16 && longest / kPiece * items_of(16) * c.kv_heads <= 1 << 20 ? 1 : 2;
+    // hold: max_length is then far above the lengths, and the other kernel's ranges of any length keep the workgroups few.  So rows that are joined are
+    // fewer than 2^24, a workgroup each.
+    p.rows = each * group <= 16 && longest / kPiece * items_of(16) * c.kv_heads < 1 << 20 ? 1 : 2;
     p.items = items_of(16 * p.rows);
     // Ranges of keys.  Two workgroups per CU in all, of 256 keys at least; four where two would have more than 1024 keys each, as longer ranges leave
     // the card waiting for the last.  One, and no second launch, where every CU has a workgroup of up to 2048 keys.  us at 1 / 2 / 4 / 8 / 16 / 32 /

@@ -197,6 +197,16 @@ def test_sizes_that_no_launch_can_have_are_refused():
     assert prompt_size(heads=15, kv_heads=15, sequences=1 << 20) == 0 and prompt_size(tokens=(1 << 25) - (1 << 12), heads=63, kv_heads=9) == 0
 
 
+def test_rows_that_are_joined_have_a_workgroup_each():
+    # the join has a workgroup of 256 threads per row: fewer than 2^24 of them
+    size = ctypes.c_size_t(0)
+    for heads, kv_heads, sequences in ((16, 1, 1 << 20), (16, 1, (1 << 20) - 1), (32, 2, 1 << 19), (64, 8, 1 << 17), (64, 8, 1 << 18), (128, 8, 1 << 17)):
+        for length in (4000, 4096, 5000, 8192, 1 << 16):
+            a = cached(tokens=sequences, heads=heads, sequences=sequences, q_starts=None, table_width=1 << 10, max_length=length)
+            assert B.lib.ap_attention_cached_size(ctypes.byref(cache(kv_heads=kv_heads)), ctypes.byref(a), ctypes.byref(size)) == 0
+            assert size.value == 0 or sequences * heads < 1 << 24, (heads, sequences, length)
+
+
 def test_workspace_of_cached_attention_is_bounded():
     # Sums of ranges are kept where row tiles are too few for the card; many rows over long caches need no more.  Few rows (16 of a key head at most, 2080 bytes per
     # range of 4096 keys of 272 bytes, twice for row tiles that are not full) need a small part of what the cache holds.
