@@ -88,7 +88,8 @@ ap_status ap_cache_read(const ap_cache *c, const int64_t *slots, int64_t tokens,
  *   max_length host's bound of the lengths, up to table_width * page_tokens and 2^30: decides how the work is divided
  *   out        device, tokens x heads x head_dim, contiguous, 16-byte aligned; only the tokens of q_starts are written
  *   work       device, ap_attention_cached_size bytes, 16-byte aligned; may be NULL where that is 0
- * Scores, softmax and sums are binary32.  Long sequences are divided among workgroups and joined by a second launch.
+ * Scores, softmax and sums are binary32; the weights of the values, times their steps, have 16 bits.  Long sequences are divided among workgroups and
+ * joined by a second launch.
  */
 typedef struct {
     ap_heads q;

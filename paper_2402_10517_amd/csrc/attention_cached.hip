@@ -2,10 +2,13 @@
 //
 // A workgroup takes a tile of query rows (token, head of the group) of one sequence and key head and a range of its keys; a wave takes 32 keys at a
 // time:
-//   S^T = C Q^T with C the key codes, v_mfma_f32_16x16x32_f16: codes 0..15 enter as binary16 64 + code (the nibble set into the mantissa of 64: a shift
-//         and one v_and_or for two), exact, and s = scale (step (S - 64 sum q) + low sum q) takes the offset back in binary32;
-//   O^T = V^T P^T, v_mfma_f32_16x16x32_bf16: codes enter as bfloat16 128 + code, the weights as p * step in two bfloat16 parts (high + rest:
-//         16 bits of mantissa, and the range of binary32 for any step); what is the same for all channels of a row, sum p low - 128 sum p step, is one number.
+//   S^T = C Q^T with C the key codes, v_mfma_f32_16x16x32_f16: a code as the low bits of a binary16 number is code * 2^-24, exact (the instruction takes
+//         subnormal numbers as they are), and s = scale (step S + low sum q) in binary32, in the unit 2^-24 until it meets the scale;
+//   O^T = V^T P^T, v_mfma_f32_16x16x32_bf16: codes enter as bfloat16 16 + code, exact (the nibble set into the mantissa of 16), the weights as p * step in
+//         two bfloat16 parts (high + rest); what is the same for all channels of a row, sum p low - 16 sum p step, is one number.
+// Rounding: the two parts keep 16 bits of a weight and the range of binary32 for any step, 2^-17 of it, a 64th of the result's own rounding; a third part
+// would cost half as many products again.  The offset is the least that bfloat16 has room for: products of 16
+// to 31 steps where the code alone would be 0 to 15 (mean of 2048 values that cancel, steps of 1.5: off by 2.1e-6; with an offset of 128, 1.2e-5).
 // With keys as rows and queries as columns a lane holds scores of one query row throughout, the scores' registers are the weights' operand as they
 // stand (the order of the keys inside a product is free, and the cache's value layout follows it), and the statistics are one number per lane. The
 // running maximum moves only when a score exceeds it by 2^8: weights stay below 2^8 and the accumulators are seldom rescaled.
@@ -41,6 +44,7 @@ constexpr int kWaves = 4;
 constexpr int kTile = 32;                   // keys per wave and step
 constexpr int kStep = kTile * kWaves;       // keys per workgroup and step
 constexpr int kPiece = 64 / 2 * kStep;      // keys whose pages a wave holds, those of one 16-key half per lane: 32 steps
+constexpr float kCodeUnit = 0x1p-24f;       // a code as the low bits of a binary16 number; scores are in this unit
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.0f;
 // Exponents are fma(score, scale, -rounded product of maximum and scale): off by that rounding, up to 2^-11 of a weight at this size.  From there on the
@@ -129,20 +133,18 @@ __device__ __forceinline__ _Float16 step_of(uint32_t pair) { return __builtin_bi
 // A binary16 number times a binary32 one in one mixed-precision instruction
 __device__ __forceinline__ float times(_Float16 x, float y) { return __builtin_fmaf((float)x, y, 0.0f); }
 
-// A constant in a vector register: (w & it) | another constant is then one v_and_or_b32, which takes one scalar operand.  The instruction itself is
-// the compiler's, who knows how far it has to stay from the matrix instruction that reads its result.
+// A constant in a vector register: (w & a constant) | it is then one v_and_or_b32, which takes one scalar operand, and w & it needs no literal.  The
+// instructions themselves are the compiler's, who knows how far it has to stay from the matrix instruction that reads its result.
 __device__ __forceinline__ uint32_t in_vector(uint32_t x)
 {
     asm("" : "+v"(x));
     return x;
 }
 
-// 8 codes as binary16 64 + code, in the order 0 4 1 5 2 6 3 7
+// 8 codes as binary16 code * kCodeUnit, in the order 0 4 1 5 2 6 3 7
 __device__ __forceinline__ half8_t key_operand(uint32_t w, uint32_t mask)
 {
-    const uint32_t bits = 0x54005400u;
-    const uint4_t x = {(w << 4 & mask) | bits, (w & mask) | bits, (w >> 4 & mask) | bits, (w >> 8 & mask) | bits};
-    return __builtin_bit_cast(half8_t, x);
+    return __builtin_bit_cast(half8_t, uint4_t{w & mask, w >> 4 & mask, w >> 8 & mask, w >> 12 & mask});
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float x, float y)
@@ -151,13 +153,16 @@ __device__ __forceinline__ uint32_t pack_bf16(float x, float y)
     return __builtin_bit_cast(uint32_t, bf2_t{(__bf16)x, (__bf16)y});
 }
 
-// Channel n of four keys of both halves as bfloat16 128 + code
-template <int D> __device__ __forceinline__ bf8_t value_operand(const Half<D> (&h)[2], int n, uint32_t mask)
+// Channel n of four keys of both halves as bfloat16 16 + code
+template <int D> __device__ __forceinline__ bf8_t value_operand(const Half<D> (&h)[2], int n, uint32_t mask, uint32_t bits)
 {
     constexpr int kH = D / 64;
     uint4_t x;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = (h[i >> 1].v[(i & 1) * kH + n / 4] >> (4 * (n & 3)) & mask) | 0x43004300u;
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t w = h[i >> 1].v[(i & 1) * kH + n / 4];
+        x[i] = ((n & 3) == 0 ? w << 3 : w >> (4 * (n & 3) - 3)) & mask | bits;
+    }
     return __builtin_bit_cast(bf8_t, x);
 }
 
@@ -208,22 +213,21 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 6
         }
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
-        q_sum[r] = sum;
+        q_sum[r] = sum * kCodeUnit;
     }
 
     const float scale = fabsf(a.scale) * kLog2e;
-    float4_t o[NR][kN], offset[NR], start[NR]; // offset: 128 sum p step, on every channel; start: what takes the keys' 64 out
+    float4_t o[NR][kN], offset[NR]; // offset: 16 sum p step, on every channel
     float m[NR], l[NR], bias[NR];
     bool far[NR]; // scores whose product with the scale is too large to be rounded by itself
-    const uint32_t key_mask = in_vector(0x00f000f0u), value_mask = in_vector(0x000f000fu);
-    const uint32_t ones = 0x43004300u; // bfloat16 128
+    const uint32_t key_mask = in_vector(0x000f000fu), value_mask = 0x00780078u;
+    const uint32_t value_bits = in_vector(0x41804180u);
+    const uint32_t ones = 0x41804180u; // bfloat16 16
     const bf8_t all = __builtin_bit_cast(bf8_t, uint4_t{ones, ones, ones, ones});
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
         m[r] = -INFINITY;
         offset[r] = float4_t{0, 0, 0, 0};
-        const float x = -64.0f * q_sum[r];
-        start[r] = float4_t{x, x, x, x};
         l[r] = bias[r] = 0;
         far[r] = false;
 #pragma unroll
@@ -262,7 +266,7 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 6
                 for (int k = 0; k < kSteps; ++k) {
                     const half8_t x = key_operand(h[half].k[k], key_mask);
 #pragma unroll
-                    for (int r = 0; r < NR; ++r) s[r][half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, q[r][k], k == 0 ? start[r] : s[r][half], 0, 0, 0);
+                    for (int r = 0; r < NR; ++r) s[r][half] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, q[r][k], k == 0 ? float4_t{0, 0, 0, 0} : s[r][half], 0, 0, 0);
                 }
             }
             bf8_t high[NR], low[NR];
@@ -330,7 +334,7 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 6
             }
 #pragma unroll
             for (int i = 0; i < kN; ++i) {
-                const bf8_t v = value_operand<D>(h, i, value_mask);
+                const bf8_t v = value_operand<D>(h, i, value_mask, value_bits);
 #pragma unroll
                 for (int r = 0; r < NR; ++r) {
                     o[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, high[r], o[r][i], 0, 0, 0);
@@ -502,7 +506,7 @@ hipError_t launch_attention_cached(const ap_cache &c, const ap_cached &a, hipStr
     k.q_starts = a.q_starts, k.lengths = a.lengths, k.tables = a.tables;
     k.tokens = (int)a.tokens, k.heads = a.heads, k.sequences = a.sequences, k.max_length = (int)a.max_length;
     k.items = (int)p.items, k.splits = p.splits, k.chunk = p.chunk;
-    k.scale = scale_in_range(a.scale);
+    k.scale = scale_in_range(a.scale) / kCodeUnit;
     k.slack = kSlack / (fabsf(k.scale) * kLog2e);
     k.out = static_cast<_Float16 *>(a.out);
     k.part = static_cast<float *>(a.work);

@@ -51,11 +51,11 @@ inline CacheShape cache_shape(const ap_cache &c)
 }
 
 // The scale that a kernel works with.  One of 0 makes all weights equal, as 1e-30 does, and leaves scores of -inf (keys that are not seen) what they are;
-// from 1e38 on, where the product with log2 e would overflow, the greatest score has all the weight either way (others are 2^-48 below it at least).
+// from 1e30 on, short of where products with log2 e and 2^24 overflow, the greatest score has all the weight either way (others are 2^-48 below it at least).
 inline float scale_in_range(float scale)
 {
     const float size = scale < 0 ? -scale : scale;
-    return size < 1e-30f ? 1e-30f : size <= 1e38f ? scale : scale < 0 ? -1e38f : 1e38f;
+    return size < 1e-30f ? 1e-30f : size <= 1e30f ? scale : scale < 0 ? -1e30f : 1e30f;
 }
 
 } // namespace apgemv

@@ -510,6 +510,60 @@ def test_the_greatest_score_of_any_size_takes_all(B, kernel, D, size, scale):
     U.check(out, want, U.HALF_EPS16 * want.abs() + err + U.SUBNORMAL16)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_cached_scores_keep_their_bits(B, D):
+    # Two keys of close scores far below the sum of the magnitudes that enter them.  The products of queries and codes are whole multiples of one quantum,
+    # all sums of them below 2^24 quanta: binary32 holds them exactly, and only the score's own roundings are left.
+    S, g = 64, torch.Generator().manual_seed(D)
+    quantum = 1 / 8 if D == 128 else 1 / 16
+    q = torch.empty((S, 1, D))
+    q[..., :D // 2] = torch.randint(1024, 2048, (S, 1, D // 2), generator=g).float()
+    q[..., D // 2:] = torch.randint(1024, 2048, (S, 1, D // 2), generator=g).float() * quantum
+    q[..., 2] = 65 * quantum if D == 128 else 129 * quantum
+    codes = torch.randint(0, 16, (S, 2, 1, D), generator=g)
+    codes[:, 1] = codes[:, 0]
+    codes[..., 0], codes[..., 1] = 0, 15                        # least and greatest of the row
+    codes[:, 0, :, 2], codes[:, 1, :, 2] = 7, 8
+    k, v = codes / 8 - 1, torch.tensor([0.0, 1.0]).view(1, 2, 1, 1).expand(S, 2, 1, D)
+    sums = (q.double() * codes[:, 0].double()).sum(-1).amax().item()
+    assert 2.0 ** 22 < sums / quantum < 2.0 ** 24
+    cache = full_cache(B, S, 1, D, 16)
+    slots = torch.arange(S)[:, None] * 16 + torch.arange(2)
+    B.ap_cache_append(cache, k.half().flatten(0, 1).cuda(), v.half().flatten(0, 1).contiguous().cuda(), slots.flatten().cuda())
+    out = B.ap_attention_cached(cache, q.half().cuda(), torch.arange(S).int()[:, None].cuda(), torch.full((S,), 2, dtype=torch.int32).cuda(), scale=1.0)
+    s = torch.matmul(k.double()[:, :, 0], q.double()[:, 0, :, None])[..., 0]
+    want = torch.sigmoid(s[:, 1] - s[:, 0])
+    # low * sum and step * sum are exact too; a score is rounded once, at its own size, and the weight's slope is at most 1 / 4
+    off = 2 * U.EPS32 * s.abs().amax().item() / 4 + 16 * U.EPS32
+    U.check(out, want[:, None, None].expand(S, 1, D).cuda(), torch.full((S, 1, D), U.HALF_EPS16 + off, dtype=torch.float64).cuda())
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_cached_sums_of_values_keep_their_bits(B, D):
+    # Equal weights, and values that cancel in pairs: what is left is the rounding of the sums.  A wave of four has 512 of 2048 keys, 16 products of 32 in two
+    # parts, each a rounding or two of sums up to 512 * step * 31 in binary32 (codes with an offset of 16), of the values and of what takes the offset
+    # out again; the roundings are independent and uniform, of variance ulp^2 / 12 with ulp <= 2^-23 of the sum.
+    S, G, m = 32, 8, 2048
+    g = torch.Generator(device="cuda").manual_seed(D)
+    step = (torch.randint(512, 1024, (m // 2, G, 1), generator=g, device="cuda") * 2 + 1).float() / 1024       # 11 bits, 1 to 2
+    codes = torch.randint(1, 16, (m // 2, G, D), generator=g, device="cuda").float()
+    codes = torch.stack([codes, 16 - codes], dim=1).flatten(0, 1)
+    codes[..., 0], codes[..., 1] = 0, 15
+    mixed = torch.randperm(m, generator=g, device="cuda")       # a pair's keys are far apart
+    codes, step = codes[mixed], step.repeat_interleave(2, 0)[mixed]
+    v = ((codes - 8) * step).half()
+    got, low, scale = U.codes_of(v)
+    assert torch.equal(got, codes) and torch.equal(scale, step) and torch.equal(low, -8 * scale)
+    cache = full_cache(B, m // 64, G, D, 64)
+    B.ap_cache_append(cache, normal(1, m, G, D), v, torch.arange(m).cuda())
+    q = torch.zeros((S, G, D), dtype=torch.float16, device="cuda")
+    out = B.ap_attention_cached(cache, q, torch.arange(m // 64).int().expand(S, -1).contiguous().cuda(), torch.full((S,), m, dtype=torch.int32).cuda())
+    rms = out[..., 2:].double().square().mean().sqrt().item()
+    most = 512 * 31 * step.mean().item()
+    bound = (2 * 4 * (2 * 2 * 16 + 8) / 12) ** 0.5 * 2.0 ** -23 * most / m
+    assert rms <= bound
+
+
 # ------------------------------------------------------------------------------------------------ verification
 
 
