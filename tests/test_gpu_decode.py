@@ -178,6 +178,45 @@ def test_channels_beyond_the_rotation_stay(B, D, rot, inter, tokens):
     assert torch.equal(torch.isnan(k_got).all(-1), ~torch.isfinite(k_out).all(-1))
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("rot,inter", [(0, False), (1.0, False), (0.5, False), (1.0, True), (0.25, True)])
+@pytest.mark.parametrize("tokens,H,G,fused", [(255, 32, 4, True), (256, 5, 1, False), (257, 32, 8, True), (1003, 64, 8, True), (2000, 40, 40, False), (8201, 28, 4, True)])
+def test_append_many_tokens(B, D, rot, inter, tokens, H, G, fused):
+    # from 256 tokens on 16 adjacent ones are taken together, and from some thousand rows on several rows by the same lanes
+    page = 64
+    table, pages = U.page_table([tokens + 5], page, seed=tokens)
+    slots = U.slots_of(table, page, 0, 5, tokens + 5)
+    slots[-tokens // 9:] = -1
+    x = normal(tokens, tokens, H + 2 * G, D)
+    q, k, v = x[:, :H], x[:, H:H + G], x[:, H + G:]
+    if not fused:
+        q, k, v = q.contiguous(), k.transpose(0, 1).contiguous().transpose(0, 1), v.contiguous()
+    rotary = B.rotary_table(9000, int(rot * D)) if rot else None
+    positions = torch.randint(0, 9000, (tokens,), generator=torch.Generator().manual_seed(4)).cuda()
+    cache = full_cache(B, pages, G, D, page)
+    before = cache.buf.clone()
+    q_out, k_out = B.ap_cache_append(cache, k, v, slots.cuda(), q=q, positions=positions if rot else None, rotary=rotary, interleaved=inter)
+    for y, got in ((q, q_out), (k, k_out)):
+        want = U.rotate(y, rotary, positions, inter)
+        U.check(got, want, U.HALF_EPS16 * want.abs() + 4 * U.EPS32 * y.double().abs().amax(-1, keepdim=True) + U.SUBNORMAL16, "rotated")
+    k_got, v_got = B.ap_cache_read(cache, slots.cuda())
+    kept = (slots >= 0).cuda()[:, None, None]
+    for y, got in ((k_out, k_got), (v, v_got)):
+        codes, low, step = U.codes_of(y)
+        assert torch.equal(got, torch.where(kept, low + step * codes, torch.zeros_like(low)).half())
+    changed = int((cache.buf != before).sum())
+    assert int(kept.sum()) * G * (D + 8) // 2 <= changed <= int(kept.sum()) * G * (D + 8)
+    # one token at a time, which takes the other kernel: the same bits
+    few = torch.arange(tokens - tokens // 9 - 40, tokens - tokens // 9 + 3).cuda()
+    again = full_cache(B, pages, G, D, page)
+    q_few, k_few = B.ap_cache_append(again, k[few], v[few], slots.cuda()[few], q=q[few], positions=positions[few] if rot else None, rotary=rotary, interleaved=inter)
+    assert torch.equal(q_few, q_out[few]) and torch.equal(k_few, k_out[few])
+    assert all(torch.equal(a, b[few]) for a, b in zip(B.ap_cache_read(again, slots.cuda()[few]), (k_got, v_got)))
+    q_in, k_in = q.clone(), k.clone()
+    B.ap_cache_append(again, k_in, v, slots.cuda(), q=q_in, positions=positions if rot else None, rotary=rotary, interleaved=inter, q_out=q_in, k_out=k_in)
+    assert torch.equal(q_in, q_out) and torch.equal(k_in, k_out) and torch.equal(again.buf, cache.buf)
+
+
 # ------------------------------------------------------------------------------------------------ attention over the cache
 
 
@@ -459,6 +498,14 @@ def test_prompt_starts_that_make_no_sense(B):
     torch.cuda.synchronize()
     empty = q[:0]
     assert B.ap_attention_prompt(empty, k, v, torch.zeros(2, dtype=torch.int32).cuda(), torch.tensor([0, 40], dtype=torch.int32).cuda()).shape == (0, 2, 64)
+
+
+def test_prompt_rows_of_senseless_starts(B):
+    q, k, v = normal(1, 40, 2, 64), normal(2, 40, 2, 64), normal(3, 40, 2, 64)
+    out = torch.full_like(q, 7.0)
+    B.ap_attention_prompt(q, k, v, torch.tensor([0, 10, 5, 2 ** 31 - 1, -4], dtype=torch.int32).cuda(),
+                          torch.tensor([-9, 10, 2 ** 31 - 1, 3, 50], dtype=torch.int32).cuda(), out=out)
+    assert not out[:10].any() and (out[10:] == 7).all()
 
 
 # ------------------------------------------------------------------------------------------------ scores of any size
