@@ -360,7 +360,9 @@ class _Cache(ctypes.Structure):
 def ap_cache_size(pages, kv_heads, head_dim, page_tokens=64):
     """Bytes of a 4-bit cache of `pages` pages of page_tokens tokens."""
     out = ctypes.c_size_t(0)
-    _check(lib.ap_cache_size(ctypes.byref(_Cache(None, pages, page_tokens, kv_heads, head_dim)), ctypes.byref(out)), "ap_cache_size")
+    shape = [x if -2 ** 31 <= x < 2 ** 31 else -1 for x in (page_tokens, kv_heads, head_dim)]          # ctypes would drop the bits above
+    cache = _Cache(None, pages if -2 ** 63 <= pages < 2 ** 63 else -1, *shape)
+    _check(lib.ap_cache_size(ctypes.byref(cache), ctypes.byref(out)), "ap_cache_size")
     return out.value
 
 

@@ -1,5 +1,6 @@
 // The Python binding's calls of the decoder operators as native functions: argument checks, output and workspace tensors, the current stream and
 // the call of the C-ABI entry point (include/apdecode.h).  They hold no logic of the library.
+#include <climits>
 #include <cmath>
 
 #include <ATen/hip/HIPContext.h>
@@ -35,9 +36,9 @@ struct Call {
         ap_cache c;
         c.data = b.data_ptr();
         c.pages = integer(PyTuple_GET_ITEM(shape, 0));
-        c.page_tokens = (int)integer(PyTuple_GET_ITEM(shape, 1));
-        c.kv_heads = (int)integer(PyTuple_GET_ITEM(shape, 2));
-        c.head_dim = (int)integer(PyTuple_GET_ITEM(shape, 3));
+        c.page_tokens = small(PyTuple_GET_ITEM(shape, 1));
+        c.kv_heads = small(PyTuple_GET_ITEM(shape, 2));
+        c.head_dim = small(PyTuple_GET_ITEM(shape, 3));
         size_t bytes = 0;
         if (ap_cache_size(&c, &bytes) == AP_OK && (size_t)room(b) < bytes) refuse("the cache", "holds fewer bytes than its pages");
         return c;
@@ -75,6 +76,13 @@ struct Call {
         const long long v = PyLong_AsLongLong(o);
         if (v == -1 && PyErr_Occurred()) throw Refused{};
         return v;
+    }
+
+    // -1, which no size may be, for what an int cannot hold
+    int small(PyObject *o)
+    {
+        const int64_t v = integer(o);
+        return v < INT_MIN || v > INT_MAX ? -1 : (int)v;
     }
 
     // (tokens, heads, head_dim) binary16 rows with contiguous heads; tokens or heads < 0: any

@@ -102,6 +102,13 @@ def test_cache_size():
     assert B.lib.ap_cache_size(None, None) == INVALID and B.lib.ap_cache_size(ctypes.byref(cache()), None) == INVALID
 
 
+@pytest.mark.parametrize("bad", [dict(page_tokens=2 ** 32 + 64), dict(kv_heads=2 ** 32 + 2), dict(head_dim=2 ** 32 + 64), dict(pages=2 ** 64 + 4), dict(page_tokens=-2 ** 32 + 16)])
+def test_cache_sizes_are_not_taken_modulo(bad):
+    with pytest.raises(B.ApError) as e:
+        B.ap_cache_size(**dict(dict(pages=4, kv_heads=2, head_dim=64, page_tokens=16), **bad))
+    assert e.value.status == SHAPE
+
+
 def of(function, *structs):
     return function(*[None if s is None else ctypes.byref(s) for s in structs], None)
 
