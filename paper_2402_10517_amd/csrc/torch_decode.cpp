@@ -207,7 +207,8 @@ PyObject *cache_append(PyObject *, PyObject *const *args, Py_ssize_t n)
             if (!a.rotary) refuse("rotary", "must have rows and columns");
             if (args[6] == Py_None) refuse("positions", "are needed with rotary");
             a.positions = static_cast<const int64_t *>(c.array(args[6], "positions", at::kLong, a.tokens));
-            a.interleaved = PyObject_IsTrue(args[8]) == 1;
+            a.interleaved = PyObject_IsTrue(args[8]);
+            if (a.interleaved < 0) throw Refused{};
         }
         const ap_status status = without_gil([&] { return ap_cache_append(&cache, &a, c.stream.address); });
         return status == AP_OK ? pair(q_out, k_out) : PyLong_FromLong(status);

@@ -217,6 +217,13 @@ def test_append_many_tokens(B, D, rot, inter, tokens, H, G, fused):
     assert torch.equal(q_in, q_out) and torch.equal(k_in, k_out) and torch.equal(again.buf, cache.buf)
 
 
+def test_interleaved_without_a_truth_value(B):
+    k = normal(1, 2, 1, 64)
+    cache = full_cache(B, 1, 1, 64, 16)
+    with pytest.raises(ValueError):                             # numpy's own error, and not one of a call that has succeeded
+        B.ap_cache_append(cache, k, k, torch.arange(2).cuda(), positions=torch.arange(2).cuda(), rotary=B.rotary_table(4, 64), interleaved=np.zeros(2))
+
+
 # ------------------------------------------------------------------------------------------------ attention over the cache
 
 
