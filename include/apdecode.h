@@ -33,8 +33,13 @@ typedef struct {
  * A paged cache.  A page holds page_tokens tokens of every key head, and a token's place is its slot: page * page_tokens + place in
  * the page.  Keys and values are held as 16 evenly spaced values per token and head: low + scale * code with low the least of the
  * head_dim values, scale = (greatest - least) / 15 rounded to binary16, and code the nearest of 0..15 (ties to even).  Of a row
- * with an infinity or a NaN every value reads back as NaN.  head_dim / 2 + 4 bytes per token, head and side. Page and head are
- * contiguous: key codes of the page's tokens, value codes, then (low, scale) pairs of the keys and of the values.
+ * with an infinity or a NaN every value reads back as NaN.  head_dim / 2 + 4 bytes per token, head and side.
+ *
+ * What 4 bits cost: on normally distributed rows (1000 keys) the result of attention is 13 % (head_dim 64) to 14 % (128) of its norm away from that over
+ * the unrounded keys and values, 9 to 10 % each from keys and values.  One step serves a whole row: where one channel of the keys is 8
+ * times the others it is 34 to 38 %.  Whether a model bears that is for its user to measure; there is no wider format.
+ *
+ * Page and head are contiguous: key codes of the page's tokens, value codes, then (low, scale) pairs of the keys and of the values.
  */
 typedef struct {
     void *data;    /* device, ap_cache_size bytes, 256-byte aligned, caller-owned; needs no initialisation */

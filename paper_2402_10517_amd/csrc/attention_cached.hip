@@ -14,9 +14,9 @@
 // running maximum moves only when a score exceeds it by 2^8: weights stay below 2^8 and the accumulators are seldom rescaled.
 //
 // A key of one head is D + 8 bytes and 4 (heads / kv_heads) D operations: HBM bounds the work, and a wave has its next 32 keys' loads in flight while
-// it works. Long sequences reach it: two of 131072 keys and 8 key heads of 128 take 51 us (285 MB, 5.6 TB/s; ap_probe_read reads as much in 44) and
+// it works. Long sequences reach it: two of 131072 keys and 8 key heads of 128 take 51 us (285 MB, 5.5 TB/s; ap_probe_read reads as much in 44) and
 // the join 5. Short ones are bound by what happens once per workgroup (start, length, page and first key one after the other, the join of the waves,
-// the second launch: some 10 us in all), and by the vector instructions per 32 keys, about 240: 4-bit codes to operands 112, softmax and weights 100.
+// the second launch: some 10 us in all), and by the vector instructions per 32 keys, about 250: 4-bit codes to operands 120, softmax and weights 100.
 // Codes staged through LDS two to four tiles ahead, or two sets of registers without moves, came out the same within 5 % on all of them.
 #include "decode_device.h"
 

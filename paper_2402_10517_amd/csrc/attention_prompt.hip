@@ -9,10 +9,14 @@
 // chunks exchanged (the lanes ask memory for the chunk that belongs at their place) so that the reads of both operands meet every bank once.
 //
 // 4 D operations and one exponential per pair of query and key: bound by the matrix cores and the vector instructions beside them. 8192 tokens of 64
-// heads and 8 key heads of 128 take 1.08 to 1.13 ms, 970 to 1016 TFLOP/s, where a library product of 8192^3 reaches 1177: the matrix cores are busy
-// for 55 % of the time and the vector units for 38 %, and the two waves of a SIMD overlap them but little. Two workgroups per CU (212 registers, 64
-// KB of LDS); no bank conflicts. Shorter prompts lose to the tiles on the diagonal and to the start of a workgroup: six of up to 2047 tokens and 40
-// heads run at 690.
+// heads and 8 key heads of 128 take 1.07 to 1.20 ms from card to card, 920 to 1020 TFLOP/s, where a library product of 8192^3 reaches 1177: the matrix
+// cores are busy for 54 % of the time and the vector units for 38 %, and the two waves of a SIMD overlap them but little. Two workgroups per CU (212
+// registers, 64 KB of LDS); no bank conflicts. Shorter prompts lose to the tiles on the diagonal and to the start of a workgroup: six of up to 2047 tokens
+// and 40 heads run at 655 to 670.
+//
+// The weights are rounded to binary16, and their sum is of the rounded ones: errors of up to 2^-11 each add 1.7e-4 of the result to the 2.0e-4 that its own
+// rounding is off by (2.65e-4 together, 8192 tokens).  With a second part of the weights, a second product per value, nothing of that is left, and the
+// same tokens take 1.57 ms instead of 1.13, the six prompts 235 us instead of 184, pieces at head_dim 64 63.5 instead of 44.6.
 #include "decode_device.h"
 
 namespace apgemv {

@@ -1,7 +1,7 @@
 // Rotation of q and k, append of k and v to the 4-bit cache, and its values read back.
 //
 // Bound by HBM: rows in, rotated rows and 4-bit codes out, each once. 16 lanes hold a row of head_dim values, so that the least and the greatest of
-// it are four exchanges away. 8.3k tokens of 64 + 2 x 8 heads take 67 us and their read-back 10 (381 MB in all, 4.8 TB/s; a copy reaches 5.15); a
+// it are four exchanges away. 8347 tokens of 64 + 2 x 8 heads take 68 us and their read-back 10 (381 MB in all, 4.8 TB/s; a copy reaches 5.15); a
 // single token 4.9 and 2.1, the time of a launch and of three dependent loads.
 #include "decode_device.h"
 
@@ -136,7 +136,7 @@ template <int V> __device__ __forceinline__ uint32_t encode(const float (&x)[V],
     uint32_t codes = 0;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        // the product is within 3e-6 of the quotient (at most 20): only near the middle between two codes does it take the division
+        // the product is within 3e-6 of the quotient (at most 22, where a step of one subnormal unit rounded down): only near the middle between two codes does it take the division
         const float y = (x[i] - least) * inverse;
         float r = rintf(y);
         if (fabsf(fabsf(y - r) - 0.5f) < 1e-5f) r = rintf((x[i] - least) / step);
@@ -293,7 +293,7 @@ hipError_t launch_cache_append(const ap_cache &c, const ap_append &a, hipStream_
     k.rot_dim = a.rotary ? a.rot_dim : 0, k.interleaved = a.interleaved;
     k.page_mask = c.page_tokens - 1;
     // With many tokens a workgroup takes 16 adjacent ones.  A group of lanes keeps its cosines and sines for up to 8 rows, all in flight at once by
-    // fours, where that leaves the card two workgroups per CU.  8.5k tokens of 64 + 2 x 8 heads, us with the values read back, at 1 / 2 / 4 / 8 / 10
+    // fours, where that leaves the card two workgroups per CU.  8347 tokens of 64 + 2 x 8 heads, us with the values read back, at 1 / 2 / 4 / 8 / 10
     // / 16 / 40 rows: 113 / 98 / 82 / 80 / 99 / 90 / 108 (381 MB, 4.8 TB/s at 8).
     const bool together = a.tokens >= 256;
     const int64_t step = together ? 1 : kRowsPerGroup, rows = k.heads + 2 * c.kv_heads, blocks = together ? (a.tokens + kRowsPerGroup - 1) / kRowsPerGroup : a.tokens;

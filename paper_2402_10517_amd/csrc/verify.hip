@@ -2,8 +2,8 @@
 //
 // The token is the argmax of w / noise with lowest index first: no sum is taken, so any division of the vocabulary gives the same token, bit for bit.
 // Bound by HBM: one row of target and draft probabilities and the noise per sequence.  Few sequences leave most of the card idle, so a vocabulary is
-// divided among workgroups (2048 tokens at least each) and joined by a second launch, small ones aside. 64 sequences over 131071 binary16 probabilities take 16 us (67
-// MB, 4.1 TB/s), 4 drafts over 32000 tokens 8.5, two launches.
+// divided among workgroups (2048 tokens at least each) and joined by a second launch, small ones aside. 64 sequences over 131071 binary16 probabilities take 16.3 to
+// 17.3 us (67 MB, 3.9 to 4.1 TB/s), 4 drafts over 32000 tokens 8.1 to 9.1, two launches.
 #include "decode_device.h"
 
 namespace apgemv {
