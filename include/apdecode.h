@@ -115,8 +115,8 @@ ap_status ap_attention_cached(const ap_cache *c, const ap_cached *a, void *strea
  * k_starts[s + 1] - 1 (device, sequences + 1 each, not descending; a sequence whose two starts descend or leave the rows has none);
  * its last query sees its last key.  Query i of n sees the first m - n + 1 + i of m keys; one that sees none gets zeros, as does
  * one whose scores are all -inf.  What a query does not see does not reach it, NaN and infinities included.
- *   q; k, v    tokens rows of heads heads (tokens * heads < 2^31 - 256, tokens * heads / 128 + sequences * kv_heads < 2^24); keys rows of kv_heads heads, their token strides in 0 ..
- *              2^24 (AP_ERR_SHAPE otherwise)
+ *   q; k, v    tokens rows of heads heads (tokens * heads < 2^31 - 256, tokens * heads / 128 + sequences * kv_heads < 2^24); keys (up to
+ *              2^30) rows of kv_heads heads, their token strides in 0 .. 2^24 (AP_ERR_SHAPE otherwise)
  *   out        device, tokens x heads x head_dim, contiguous, 16-byte aligned; only the tokens of q_starts are written
  *   work       device, ap_attention_prompt_size bytes, 16-byte aligned; may be NULL where that is 0
  * Scores, softmax and sums are binary32; the weights of the values are rounded to binary16.  Where the rows are too few for the

@@ -20,6 +20,7 @@ bool rows_ok(const ap_heads &r)
 bool head_dim_ok(int d) { return d == 64 || d == 128; }
 
 constexpr int64_t kMaxTokens = 0x7fffff00; // tokens of a call: the starts of sequences are 32-bit
+constexpr int64_t kMaxKeys = (int64_t)1 << 30; // of a sequence: the ends of ranges behind its last key are 32-bit too
 
 ap_status check_cache_shape(const ap_cache *c)
 {
@@ -52,7 +53,7 @@ ap_status check_cached(const ap_cache *c, const ap_cached *a)
     if ((a->tokens > 0 && a->sequences < 1) || a->tokens * a->heads > kMaxTokens) return AP_ERR_SHAPE;
     if (!groups_ok(a->tokens * a->heads, 16, a->sequences, c->kv_heads)) return AP_ERR_SHAPE;
     if (!a->q_starts && a->sequences > 0 && a->tokens % a->sequences) return AP_ERR_SHAPE;
-    if (a->table_width < 0 || a->table_width >= (int64_t)1 << 31 || a->max_length < 0 || a->max_length > 1 << 30 ||
+    if (a->table_width < 0 || a->table_width >= (int64_t)1 << 31 || a->max_length < 0 || a->max_length > kMaxKeys ||
         a->max_length > a->table_width * c->page_tokens)
         return AP_ERR_SHAPE;
     return AP_OK;
@@ -128,7 +129,7 @@ static ap_status check_prompt(const ap_prompt *a)
     if (!head_dim_ok(a->head_dim)) return AP_ERR_SHAPE;
     const ap_status s = check_heads(a->heads, a->kv_heads);
     if (s != AP_OK) return s;
-    if (a->tokens < 0 || a->tokens > kMaxTokens || a->keys < 0 || a->keys > kMaxTokens || a->sequences < 0 || a->sequences > (1 << 20) ||
+    if (a->tokens < 0 || a->tokens > kMaxTokens || a->keys < 0 || a->keys > kMaxKeys || a->sequences < 0 || a->sequences > (1 << 20) ||
         (a->tokens > 0 && a->sequences < 1) || a->tokens * a->heads > kMaxTokens || !groups_ok(a->tokens * a->heads, 128, a->sequences, a->kv_heads))
         return AP_ERR_SHAPE;
     // a tile of 64 rows of k or v is addressed by 32 bits from its first

@@ -204,6 +204,14 @@ def test_sizes_that_no_launch_can_have_are_refused():
     assert prompt_size(heads=15, kv_heads=15, sequences=1 << 20) == 0 and prompt_size(tokens=(1 << 25) - (1 << 12), heads=63, kv_heads=9) == 0
 
 
+def test_prompt_keys_whose_ranges_would_end_beyond_32_bits_are_refused():
+    # the last of 64 ranges of 2^31 - 256 keys would end at 2^31: with token strides of 0 they need no memory
+    size = ctypes.c_size_t(7)
+    for keys, status in ((1 << 30, 0), ((1 << 30) + 1, SHAPE), (0x7fffff00, SHAPE)):
+        a = prompt(keys=keys, k=rows(token_stride=0), v=rows(token_stride=0))
+        assert B.lib.ap_attention_prompt_size(ctypes.byref(a), ctypes.byref(size)) == status
+
+
 def test_rows_that_are_joined_have_a_workgroup_each():
     # the join has a workgroup of 256 threads per row: fewer than 2^24 of them
     size = ctypes.c_size_t(0)
