@@ -1,7 +1,8 @@
 /*
  * The operators of a decoder step beside the any-precision products of apgemv.h, for AMD MI355X (gfx950): rotation of q and k and
  * the append of k and v to a paged cache held in 4 bits, attention of new tokens over that cache, causal attention over packed
- * prompts, and the verification of tokens that a model at fewer bits has drafted.
+ * prompts, and the verification of tokens that a model at fewer bits has drafted; and what a step needs around them: attention of
+ * sequences that share a prefix, the norms around a block, sampling from logits.
  *
  * Conventions are those of apgemv.h: activations are binary16, every function returns an ap_status and neither throws, aborts nor
  * prints, arguments are checked before the first HIP call, work is enqueued on `stream` (a hipStream_t; NULL = the default stream),
@@ -165,6 +166,90 @@ typedef struct {
 } ap_verification;
 ap_status ap_verify_size(const ap_verification *a, size_t *bytes);
 ap_status ap_verify(const ap_verification *a, void *stream);
+
+/*
+ * Attention of new tokens over the cache where sequences share prefixes: out[i] = sum_j softmax_j(scale * q[i] . k[j]) v[j] over the keys of the
+ * sequence's prefix and its own.  A prefix is read once for all rows of its sequences.
+ *   own        as for ap_attention_cached: q, the sequences' own keys (lengths and tables count from the first one behind the prefix), max_length
+ *              the bound of their number, out, work (ap_attention_shared_size bytes).  tables may be NULL where max_length is 0
+ *   prefixes   up to 2^20, (tokens * heads / 8 + (sequences + prefixes) * kv_heads) < 2^24, tokens * heads < 2^24
+ *   prefix_starts device, prefixes + 1: prefix p belongs to the sequences prefix_starts[p] .. prefix_starts[p + 1] - 1; not descending (a prefix
+ *              whose two starts descend or leave 0 .. sequences has no sequences, nor has one whose sequences' tokens do in q_starts).  Sequences
+ *              before the first and behind the last have no prefix.  NULL: sequences / prefixes each
+ *   prefix_lengths device, prefixes: their keys, all of which every token of their sequences sees; above max_prefix taken as max_prefix
+ *   prefix_tables  device, prefixes x prefix_width page numbers; may be NULL where max_prefix is 0
+ *   max_prefix host's bound of prefix_lengths, up to prefix_width * page_tokens and 2^30: decides how the work is divided
+ * A token that sees no key at all gets zeros.  A prefix need not fill its last page; pages may be shared in any way.  Scores, softmax and sums are
+ * binary32.  Where a prefix has more than 32 rows per key head, its values enter the products as ap_cache_read gives them and its weights rounded
+ * to binary16; else, and for the sequences' own keys, as in ap_attention_cached.
+ */
+typedef struct {
+    ap_cached own;
+    int prefixes;
+    const int32_t *prefix_starts, *prefix_lengths, *prefix_tables;
+    int64_t prefix_width, max_prefix;
+} ap_shared;
+ap_status ap_attention_shared_size(const ap_cache *c, const ap_shared *a, size_t *bytes);
+ap_status ap_attention_shared(const ap_cache *c, const ap_shared *a, void *stream);
+
+/*
+ * The end of one block of a decoder layer and the start of the next, in one launch:
+ *   y = post ? norm(x) * post_weight + post_bias : x,   r = residual + scale * gate * y rounded to the residual's type,   out = norm(r) * weight + bias
+ * with norm(a) = a / sqrt(mean(a^2) + eps), or (centred) (a - mean(a)) / sqrt(mean((a - mean(a))^2) + eps).
+ *   tokens, columns  up to 2^31 - 256 rows of up to 32768 values, which are contiguous; rows may have any stride (in elements; 0 = the same row for all, of
+ *              what is read)
+ *   x          binary16, the block's output; NULL = none (r = residual; gate, post and scale are not looked at)
+ *   residual   binary32, or binary16 where half != 0; NULL = none (r = scale * gate * y); x and residual are not both NULL
+ *   gate       binary16; NULL = 1.  A gate per channel has stride 0
+ *   weight, bias, post_weight, post_bias  binary16, columns values; NULL = 1 and 0
+ *   residual_out  r, of the residual's type; may be the residual itself (same address and stride); NULL = not wanted
+ *   out        binary16; may be x itself (same address and stride); NULL = not wanted
+ * Sums over a row are binary32 for up to 32 values and binary64 beyond; each value is computed in binary32 and rounded once, the norm of r starts from r as it is rounded.
+ */
+typedef struct {
+    const void *data; /* device, aligned to its type */
+    int64_t stride;   /* elements from row to row, |stride| < 2^40 */
+} ap_rows;
+typedef struct {
+    ap_rows x, residual, gate, residual_out, out;
+    int64_t tokens, columns;
+    int half, post, centred;
+    const void *weight, *bias, *post_weight, *post_bias;
+    float scale, eps;
+} ap_normed;
+ap_status ap_norm(const ap_normed *a, void *stream);
+
+/*
+ * Tokens from logits and random numbers.  With t = temperature[r], the weight of token v of row r is exp((x[v] - max x) / t); tokens are ordered by
+ * descending logit, equal ones by ascending number.  Of the first top_k of them (all where top_k[r] < 1), the shortest beginning whose weights reach
+ * top_p of those' sum (all where top_p[r] is not below 1), of these the ones whose weight is at least min_p (where min_p[r] is above 0; the first one in
+ * any case) are kept.  probabilities = weight / sum of the kept, 0 for the others, and tokens[r] is the first token, by number, at which the kept weights up to it pass
+ * uniform[r] * their sum (the last kept one where none does: a uniform number not below 1, or NaN).
+ *   t not above 0 (or NaN): the first token alone.  A logit that is NaN counts as -inf, which is never kept; where one is +inf only such are.  A row
+ *   that keeps nothing has the token -1 and probabilities of 0.
+ *   logits     device, rows x vocabulary binary32, or binary16 where half != 0; rows up to 2^21, vocabulary up to 2^20, contiguous in a row, stride elements
+ *              from row to row
+ *   uniform, temperature, top_p, min_p  device, rows binary32;  top_k  device, rows int32;  each but uniform may be NULL: 1, 1, 0 and 0
+ *   tokens     device, rows
+ *   probabilities device, rows x vocabulary contiguous binary32, or binary16 where half_probabilities != 0; NULL = not wanted
+ *   work       device, ap_sample_size bytes, 16-byte aligned; may be NULL where that is 0
+ * Weights are binary64 and their sums 64-bit fixed point, exact in any order: what is kept and which token is drawn does not depend on how the work is
+ * divided.  A weight below 2^-42 of the greatest (2^-62 of it times the vocabulary) may count as nothing in the sums.
+ */
+typedef struct {
+    const void *logits;
+    int64_t stride;
+    int half, half_probabilities;
+    int64_t rows, vocabulary;
+    const float *uniform, *temperature, *top_p, *min_p;
+    const int32_t *top_k;
+    int64_t *tokens;
+    void *probabilities;
+    void *work;
+    size_t work_bytes;
+} ap_sampling;
+ap_status ap_sample_size(const ap_sampling *a, size_t *bytes);
+ap_status ap_sample(const ap_sampling *a, void *stream);
 
 #ifdef __cplusplus
 }

@@ -28,7 +28,8 @@ EXPORTS = ["ap_packed_size", "ap_pack_host", "ap_unpack_host", "ap_blob_lut_entr
            "ap_free", "ap_strerror"]
 
 DECODE_EXPORTS = ["ap_cache_size", "ap_cache_append", "ap_cache_read", "ap_attention_cached_size", "ap_attention_cached",
-                  "ap_attention_prompt_size", "ap_attention_prompt", "ap_verify_size", "ap_verify"]   # include/apdecode.h
+                  "ap_attention_prompt_size", "ap_attention_prompt", "ap_verify_size", "ap_verify", "ap_attention_shared_size", "ap_attention_shared",
+                  "ap_norm", "ap_sample_size", "ap_sample"]   # include/apdecode.h
 
 
 OPTIONS = {"waves": 0, "row_groups": 1, "mfma_min_batch": 2, "variant": 3}
@@ -83,6 +84,11 @@ def _load():
     L.ap_attention_prompt.argtypes = [vp, vp]
     L.ap_verify_size.argtypes = [vp, psz]
     L.ap_verify.argtypes = [vp, vp]
+    L.ap_attention_shared_size.argtypes = [vp, vp, psz]
+    L.ap_attention_shared.argtypes = [vp, vp, vp]
+    L.ap_norm.argtypes = [vp, vp]
+    L.ap_sample_size.argtypes = [vp, psz]
+    L.ap_sample.argtypes = [vp, vp]
     L.ap_strerror.argtypes = [ci]
     L.ap_strerror.restype = ctypes.c_char_p
     for name in DECODE_EXPORTS:
@@ -434,4 +440,51 @@ def ap_verify(target, draft, drafted, uniform, noise, counts=None, work=None, st
     r = _torch_call.verify(target, draft, drafted, uniform, noise, counts, work, None if stream is None else stream.cuda_stream)
     if type(r) is int:
         raise ApError(abs(r), "ap_verify" if r > 0 else "ap_verify_size")
+    return r
+
+
+def ap_attention_shared(cache, q, prefix_tables, prefix_lengths, tables, lengths, prefix_starts=None, q_starts=None, scale=None, max_prefix=None,
+                        max_length=None, out=None, work=None, stream=None):
+    """Attention of new tokens q (tokens, heads, head_dim) over the cache where sequences share prefixes: a token sees its sequence's prefix and its own keys.
+
+    prefix_tables: int32 (prefixes, pages), prefix_lengths: int32 (prefixes,), prefix_starts: int32 (prefixes + 1,): prefix p belongs to the sequences
+    prefix_starts[p] .. prefix_starts[p + 1] - 1, None = sequences / prefixes each; max_prefix: a bound of prefix_lengths, None = what the tables hold.  tables,
+    lengths and max_length are of the sequences' own keys, behind the prefix; they, q_starts, scale, out, work and `stream` as in ap_attention_cached."""
+    r = _torch_call.attention_shared(cache.buf, cache.shape, q, prefix_tables, prefix_lengths, tables, lengths, prefix_starts, q_starts, scale, max_prefix,
+                                     max_length, out, work, None if stream is None else stream.cuda_stream)
+    if type(r) is int:
+        raise ApError(abs(r), "ap_attention_shared" if r > 0 else "ap_attention_shared_size")
+    return r
+
+
+def ap_norm(x, residual=None, weight=None, bias=None, post_weight=None, post_bias=None, post=None, gate=None, scale=1.0, eps=1e-6, centred=False, normed=True,
+            out=None, residual_out=None, stream=None):
+    """r = residual + scale * gate * post_norm(x) and norm(r) of (tokens, columns); returns (norm(r) float16, r).
+
+    x: float16, a block's output, None = none; residual: float32 or float16, None = none; weight, bias, post_weight, post_bias: float16 (columns,), None = 1 and
+    0; post: whether x is normed, None = where post_weight or post_bias is given; gate: float16 (tokens, columns), or (1, columns) for all; centred: means are
+    taken away; normed: False = norm(r) is not wanted (None).  r is allocated where x and a residual are given, else written only to a given residual_out, and
+    None otherwise; residual_out may be residual, out may be x.  `stream` as in ap_gemv."""
+    if post is None:
+        post = post_weight is not None or post_bias is not None
+    r = _torch_call.norm(x, residual, weight, bias, post_weight, post_bias, post, gate, scale, eps, centred, normed, out, residual_out,
+                         None if stream is None else stream.cuda_stream)
+    if type(r) is int:
+        raise ApError(r, "ap_norm")
+    return r
+
+
+def ap_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None, probabilities=None, work=None, stream=None):
+    """One token per row of logits (rows, vocabulary), float32 or float16, by uniform numbers in [0, 1); returns (tokens int64 (rows,), probabilities).
+
+    temperature, top_p, min_p: float32 (rows,), top_k: int32 (rows,), None = 1, 1, 0 and 0, which keep every token; a temperature of 0 takes the greatest.
+    probabilities: torch.float32 or torch.float16 = those that the token was drawn from, 0 for tokens that were not kept (what ap_verify takes); a
+    tensor (rows, vocabulary) = written there; None = not wanted.  `stream` and work as in ap_attention_cached."""
+    if probabilities is None or isinstance(probabilities, torch.dtype):
+        kinds = {None: 0, torch.float32: 1, torch.float16: 2}
+        assert probabilities in kinds, "probabilities are float32 or float16"
+        probabilities = kinds[probabilities]
+    r = _torch_call.sample(logits, uniform, temperature, top_k, top_p, min_p, probabilities, work, None if stream is None else stream.cuda_stream)
+    if type(r) is int:
+        raise ApError(abs(r), "ap_sample" if r > 0 else "ap_sample_size")
     return r

@@ -10,7 +10,8 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libapgemv.so")
 TORCH_CALL = os.path.join(HERE, "_torch_call.so")   # Python module; host code only
 SOURCES = ["gemv_alu.hip", "gemv_quad.hip", "gemv_matrix.hip", "gemv_tile.hip", "dequant.hip", "gemm_fused.hip", "gemm_static.hip", "dispatch.cpp", "api.cpp", "pack.cpp",
-           "dense_gemm.cpp", "quantize.cpp", "cache.hip", "attention_cached.hip", "attention_prompt.hip", "verify.hip", "decode_api.cpp"]
+           "dense_gemm.cpp", "quantize.cpp", "cache.hip", "attention_cached.hip", "attention_prompt.hip", "verify.hip", "decode_api.cpp",
+           "attention_shared.hip", "norm.hip", "sample.hip"]
 TORCH_SOURCES = ["torch_call.cpp", "torch_decode.cpp"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -193,3 +193,96 @@ extern "C" ap_status ap_verify(const ap_verification *a, void *stream)
     if (a->work_bytes < need) return AP_ERR_BUFFER_TOO_SMALL;
     return done(launch_verify(*a, static_cast<hipStream_t>(stream)));
 }
+
+static ap_status check_shared(const ap_cache *c, const ap_shared *a)
+{
+    if (!a) return c ? AP_ERR_INVALID_ARG : check_cache_shape(c);
+    const ap_status s = check_cached(c, &a->own);
+    if (s != AP_OK) return s;
+    if (a->own.tokens * a->own.heads >= (int64_t)1 << 24) return AP_ERR_SHAPE; // a workgroup of 256 threads joins the ranges of a row
+    if (a->prefixes < 0 || a->prefixes > (1 << 20)) return AP_ERR_SHAPE;
+    if (!a->prefix_starts && a->prefixes > 0 && a->own.sequences % a->prefixes) return AP_ERR_SHAPE;
+    if (!groups_ok(a->own.tokens * a->own.heads, 8, (int64_t)a->own.sequences + a->prefixes, c->kv_heads)) return AP_ERR_SHAPE;
+    if (a->prefix_width < 0 || a->prefix_width >= (int64_t)1 << 31 || a->max_prefix < 0 || a->max_prefix > kMaxKeys ||
+        a->max_prefix > a->prefix_width * c->page_tokens)
+        return AP_ERR_SHAPE;
+    return AP_OK;
+}
+
+extern "C" ap_status ap_attention_shared_size(const ap_cache *c, const ap_shared *a, size_t *bytes)
+{
+    const ap_status s = check_shared(c, a);
+    if (s != AP_OK) return s;
+    if (!bytes) return AP_ERR_INVALID_ARG;
+    *bytes = a->own.tokens == 0 ? 0 : attention_shared_work(*c, *a);
+    return AP_OK;
+}
+
+extern "C" ap_status ap_attention_shared(const ap_cache *c, const ap_shared *a, void *stream)
+{
+    ap_status s = check_shared(c, a);
+    if (s != AP_OK) return s;
+    s = check_cache(c);
+    if (s != AP_OK) return s;
+    const ap_cached &o = a->own;
+    if (o.tokens == 0) return AP_OK;
+    if (!rows_ok(o.q) || !o.lengths || !o.out || !aligned(o.out, 16) || !aligned(o.lengths, 4) || !aligned(o.q_starts, 4) || !aligned(o.tables, 4) ||
+        (!o.tables && o.max_length > 0) || !std::isfinite(o.scale))
+        return AP_ERR_INVALID_ARG;
+    if (!aligned(a->prefix_starts, 4) || !aligned(a->prefix_lengths, 4) || !aligned(a->prefix_tables, 4) || (a->prefixes > 0 && !a->prefix_lengths) ||
+        (a->prefixes > 0 && a->max_prefix > 0 && !a->prefix_tables))
+        return AP_ERR_INVALID_ARG;
+    const size_t need = attention_shared_work(*c, *a);
+    if (need && (!o.work || !aligned(o.work, 16))) return AP_ERR_INVALID_ARG;
+    if (o.work_bytes < need) return AP_ERR_BUFFER_TOO_SMALL;
+    return done(launch_attention_shared(*c, *a, static_cast<hipStream_t>(stream)));
+}
+
+extern "C" ap_status ap_norm(const ap_normed *a, void *stream)
+{
+    if (!a) return AP_ERR_INVALID_ARG;
+    if (a->tokens < 0 || a->tokens > kMaxTokens || a->columns < 1 || a->columns > 32768) return AP_ERR_SHAPE;
+    if (a->tokens == 0) return AP_OK;
+    const int64_t most = (int64_t)1 << 40;
+    const uintptr_t wide = a->half ? 2 : 4;
+    const auto ok = [&](const ap_rows &r, uintptr_t element) { return aligned(r.data, element) && r.stride > -most && r.stride < most; };
+    if ((!a->x.data && !a->residual.data) || !ok(a->x, 2) || !ok(a->gate, 2) || !ok(a->out, 2) || !ok(a->residual, wide) || !ok(a->residual_out, wide))
+        return AP_ERR_INVALID_ARG;
+    if (!aligned(a->weight, 2) || !aligned(a->bias, 2) || !aligned(a->post_weight, 2) || !aligned(a->post_bias, 2)) return AP_ERR_INVALID_ARG;
+    if (!std::isfinite(a->scale) || !(a->eps >= 0) || !std::isfinite(a->eps)) return AP_ERR_INVALID_ARG;
+    if (!a->out.data && !a->residual_out.data) return AP_OK;
+    return done(launch_norm(*a, static_cast<hipStream_t>(stream)));
+}
+
+static ap_status check_sample(const ap_sampling *a)
+{
+    if (!a) return AP_ERR_INVALID_ARG;
+    const int64_t most = (int64_t)1 << 40;
+    // a workgroup of up to 1024 threads per row
+    if (a->rows < 0 || a->rows > 1 << 21 || a->vocabulary < 1 || a->vocabulary > 1 << 20 || a->stride <= -most || a->stride >= most) return AP_ERR_SHAPE;
+    return AP_OK;
+}
+
+extern "C" ap_status ap_sample_size(const ap_sampling *a, size_t *bytes)
+{
+    const ap_status s = check_sample(a);
+    if (s != AP_OK) return s;
+    if (!bytes) return AP_ERR_INVALID_ARG;
+    *bytes = a->rows == 0 ? 0 : sample_work(*a);
+    return AP_OK;
+}
+
+extern "C" ap_status ap_sample(const ap_sampling *a, void *stream)
+{
+    const ap_status s = check_sample(a);
+    if (s != AP_OK) return s;
+    if (a->rows == 0) return AP_OK;
+    if (!a->logits || !aligned(a->logits, a->half ? 2 : 4) || !a->uniform || !aligned(a->uniform, 4) || !a->tokens || !aligned(a->tokens, 8) ||
+        !aligned(a->temperature, 4) || !aligned(a->top_p, 4) || !aligned(a->min_p, 4) || !aligned(a->top_k, 4) ||
+        !aligned(a->probabilities, a->half_probabilities ? 2 : 4))
+        return AP_ERR_INVALID_ARG;
+    const size_t need = sample_work(*a);
+    if (need && (!a->work || !aligned(a->work, 16))) return AP_ERR_INVALID_ARG;
+    if (a->work_bytes < need) return AP_ERR_BUFFER_TOO_SMALL;
+    return done(launch_sample(*a, static_cast<hipStream_t>(stream)));
+}

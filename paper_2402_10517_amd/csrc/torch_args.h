@@ -79,6 +79,9 @@ PyObject *cache_read(PyObject *, PyObject *const *args, Py_ssize_t n);
 PyObject *attention_cached(PyObject *, PyObject *const *args, Py_ssize_t n);
 PyObject *attention_prompt(PyObject *, PyObject *const *args, Py_ssize_t n);
 PyObject *verify(PyObject *, PyObject *const *args, Py_ssize_t n);
+PyObject *attention_shared(PyObject *, PyObject *const *args, Py_ssize_t n);
+PyObject *norm(PyObject *, PyObject *const *args, Py_ssize_t n);
+PyObject *sample(PyObject *, PyObject *const *args, Py_ssize_t n);
 
 } // namespace apgemv_torch
 #endif

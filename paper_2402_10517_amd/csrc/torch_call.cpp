@@ -132,6 +132,9 @@ PyMethodDef methods[] = {
     {"attention_cached", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(attention_cached)), METH_FASTCALL, nullptr},
     {"attention_prompt", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(attention_prompt)), METH_FASTCALL, nullptr},
     {"verify", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(verify)), METH_FASTCALL, nullptr},
+    {"attention_shared", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(attention_shared)), METH_FASTCALL, nullptr},
+    {"norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(norm)), METH_FASTCALL, nullptr},
+    {"sample", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(sample)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

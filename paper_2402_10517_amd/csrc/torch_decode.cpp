@@ -108,6 +108,17 @@ struct Call {
         return t.data_ptr();
     }
 
+    // (tokens, columns) rows of `type` with contiguous columns; `rows` of them, or one for all where `shared` allows
+    ap_rows matrix(PyObject *o, const char *what, at::ScalarType type, int64_t count, int64_t columns, bool shared = false)
+    {
+        const at::Tensor &t = tensor(o, what);
+        if (t.device() != device || t.scalar_type() != type || t.dim() != 2 || t.size(1) != columns || (t.size(0) != count && !(shared && t.size(0) == 1)) ||
+            (columns > 1 && t.stride(1) != 1))
+            refuse(what, type == at::kHalf ? "must be a float16 tensor (tokens, columns) of the call's size on its GPU, with contiguous columns"
+                                           : "must be a float32 tensor (tokens, columns) of the call's size on its GPU, with contiguous columns");
+        return ap_rows{t.data_ptr(), t.size(0) > 1 ? t.stride(0) : 0};
+    }
+
     // the output that was given, or a new one
     at::Tensor output(PyObject *given, const char *what, at::IntArrayRef sizes, at::ScalarType type)
     {
@@ -335,6 +346,151 @@ PyObject *verify(PyObject *, PyObject *const *args, Py_ssize_t n)
         a.accepted = static_cast<int32_t *>(accepted.data_ptr());
         status = without_gil([&] { return ap_verify(&a, c.stream.address); });
         return status == AP_OK ? pair(tokens, accepted) : PyLong_FromLong(status);
+    });
+}
+
+// attention_shared(buffer, shape, q, prefix_tables, prefix_lengths, tables, lengths, prefix_starts, q_starts, scale, max_prefix, max_length, out, work, stream) ->
+// out, or a status
+PyObject *attention_shared(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded(args, n, 15, [&]() -> PyObject * {
+        Call c;
+        const ap_cache cache = c.cache(args[0], args[1]);
+        ap_shared a = {};
+        ap_cached &o = a.own;
+        const at::Tensor *q = nullptr;
+        o.q = c.rows(args[2], "q", -1, -1, cache.head_dim, &q);
+        o.tokens = q->size(0);
+        o.heads = (int)std::min<int64_t>(q->size(1), INT_MAX);
+        const auto table = [&](PyObject *given, const char *what, int *rows, int64_t *width) {
+            const at::Tensor &t = c.tensor(given, what);
+            if (t.dim() != 2 || t.size(0) > INT_MAX) refuse(what, "must have two dimensions");
+            *rows = (int)t.size(0);
+            *width = t.size(1);
+            return static_cast<const int32_t *>(c.array(given, what, at::kInt, t.numel()));
+        };
+        const auto ints = [&](PyObject *given, const char *what, int64_t count) { return static_cast<const int32_t *>(c.array(given, what, at::kInt, count)); };
+        a.prefix_tables = table(args[3], "prefix_tables", &a.prefixes, &a.prefix_width);
+        o.tables = table(args[5], "tables", &o.sequences, &o.table_width);
+        a.prefix_lengths = ints(args[4], "prefix_lengths", a.prefixes);
+        o.lengths = ints(args[6], "lengths", o.sequences);
+        if (args[7] != Py_None) a.prefix_starts = ints(args[7], "prefix_starts", (int64_t)a.prefixes + 1);
+        if (args[8] != Py_None) o.q_starts = ints(args[8], "q_starts", (int64_t)o.sequences + 1);
+        o.scale = c.scale(args[9], cache.head_dim);
+        a.max_prefix = args[10] == Py_None ? a.prefix_width * cache.page_tokens : c.integer(args[10]);
+        o.max_length = args[11] == Py_None ? o.table_width * cache.page_tokens : c.integer(args[11]);
+        size_t bytes = 0;
+        ap_status status = ap_attention_shared_size(&cache, &a, &bytes);
+        if (status != AP_OK) return PyLong_FromLong(-(long)status);
+        c.start(args[14]);
+        const at::Tensor out = c.output(args[12], "out", {o.tokens, o.heads, cache.head_dim}, at::kHalf);
+        const at::Tensor work = c.workspace(args[13], bytes, &o.work, &o.work_bytes);
+        o.out = out.data_ptr();
+        status = without_gil([&] { return ap_attention_shared(&cache, &a, c.stream.address); });
+        return status == AP_OK ? THPVariable_Wrap(out) : PyLong_FromLong(status);
+    });
+}
+
+// norm(x, residual, weight, bias, post_weight, post_bias, post, gate, scale, eps, centred, normed, out, residual_out, stream) -> (out, residual_out), or a status
+PyObject *norm(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded(args, n, 15, [&]() -> PyObject * {
+        Call c;
+        const bool has_x = args[0] != Py_None, has_residual = args[1] != Py_None;
+        const at::Tensor &first = c.tensor(has_x ? args[0] : args[1], has_x ? "x" : "residual");
+        if (!first.is_cuda() || first.dim() != 2) refuse(has_x ? "x" : "residual", "must be a tensor (tokens, columns) on the GPU");
+        c.on(first.device());
+        ap_normed a = {};
+        const int64_t T = a.tokens = first.size(0), K = a.columns = first.size(1);
+        const auto truth = [&](PyObject *o) {
+            const int t = PyObject_IsTrue(o);
+            if (t < 0) throw Refused{};
+            return t;
+        };
+        // the residual's type: that of the one given, else of the output given, else binary32
+        at::ScalarType wide = at::kFloat;
+        if (has_residual) wide = c.tensor(args[1], "residual").scalar_type();
+        else if (args[13] != Py_None) wide = c.tensor(args[13], "residual_out").scalar_type();
+        if (wide != at::kFloat && wide != at::kHalf) refuse("residual", "must be a float32 or float16 tensor");
+        a.half = wide == at::kHalf;
+        if (has_x) a.x = c.matrix(args[0], "x", at::kHalf, T, K);
+        if (has_residual) a.residual = c.matrix(args[1], "residual", wide, T, K);
+        if (args[7] != Py_None) a.gate = c.matrix(args[7], "gate", at::kHalf, T, K, true);
+        const auto vector = [&](PyObject *o, const char *what) -> const void * { return o == Py_None ? nullptr : c.array(o, what, at::kHalf, K); };
+        a.weight = vector(args[2], "weight");
+        a.bias = vector(args[3], "bias");
+        a.post_weight = vector(args[4], "post_weight");
+        a.post_bias = vector(args[5], "post_bias");
+        a.post = truth(args[6]);
+        a.scale = c.scale(args[8], 1);
+        a.eps = c.scale(args[9], 1);
+        a.centred = truth(args[10]);
+        const bool normed = truth(args[11]);
+        c.start(args[14]);
+        at::Tensor out, residual_out;
+        const auto given = [&](PyObject *o, const char *what, at::ScalarType type, ap_rows *rows) {
+            *rows = c.matrix(o, what, type, T, K);
+            return c.tensor(o, what);
+        };
+        const auto fresh = [&](at::ScalarType type, ap_rows *rows) {
+            const at::Tensor t = allocate({T, K}, type, c.device, c.stream, true);
+            *rows = ap_rows{t.data_ptr(), K};
+            return t;
+        };
+        if (args[12] != Py_None) out = given(args[12], "out", at::kHalf, &a.out);
+        else if (normed) out = fresh(at::kHalf, &a.out);
+        if (args[13] != Py_None) residual_out = given(args[13], "residual_out", wide, &a.residual_out);
+        else if (has_x && has_residual) residual_out = fresh(wide, &a.residual_out);
+        const ap_status status = without_gil([&] { return ap_norm(&a, c.stream.address); });
+        return status == AP_OK ? pair(out, residual_out) : PyLong_FromLong(status);
+    });
+}
+
+// sample(logits, uniform, temperature, top_k, top_p, min_p, probabilities (a tensor, 0 = none, 1 = float32, 2 = float16), work, stream) -> (tokens, probabilities),
+// or a status
+PyObject *sample(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded(args, n, 9, [&]() -> PyObject * {
+        Call c;
+        const at::Tensor &logits = c.tensor(args[0], "logits");
+        if (!logits.is_cuda() || logits.dim() != 2 || (logits.scalar_type() != at::kHalf && logits.scalar_type() != at::kFloat))
+            refuse("logits", "must be a float32 or float16 tensor (rows, vocabulary) on the GPU");
+        c.on(logits.device());
+        ap_sampling a = {};
+        const int64_t S = a.rows = logits.size(0), V = a.vocabulary = logits.size(1);
+        a.half = logits.scalar_type() == at::kHalf;
+        const ap_rows rows = c.matrix(args[0], "logits", logits.scalar_type(), S, V);
+        a.logits = rows.data;
+        a.stride = rows.stride;
+        const auto floats = [&](PyObject *o, const char *what) { return o == Py_None ? nullptr : static_cast<const float *>(c.array(o, what, at::kFloat, S)); };
+        a.uniform = static_cast<const float *>(c.array(args[1], "uniform", at::kFloat, S));
+        a.temperature = floats(args[2], "temperature");
+        if (args[3] != Py_None) a.top_k = static_cast<const int32_t *>(c.array(args[3], "top_k", at::kInt, S));
+        a.top_p = floats(args[4], "top_p");
+        a.min_p = floats(args[5], "min_p");
+        size_t bytes = 0;
+        ap_status status = ap_sample_size(&a, &bytes);
+        if (status != AP_OK) return PyLong_FromLong(-(long)status);
+        c.start(args[8]);
+        const at::Tensor tokens = allocate({S}, at::kLong, c.device, c.stream, true);
+        at::Tensor probabilities;
+        if (PyLong_Check(args[6])) {
+            const int64_t kind = c.integer(args[6]);
+            if (kind) probabilities = allocate({S, V}, kind == 2 ? at::kHalf : at::kFloat, c.device, c.stream, true);
+        } else {
+            probabilities = c.tensor(args[6], "probabilities");
+            if (probabilities.dim() != 2 || (probabilities.scalar_type() != at::kHalf && probabilities.scalar_type() != at::kFloat))
+                refuse("probabilities", "must be a float32 or float16 tensor (rows, vocabulary)");
+            c.array(args[6], "probabilities", probabilities.scalar_type(), S * V);
+        }
+        const at::Tensor work = c.workspace(args[7], bytes, &a.work, &a.work_bytes);
+        a.tokens = static_cast<int64_t *>(tokens.data_ptr());
+        if (probabilities.defined()) {
+            a.probabilities = probabilities.data_ptr();
+            a.half_probabilities = probabilities.scalar_type() == at::kHalf;
+        }
+        status = without_gil([&] { return ap_sample(&a, c.stream.address); });
+        return status == AP_OK ? pair(tokens, probabilities) : PyLong_FromLong(status);
     });
 }
 
