@@ -6,6 +6,9 @@
 // weight per token), not where a rounding of a long binary32 sum would.
 //
 // A workgroup has a row, whose first tokens it keeps in LDS.
+#include <cfloat>
+#include <type_traits>
+
 #include "decode_device.h"
 
 namespace apgemv {
@@ -26,10 +29,12 @@ struct SampleArgs {
 constexpr int kEach = 8;          // adjacent tokens of a lane and tile
 constexpr int kTile = 64 * kEach; // tokens of a wave and step: up to 2^20 / kTile sums of tiles take the histogram's place
 constexpr int kBins = 2048;
-constexpr int kList = 1024;       // tokens of one bin that are listed
-constexpr int kFew = 128;         // top-k up to which the tokens are ranked among each other,
+constexpr int kList = 2048;       // tokens that are listed
+constexpr int kMostListed = 1024; // top-k up to which a row's candidates are listed,
+constexpr int kFew = 128;         // and ranked among each other,
 constexpr int kRanked = 256;      // so many at most
 constexpr int kWaves = 16;        // of a workgroup, at most
+constexpr int kFinders = 4;       // waves that look for a place in the bins: all 16 take turns on the four SIMDs, and twice as long
 constexpr double kLog2e = 1.4426950408889634, kLn2 = 0.6931471805599453;
 
 // Greater logits have smaller keys; -0 and 0 the same one
@@ -64,8 +69,8 @@ __device__ __forceinline__ uint64_t lane_of(uint64_t x, int lane)
     return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, lane);
 }
 
-// 2^(j / 64), by the power series of exp
-constexpr int kSteps = 64;
+// 2^(j / kSteps), by the power series of exp
+constexpr int kSteps = 512;
 struct Powers {
     double x[kSteps];
     constexpr Powers() : x()
@@ -79,34 +84,49 @@ struct Powers {
 };
 __device__ constexpr Powers kPowers;
 
-// What the tokens of a row weigh: 2^(d / 64) with d = 64 log2 e (x - most) / temperature <= 0, as 2^n times a table's 2^(j / 64) times the power series of exp on
-// half a step either way, off by 4e-14.  Adding 1.5 2^52 leaves the whole part of d in the low bits of the sum.
+constexpr uint64_t kFixedBase = 0x4330000000000000ull; // the bits of 2^52
+
+// What the tokens of a row weigh: 2^(d / kSteps) with d = kSteps log2 e (x - most) / temperature <= 0, as 2^n times a table's 2^(j / kSteps) times the power series
+// of exp on half a step either way, off by 1e-14 (with a table of 64 one more term).  Adding 1.5 2^52 leaves the whole part of d in the low bits of the sum.
 struct Weights {
     double most, rate;
     const double *table; // LDS
     int unit;
-    // 2^scale times the weight, d not below `least`
-    __device__ double of(float x, int scale, double least) const
+    float floor, far; // logits that weigh less than 2^-3 in fixed point, and less than 2^-160; not infinite
+    // 2^scale times the weight of x
+    __device__ double of(float x, int scale) const
     {
-        const double magic = 0x1.8p52 + 64.0 * scale, d = fmax(((double)x - most) * rate, least), t = d + magic, f = d - (t - magic);
+        const double magic = 0x1.8p52 + (double)kSteps * scale, y = (double)x - most, t = __builtin_fma(y, rate, magic), f = __builtin_fma(y, rate, magic - t);
         const int k = (int)(uint32_t)__double_as_longlong(t);
-        constexpr double c = kLn2 / 64;
-        double p = __builtin_fma(c * c * c * c / 24, f, c * c * c / 6);
-        p = __builtin_fma(p, f, c * c / 2);
+        constexpr double c = kLn2 / kSteps;
+        double p = __builtin_fma(c * c * c / 6, f, c * c / 2);
         p = __builtin_fma(p, f, c);
         p = __builtin_fma(p, f, 1.0);
-        return __longlong_as_double(__double_as_longlong(table[k & 63] * p) + ((long long)(k >> 6) << 52));
+        return __longlong_as_double(__double_as_longlong(table[k & (kSteps - 1)] * p) + ((long long)(k >> 9) << 52));
     }
-    // In fixed point: a number below 2^52 added to 2^52 has its integer part in the low bits.  2^-3 and less are 0, as is the weight of -inf.
-    __device__ uint64_t fixed(float x) const { return (uint64_t)__double_as_longlong(of(x, unit, -64.0 * (unit + 3)) + 0x1p52) & 0xfffffffffffffull; }
-    __device__ double exact(float x) const { return of(x, 0, -64.0 * 1000); }
+    // In fixed point: a number below 2^52 added to 2^52 has its integer part in the low bits, kFixedBase above them.  Not for logits below floor.
+    __device__ uint64_t fixed_up(float x) const { return (uint64_t)__double_as_longlong(of(x, unit) + 0x1p52); }
+    __device__ uint64_t fixed(float x) const { return fixed_up(fmaxf(x, floor)) - kFixedBase; }
+    // a number below 2^-159 instead of any less
+    __device__ double exact(float x) const { return of(fmaxf(x, far), 0); }
 };
+static_assert(kSteps == 1 << 9, "the shift of Weights::of");
 
 // The beginning of the order that is kept: logits above x, and of those equal to it the tokens up to `last`
 struct Cut {
     float x;
     int last;
     __device__ bool keeps(float y, int v) const { return y > x || (y == x && v <= last); }
+    // of n adjacent tokens; mostly all that are equal to x are kept
+    template <int n> __device__ void keeps(const float (&y)[n], int v, bool (&out)[n]) const
+    {
+#pragma unroll
+        for (int i = 0; i < n; ++i) out[i] = y[i] >= x && y[i] > -INFINITY;
+        if (last < 0x7fffffff) {
+#pragma unroll
+            for (int i = 0; i < n; ++i) out[i] = keeps(y[i], v + i);
+        }
+    }
 };
 
 // 8 adjacent values of rows that start at any element: 16-byte accesses that ask for the element's alignment only
@@ -141,9 +161,10 @@ template <class T> struct Row {
     int staged, vocabulary;
     bool infinite; // +inf is the greatest: such logits are 0, all others -inf
 
+    // NaN stays: no comparison holds for it
     __device__ float value(T t) const
     {
-        const float x = fmaxf((float)t, -INFINITY); // NaN counts as -inf
+        const float x = (float)t;
         if (infinite) return x == INFINITY ? 0.0f : -INFINITY;
         return x;
     }
@@ -155,19 +176,29 @@ template <class T> struct Row {
     __device__ int tile(int t, float (&out)[kEach]) const
     {
         const int v = t * kTile + (threadIdx.x & 63) * kEach;
-        const auto e = raw(v);
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) out[i] = value(e[i]);
+        values(raw(v), out);
         return v;
     }
-    // f(first token, logits) for the wave's tiles
+    __device__ void values(const typename Eight<T>::values_t &e, float (&out)[kEach]) const
+    {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) out[i] = (float)e[i];
+        if (infinite) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) out[i] = out[i] == INFINITY ? 0.0f : -INFINITY;
+        }
+    }
+    // f(logits, first token) for the wave's tiles
     template <class F> __device__ void tiles(const F &f) const
     {
-        const int waves = blockDim.x >> 6;
-        for (int t = threadIdx.x >> 6; t * kTile < vocabulary; t += waves) {
+        const int step = (blockDim.x >> 6) * kTile;
+        int v = (threadIdx.x >> 6) * kTile + (threadIdx.x & 63) * kEach;
+        auto next = raw(v);
+        for (int end = v - (threadIdx.x & 63) * kEach; end < vocabulary; end += step, v += step) {
             float e[kEach];
-            const int v = tile(t, e);
-            f(v, e);
+            values(next, e);
+            if (end + step < vocabulary) next = raw(v + step);
+            f(e, v);
         }
     }
     // f(logit, token), in little code for what is seldom run
@@ -178,12 +209,26 @@ template <class T> struct Row {
     }
 };
 
+// The tokens that s.list holds, as few as may be kept
+struct List {
+    const uint2 *list;
+    int count, vocabulary;
+    template <class F> __device__ void tiles(const F &f) const
+    {
+        for (int i = threadIdx.x; i < count; i += blockDim.x) {
+            const uint2 x = list[i];
+            const float e[1] = {logit_of(x.y)};
+            f(e, (int)x.x);
+        }
+    }
+};
+
 struct Shared {
     uint64_t bins[kBins];        // or the sums of tiles
     uint2 list[kList];           // (token, key)
-    uint64_t wave_sum[kWaves];
     double table[kSteps];
-    uint64_t before, amount;
+    uint64_t wave_sum[kFinders];
+    uint64_t before, amount, all, wanted;
     float wave_most[kWaves];
     uint32_t low, high;
     int count, place, kept;
@@ -202,36 +247,63 @@ __device__ __forceinline__ uint64_t share_of(float p, uint64_t sum)
     return x >= 1 ? (uint64_t)x : 1;
 }
 
-// The first of `count` numbers in LDS at which the sum up to it reaches the target that target(sum of all) gives: s.place, s.before (the sum
-// before it) and s.amount (it).  count <= kBins.  A target is 1 at least; one beyond the sum leaves s.place at -1.
-template <class F> __device__ uint64_t find(Shared &s, int count, const F &target)
+// The first of `count` numbers in LDS at which the sum up to it reaches the target that target(sum of all) gives: s.place, s.before (the sum before it), s.amount
+// (it), s.all and s.wanted, the target.  count <= kBins.  A target is 1 at least; one beyond the sum leaves s.place at -1.
+template <class F> __device__ void find(Shared &s, int count, const F &target)
 {
-    const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6, lane = threadIdx.x & 63;
-    const int per = blockDim.x == 1024 ? kBins / 1024 : (count + blockDim.x - 1) / blockDim.x, first = threadIdx.x * per;
-    uint64_t mine = 0;
-    for (int i = 0; i < per; ++i)
-        if (first + i < count) mine += s.bins[first + i];
-    const uint64_t upto = wave_scan(mine);
-    if (lane == 63) s.wave_sum[wave] = upto;
-    if (threadIdx.x == 0) s.place = -1;
-    __syncthreads();
-    const uint64_t sums = row_scan((lane & 15) < waves ? s.wave_sum[lane & 15] : 0), all = lane_of(sums, 15);
-    uint64_t before = upto - mine + (wave > 0 ? lane_of(sums, wave - 1) : 0);
-    const uint64_t wanted = target(all);
-    if (before < wanted && wanted <= before + mine) {
-        for (int i = 0; i < per; ++i) {
-            const uint64_t x = s.bins[first + i];
-            if (wanted <= before + x) {
-                s.place = first + i;
-                s.before = before;
-                s.amount = x;
-                break;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, finders = blockDim.x >> 6 < kFinders ? blockDim.x >> 6 : kFinders;
+    const int per = (count + 64 * finders - 1) / (64 * finders), first = threadIdx.x * per;
+    constexpr int kMost = kBins / (64 * kFinders);
+    const bool all_bins = count == kBins && finders == kFinders;
+    uint64_t x[kMost], mine = 0, upto = 0;
+    if (wave < finders) {
+        if (all_bins) {
+            typedef uint64_t pair_t __attribute__((ext_vector_type(2)));
+#pragma unroll
+            for (int i = 0; i < kMost; i += 2) {
+                const pair_t y = *reinterpret_cast<const pair_t *>(&s.bins[first + i]);
+                x[i] = y[0], x[i + 1] = y[1];
+                mine += y[0] + y[1];
             }
-            before += x;
+        } else {
+            for (int i = 0; i < per; ++i)
+                if (first + i < count) mine += s.bins[first + i];
+        }
+        upto = wave_scan(mine);
+        if (lane == 63) s.wave_sum[wave] = upto;
+        if (threadIdx.x == 0) s.place = -1;
+    }
+    __syncthreads();
+    if (wave < finders) {
+        uint64_t before = upto - mine, all = 0;
+#pragma unroll
+        for (int w = 0; w < kFinders; ++w) {
+            const uint64_t y = w < finders ? s.wave_sum[w] : 0;
+            before += w < wave ? y : 0;
+            all += y;
+        }
+        const uint64_t wanted = target(all);
+        if (threadIdx.x == 0) s.all = all, s.wanted = wanted;
+        if (before < wanted && wanted <= before + mine) {
+            if (all_bins) {
+#pragma unroll
+                for (int i = 0; i < kMost; ++i) {
+                    if (before < wanted && wanted <= before + x[i]) s.place = first + i, s.before = before, s.amount = x[i];
+                    before += x[i];
+                }
+            } else {
+                for (int i = 0; i < per; ++i) {
+                    const uint64_t y = s.bins[first + i];
+                    if (wanted <= before + y) {
+                        s.place = first + i, s.before = before, s.amount = y;
+                        break;
+                    }
+                    before += y;
+                }
+            }
         }
     }
     __syncthreads();
-    return all;
 }
 
 __device__ __forceinline__ void clear_bins(Shared &s)
@@ -241,8 +313,10 @@ __device__ __forceinline__ void clear_bins(Shared &s)
 }
 __device__ __forceinline__ void add(Shared &s, int bin, uint64_t x) { atomicAdd((unsigned long long *)&s.bins[bin], (unsigned long long)x); }
 
-// The place of a logit among the first bins, which are even in it, 64 to a factor of two in the weight: tokens spread over many, and few are in the one
-// that matters.  The last bin holds all the rest.
+// The place of a logit among the first bins, which are even in it, 40 to a factor of two in the weight: tokens spread over many, and few are in the one
+// that matters.  The last bin holds all the rest, whose weights are 0 in fixed point.
+constexpr int kBinsPerOctave = 40;
+static_assert(kBins / kBinsPerOctave >= 51, "the smallest weight in fixed point");
 struct Even {
     float most, rate;
     __device__ float place(float x) const { return (most - x) * rate; }
@@ -253,47 +327,55 @@ struct Even {
 //
 // The tokens of the even bin that reaches it are listed.  Their interval of keys is divided into bins until one key is left; where it has more tokens than
 // are wanted, an interval of token numbers is, for the first ones.  A bin that holds more than the list is looked for in the row.
-template <class T> __device__ Cut select(Shared &s, const Row<T> &row, const Weights &w, const Cut cut, const Even even, bool weigh, int count, float p)
+template <class S> __device__ Cut select(Shared &s, const S &source, const Weights &w, const Cut cut, const Even even, bool weigh, int count, float p)
 {
+    constexpr bool kListed = std::is_same_v<S, List>;
     clear_bins(s);
-    row.tiles([&](int v, const float(&e)[kEach]) {
-        uint64_t x[kEach];
+    source.tiles([&](const auto &e, int v) {
+        constexpr int n = sizeof(e) / sizeof(e[0]);
+        bool keep[n];
+        cut.keeps(e, v, keep);
+        if (weigh) { // (weights of 0 stay away: they are many where one token has nearly all)
+            uint64_t x[n];
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) x[i] = 1;
-        if (weigh) {
+            for (int i = 0; i < n; ++i) x[i] = w.fixed(e[i]);
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) x[i] = w.fixed(e[i]);
+            for (int i = 0; i < n; ++i)
+                if (keep[i] && e[i] >= w.floor) add(s, even.bin(e[i]), x[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < n; ++i)
+                if (keep[i]) add(s, even.bin(e[i]), 1);
         }
-#pragma unroll
-        for (int i = 0; i < kEach; ++i)
-            if (cut.keeps(e[i], v + i)) add(s, even.bin(e[i]), x[i]);
     });
     if (threadIdx.x == 0) s.count = 0, s.low = 0xffffffffu, s.high = 0;
     __syncthreads();
-    uint64_t wanted = 0;
-    find(s, kBins, [&](uint64_t all) { return wanted = weigh ? share_of(p, all) : (uint64_t)count; });
+    find(s, kBins, [&](uint64_t all) { return weigh ? share_of(p, all) : (uint64_t)count; });
     const int bin = s.place;
     if (bin < 0) return cut; // fewer tokens than wanted
-    wanted -= s.before;
-    uint64_t amount = s.amount;
+    uint64_t wanted = s.wanted - s.before, amount = s.amount;
     const float from = bin, to = bin == kBins - 1 ? __builtin_nanf("") : (float)(bin + 1); // not at or beyond NaN: everything
     const auto inside = [&](float x, int v) {
         const float at = even.place(x);
         return at >= from && !(at >= to) && cut.keeps(x, v);
     };
-    row.tiles([&](int v, const float(&e)[kEach]) {
+    source.tiles([&](const auto &e, int v) {
+        constexpr int n = sizeof(e) / sizeof(e[0]);
 #pragma unroll
-        for (int i = 0; i < kEach; ++i)
+        for (int i = 0; i < n; ++i)
             if (inside(e[i], v + i)) {
                 const uint32_t key = key_of(e[i]);
-                const int at = atomicAdd(&s.count, 1);
-                if (at < kList) s.list[at] = make_uint2(v + i, key);
+                if (!kListed) {
+                    const int at = atomicAdd(&s.count, 1);
+                    if (at < kList) s.list[at] = make_uint2(v + i, key);
+                }
                 atomicMin(&s.low, key);
                 atomicMax(&s.high, key);
             }
     });
     __syncthreads();
-    const int listed = s.count;
+    int listed = s.count;
+    if constexpr (kListed) listed = source.count;
     uint32_t low = s.low, high = s.high, key = 0;
     bool numbers = false; // of the tokens with `key`
     for (;;) {
@@ -305,7 +387,7 @@ template <class T> __device__ Cut select(Shared &s, const Row<T> &row, const Wei
             wanted = (wanted + one - 1) / one;
             if (wanted >= amount / one) return Cut{x, x == cut.x ? cut.last : 0x7fffffff};
             numbers = true;
-            low = 0, high = row.vocabulary - 1;
+            low = 0, high = source.vocabulary - 1;
         }
         const int bits = 32 - __builtin_clz(high - low), shift = bits > 11 ? bits - 11 : 0;
         clear_bins(s);
@@ -314,9 +396,12 @@ template <class T> __device__ Cut select(Shared &s, const Row<T> &row, const Wei
             if (number >= low && number <= high && (!numbers || k == key)) add(s, (number - low) >> shift, weigh && !numbers ? w.fixed(logit_of(k)) : 1);
         };
         if (listed <= kList) {
-            for (int i = threadIdx.x; i < listed; i += blockDim.x) consider((int)s.list[i].x, s.list[i].y);
-        } else {
-            row.each([&](float x, int v) {
+            for (int i = threadIdx.x; i < listed; i += blockDim.x) {
+                const uint2 x = s.list[i];
+                if (!kListed || cut.keeps(logit_of(x.y), (int)x.x)) consider((int)x.x, x.y);
+            }
+        } else if constexpr (!kListed) {
+            source.each([&](float x, int v) {
                 if (inside(x, v)) consider(v, key_of(x));
             });
         }
@@ -332,82 +417,117 @@ template <class T> __device__ Cut select(Shared &s, const Row<T> &row, const Wei
     }
 }
 
-// Few tokens that a row keeps at most, ranked among each other.  The k-th best of the lanes' own best tokens leaves k tokens before it at least, and few more
-// where k is small beside the lanes: those are listed, a thread each.  False where that does not hold; the kept ones' *cut and the sum of their weights otherwise.
-template <class T> __device__ bool few(Shared &s, const Row<T> &row, const Weights &w, const Even even, float lane_most, int k, float p, float least, float u, int64_t *token, Cut *cut, uint64_t *all)
+// Candidates of a small top-k.  The k-th best of the greatest logits of groups of tokens leaves k tokens before it at least, and few more where k is small beside the
+// groups: those are listed.  Groups are the tokens of a lane (groups = false: of 1024) or 8 adjacent ones.  Returns their number, -1 where the place is not to be had.
+template <class T> __device__ int candidates(Shared &s, const Row<T> &row, const Even even, float lane_most, int k, bool groups)
 {
+    const auto top_of = [](const float(&e)[kEach]) {
+        float top = e[0];
+#pragma unroll
+        for (int i = 1; i < kEach; ++i) top = fmaxf(top, e[i]);
+        return top;
+    };
     clear_bins(s);
-    if (lane_most != -INFINITY) add(s, even.bin(lane_most), 1);
+    if (groups) {
+        row.tiles([&](const float(&e)[kEach], int) {
+            const float top = top_of(e);
+            if (top > -INFINITY) add(s, even.bin(top), 1);
+        });
+    } else if (lane_most != -INFINITY) {
+        add(s, even.bin(lane_most), 1);
+    }
     if (threadIdx.x == 0) s.count = 0, s.kept = 0;
     __syncthreads();
     find(s, kBins, [&](uint64_t) { return (uint64_t)k; });
     const int bin = s.place;
-    if (bin < 0 || bin == kBins - 1) return false;
+    if (bin < 0 || bin == kBins - 1) return -1;
     const float limit = bin + 1;
-    row.tiles([&](int v, const float(&e)[kEach]) {
-        float top = e[0];
+    const auto put = [&](float x, int v) {
+        if (!(even.place(x) < limit)) return;
+        const int at = atomicAdd(&s.count, 1);
+        if (at < kList) s.list[at] = make_uint2(v, key_of(x));
+    };
+    if (groups) {
+        row.tiles([&](const float(&e)[kEach], int v) {
+            if (!(even.place(top_of(e)) < limit)) return;
 #pragma unroll
-        for (int i = 1; i < kEach; ++i) top = fmaxf(top, e[i]);
-        if (!(even.place(top) < limit)) return;
-#pragma unroll
-        for (int i = 0; i < kEach; ++i)
-            if (even.place(e[i]) < limit) {
-                const int at = atomicAdd(&s.count, 1);
-                if (at < kRanked) s.list[at] = make_uint2(v + i, key_of(e[i]));
-            }
-    });
-    __syncthreads();
-    const int n = s.count, i = threadIdx.x;
-    if (n > kRanked || n > (int)blockDim.x) {
+            for (int i = 0; i < kEach; ++i) put(e[i], v + i);
+        });
+    } else {
+        // the lanes that have one, then a thread for each token of theirs
+        int *const lanes = reinterpret_cast<int *>(s.bins);
+        if (even.place(lane_most) < limit) lanes[atomicAdd(&s.kept, 1)] = threadIdx.x;
         __syncthreads();
-        return false;
+        const int waves = blockDim.x >> 6, each = (row.vocabulary + kTile * waves - 1) / (kTile * waves) * kEach, items = s.kept * each;
+        for (int i = threadIdx.x; i < items; i += blockDim.x) {
+            const int l = i / each, j = i - l * each, of = lanes[l], v = ((of >> 6) + j / kEach * waves) * kTile + (of & 63) * kEach + j % kEach;
+            if (v < row.vocabulary) put(row.value(v < row.staged ? row.stage[v] : row.x[v]), v);
+        }
     }
-    // Loops over the n tokens take eight at a time, all waves that have one together; behind the last one are tokens that come after all and weigh nothing.
-    constexpr int kStep = 8;
-    uint64_t *const orders = reinterpret_cast<uint64_t *>(s.list), *const weights = s.bins;
-    const bool mine = i < n;
-    const uint2 me = mine ? s.list[i] : make_uint2(0xffffffffu, 0xffffffffu);
-    const uint64_t order = (uint64_t)me.y << 32 | me.x;
-    const uint64_t weight = mine ? w.fixed(logit_of(me.y)) : 0;
-    for (int j = i; j < n + kStep; j += blockDim.x) weights[j] = j == i ? weight : 0;
-    if (i < kStep) s.list[n + i] = make_uint2(0xffffffffu, 0xffffffffu);
     __syncthreads();
-    int rank = 0;
-    uint64_t before = 0;
-    if (i < (n + 63 & ~63))
-        for (int j = 0; j < n; j += kStep)
-#pragma unroll
-            for (int l = 0; l < kStep; ++l) {
-                const uint64_t other = orders[j + l], x = weights[j + l]; // (token, key): the key is the high half
-                const bool ahead = other < order;
-                rank += ahead;
-                before += ahead ? x : 0;
-            }
-    if (mine && rank == (k < n ? k : n) - 1) s.amount = before + weight;
+    return s.count;
+}
+
+// Ranks the n listed tokens among each other.  *token, and the kept ones' *cut and the sum of their weights.
+//
+// The sum of the weights ahead of a token is that over all others: their number is divided among the waves, whose parts meet in LDS.
+__device__ void rank(Shared &s, const Weights &w, int n, int k, float p, float least, float u, int64_t *token, Cut *cut, uint64_t *all)
+{
+    const uint64_t *const orders = reinterpret_cast<const uint64_t *>(s.list); // (token, key): the key is the high half
+    uint64_t *const weights = s.bins, *const aheads = s.bins + kRanked;
+    int *const ranks = reinterpret_cast<int *>(s.bins + 2 * kRanked);
+    const int i = threadIdx.x, columns = (n + 63) & ~63, parts = blockDim.x / columns, column = i % columns, part = i / columns; // parts of the others
+    const bool mine = i < n, work = column < n && part < parts;
+    uint64_t weight = 0;
+    float x = 0;
+    if (i < columns) {
+        x = mine ? logit_of(s.list[i].y) : 0.0f;
+        weight = mine ? w.fixed(x) : 0;
+        weights[i] = weight, aheads[i] = 0, ranks[i] = 0;
+    }
+    if (threadIdx.x == 0) s.kept = 0;
     __syncthreads();
-    const bool kept = mine && rank < k && (!(p < 1) || before < share_of(p, s.amount)) && (rank == 0 || logit_of(me.y) >= least);
+    // f(other's place) for the part
+    const auto others = [&](const auto &f) {
+        if (work)
+            for (int j = part; j < n; j += parts) f(j);
+    };
+    uint64_t ahead = 0;
+    int before = 0;
+    const uint64_t order = orders[column < n ? column : 0];
+    others([&](int j) {
+        const bool first = orders[j] < order;
+        before += first;
+        ahead += first ? weights[j] : 0;
+    });
+    if (work) {
+        atomicAdd(&ranks[column], before);
+        atomicAdd((unsigned long long *)&aheads[column], (unsigned long long)ahead);
+    }
+    __syncthreads();
+    if (mine) {
+        before = ranks[i];
+        ahead = aheads[i];
+        if (before == (k < n ? k : n) - 1) s.amount = ahead + weight;
+    }
+    __syncthreads();
+    const bool kept = mine && before < k && (!(p < 1) || ahead < share_of(p, s.amount)) && (before == 0 || x >= least);
     const uint64_t wave_kept = __ballot(kept);
     if ((threadIdx.x & 63) == 0 && wave_kept) atomicAdd(&s.kept, __builtin_popcountll(wave_kept));
-    if (mine) weights[i] = kept ? weight : 0;
+    if (i < columns) weights[i] = kept ? weight : 0, aheads[i] = 0;
     __syncthreads();
-    if (kept && rank == s.kept - 1) s.low = me.y, s.high = me.x; // the kept ones are the first in the order
-    uint64_t sum = 0;
-    before = 0;
-    if (i < (n + 63 & ~63))
-        for (int j = 0; j < n; j += kStep)
-#pragma unroll
-            for (int l = 0; l < kStep; ++l) {
-                const uint64_t x = weights[j + l];
-                sum += x;
-                before += (uint32_t)orders[j + l] < me.x ? x : 0;
-            }
-    const uint64_t wanted = wanted_of(u, sum);
-    if (kept && before < wanted && wanted <= before + weight) *token = (int)me.x;
-    if (i == 0) s.before = sum;
+    // the kept ones are the first in the order
+    if (kept && before == s.kept - 1) s.low = s.list[i].y, s.high = s.list[i].x, s.all = ahead + weight;
+    ahead = 0;
+    others([&](int j) { ahead += (uint32_t)orders[j] < (uint32_t)order ? weights[j] : 0; });
+    if (work) atomicAdd((unsigned long long *)&aheads[column], (unsigned long long)ahead);
     __syncthreads();
+    if (kept) {
+        const uint64_t wanted = wanted_of(u, s.all), from = aheads[i];
+        if (from < wanted && wanted <= from + weight) *token = s.list[i].x;
+    }
     *cut = Cut{logit_of(s.low), (int)s.high};
-    *all = s.before;
-    return true;
+    *all = s.all;
 }
 
 // The least logit whose weight is `share` at least: 64 keys at a time (64 lanes call together)
@@ -446,7 +566,7 @@ template <class T, class P, int STAGE> __global__ __launch_bounds__(64 * kWaves)
         for (int i = 0; i < kEach; ++i) lane_most = fmaxf(lane_most, (float)e[i]);
         if (v < row.staged) *reinterpret_cast<typename Eight<T>::values_t *>(stage + v) = e;
     }
-    if (threadIdx.x < kSteps) s.table[lane] = kPowers.x[lane];
+    for (int i = threadIdx.x; i < kSteps; i += blockDim.x) s.table[i] = kPowers.x[i];
     float most = lane_most;
     for (int m = 1; m < 64; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
     if (lane == 0) s.wave_most[wave] = most;
@@ -467,7 +587,7 @@ template <class T, class P, int STAGE> __global__ __launch_bounds__(64 * kWaves)
     typedef typename Eight<P>::values_t out_t;
     if (!(t > 0) || most == -INFINITY) { // the first token alone, or none
         if (most != -INFINITY && lane_most == most) {
-            row.tiles([&](int v, const float(&e)[kEach]) {
+            row.tiles([&](const float(&e)[kEach], int v) {
 #pragma unroll
                 for (int i = 0; i < kEach; ++i)
                     if (e[i] == most) atomicMin(&s.place, v + i);
@@ -491,46 +611,123 @@ template <class T, class P, int STAGE> __global__ __launch_bounds__(64 * kWaves)
     }
     Weights w;
     w.most = most;
-    w.rate = 64 * kLog2e / (double)t;
+    w.rate = kSteps * kLog2e / (double)t;
     w.table = s.table;
     w.unit = a.unit;
-    const Even even{most, fmaxf(fminf((float)w.rate, 1e30f), 1e-30f)};
+    // From a rate on the next logit below the greatest weighs 2^-512, nothing by any measure: a greater one would only take exponents out of their range
+    const double next = (double)most - (double)logit_of(key_of(most) + 1);
+    if (w.rate * next > 0x1p18 && next < (double)FLT_MAX) w.rate = 0x1p18 / next;
+    const double floor = (double)most - kSteps * (a.unit + 4) / w.rate;
+    w.floor = floor >= -(double)FLT_MAX ? (float)floor : -FLT_MAX;
+    if ((double)w.floor > floor) w.floor = w.floor > -FLT_MAX ? logit_of(key_of(w.floor) + 1) : -FLT_MAX;
+    const double far = (double)most - kSteps * 161 / w.rate;
+    w.far = far >= -(double)FLT_MAX ? (float)far : -FLT_MAX;
+    if ((double)w.far > far) w.far = w.far > -FLT_MAX ? logit_of(key_of(w.far) + 1) : -FLT_MAX;
+    const Even even{most, fmaxf(fminf((float)(w.rate * ((double)kBinsPerOctave / kSteps)), 1e30f), 1e-30f)};
     const float least = min_p > 0 ? least_logit(w, most, min_p < 1 ? (double)min_p : 1.0) : -INFINITY;
 
     Cut cut{-INFINITY, -1};
     uint64_t all = 0; // weights kept
-    if (!(k > 0 && k < V && k <= kFew && few(s, row, w, even, lane_most, k, p, least, u, a.tokens + r, &cut, &all))) {
+    int listed = -1;
+    if (k > 0 && k < V && k <= kMostListed) {
+        if (4 * k <= (int)blockDim.x && k <= kFew) {
+            listed = candidates(s, row, even, lane_most, k, false);
+            if (listed > kRanked || listed > (int)blockDim.x) listed = -1;
+        }
+        if (listed < 0 && 32 * k <= V) {
+            __syncthreads();
+            listed = candidates(s, row, even, lane_most, k, true);
+            if (listed > kList) listed = -1;
+        }
+    }
+    __syncthreads();
+    const auto cuts = [&](const auto &source) {
 #pragma unroll 1
         for (int weigh = 0; weigh < 2; ++weigh)
-            if (weigh ? p < 1 : k > 0 && k < V) cut = select(s, row, w, cut, even, weigh, k, p);
+            if (weigh ? p < 1 : k > 0 && k < V) cut = select(s, source, w, cut, even, weigh, k, p);
         if (least > cut.x) cut = Cut{least, 0x7fffffff};
         __syncthreads();
-        for (int i = wave; i < tiles; i += waves) {
-            float e[kEach];
-            const int v = row.tile(i, e);
-            uint64_t sum = 0;
+    };
+    if (listed >= 0 && listed <= kRanked && listed <= (int)blockDim.x) {
+        rank(s, w, listed, k, p, least, u, a.tokens + r, &cut, &all);
+    } else if (listed >= 0) {
+        const List list{s.list, listed, V};
+        cuts(list);
+        clear_bins(s);
+        list.tiles([&](const auto &e, int v) {
+            if (cut.keeps(e[0], v)) add(s, v / kTile, w.fixed(e[0]));
+        });
+        if (threadIdx.x == 0) s.count = 0;
+        __syncthreads();
+        find(s, tiles, [&](uint64_t sum) { return wanted_of(u, sum); });
+        const int tile = s.place;
+        const uint64_t wanted = s.wanted - s.before;
+        all = s.all;
+        // the kept tokens of the tile, each with the sum of those before it
+        uint64_t *const weights = s.bins, *const numbers = s.bins + kTile;
+        list.tiles([&](const auto &e, int v) {
+            if (v / kTile != tile || !cut.keeps(e[0], v)) return;
+            const int at = atomicAdd(&s.count, 1);
+            weights[at] = w.fixed(e[0]), numbers[at] = v;
+        });
+        __syncthreads();
+        for (int i = threadIdx.x; i < s.count; i += blockDim.x) {
+            uint64_t before = 0;
+            for (int j = 0; j < s.count; ++j) before += numbers[j] < numbers[i] ? weights[j] : 0;
+            if (before < wanted && wanted <= before + weights[i]) a.tokens[r] = numbers[i];
+        }
+    } else {
+        cuts(row);
+        // Sums of groups of up to 4 tiles, a wave each; then a wave for each tile of the group that the random number meets
+        const int group = tiles >= 4 * waves ? 4 : tiles >= 2 * waves ? 2 : 1, groups = (tiles + group - 1) / group;
+        // a logit that is not kept is taken as one that weighs nothing
+        const auto weigh = [&](const float(&e)[kEach], int v, uint64_t (&x)[kEach]) {
+            bool keep[kEach];
+            cut.keeps(e, v, keep);
 #pragma unroll
-            for (int j = 0; j < kEach; ++j) {
-                const uint64_t x = w.fixed(e[j]);
-                sum += cut.keeps(e[j], v + j) ? x : 0;
+            for (int j = 0; j < kEach; ++j) x[j] = w.fixed_up(keep[j] && e[j] >= w.floor ? e[j] : w.floor);
+            if (w.floor == -FLT_MAX) { // at the greatest temperatures every logit weighs something
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) x[j] = keep[j] ? x[j] : kFixedBase;
             }
-            sum = wave_scan(sum);
+        };
+        for (int i = wave; i < groups; i += waves) {
+            uint64_t sum = 0;
+            auto next = row.raw(i * group * kTile + lane * kEach);
+#pragma unroll 1
+            for (int t = 0; t < group; ++t) {
+                const int v = (i * group + t) * kTile + lane * kEach;
+                float e[kEach];
+                uint64_t x[kEach];
+                row.values(next, e);
+                if (t + 1 < group) next = row.raw(v + kTile);
+                weigh(e, v, x);
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) sum += x[j];
+            }
+            sum = wave_scan(sum - (uint64_t)(group * kEach) * kFixedBase);
             if (lane == 63) s.bins[i] = sum;
         }
         __syncthreads();
-        uint64_t wanted = 0;
-        all = find(s, tiles, [&](uint64_t sum) { return wanted = wanted_of(u, sum); });
-        if (wave == 0) {
+        find(s, groups, [&](uint64_t sum) { return wanted_of(u, sum); });
+        all = s.all;
+        const uint64_t wanted = s.wanted;
+        uint64_t x[kEach], sum = 0, upto = 0;
+        const int v = (s.place * group + wave) * kTile + lane * kEach;
+        if (wave < group) {
             float e[kEach];
-            const int v = row.tile(s.place, e);
-            uint64_t x[kEach], sum = 0;
+            row.values(row.raw(v), e);
+            weigh(e, v, x);
 #pragma unroll
-            for (int j = 0; j < kEach; ++j) {
-                x[j] = w.fixed(e[j]);
-                x[j] = cut.keeps(e[j], v + j) ? x[j] : 0;
-                sum += x[j];
-            }
-            uint64_t before = s.before + wave_scan(sum) - sum;
+            for (int j = 0; j < kEach; ++j) sum += x[j] -= kFixedBase;
+            upto = wave_scan(sum);
+            if (lane == 63) s.wave_sum[wave] = upto;
+        }
+        __syncthreads();
+        if (wave < group) {
+            uint64_t before = s.before + upto - sum;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) before += i < wave ? s.wave_sum[i] : 0;
             if (before < wanted && wanted <= before + sum) {
 #pragma unroll
                 for (int j = 0; j < kEach; ++j) {
@@ -545,17 +742,18 @@ template <class T, class P, int STAGE> __global__ __launch_bounds__(64 * kWaves)
         float e[kEach];
         const int v = row.tile(tile, e);
         out_t y;
-        bool some = false;
+        bool keep[kEach], some = false;
+        cut.keeps(e, v, keep);
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             y[i] = (P)0.0f;
-            some = some || cut.keeps(e[i], v + i);
+            some = some || keep[i];
         }
         if (some) {
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
                 const float x = (float)(w.exact(e[i]) * share);
-                y[i] = (P)(cut.keeps(e[i], v + i) ? x : 0.0f);
+                y[i] = (P)(keep[i] ? x : 0.0f);
             }
         }
         return y;
@@ -564,10 +762,10 @@ template <class T, class P, int STAGE> __global__ __launch_bounds__(64 * kWaves)
 
 template <class T, class P> void launch(const SampleArgs &k, hipStream_t stream)
 {
-    const int tiles = (k.vocabulary + kTile - 1) / kTile, threads = 64 * (tiles < kWaves ? tiles : kWaves);
+    const int tiles = (k.vocabulary + kTile - 1) / kTile, most = k.rows > 256 ? kWaves / 2 : kWaves, threads = 64 * (tiles < most ? tiles : most);
     const dim3 grid((unsigned)k.rows);
-    if (k.rows > 256 || tiles * kTile * sizeof(T) <= 52 << 10) sample_kernel<T, P, 52 << 10><<<grid, threads, 0, stream>>>(k);
-    else sample_kernel<T, P, 128 << 10><<<grid, threads, 0, stream>>>(k);
+    if (k.rows > 256 || tiles * kTile * sizeof(T) <= 43 << 10) sample_kernel<T, P, 43 << 10><<<grid, threads, 0, stream>>>(k);
+    else sample_kernel<T, P, 120 << 10><<<grid, threads, 0, stream>>>(k);
 }
 
 } // namespace
