@@ -154,6 +154,9 @@ template <class T> struct Eight {
     }
 };
 
+// The wave's number as a scalar, so that branches on its tiles are
+__device__ __forceinline__ int wave_of_block() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
 // A row of logits.  Its first `staged` tokens (a multiple of kTile) are in LDS, -inf behind the last one; the others are read again in every pass.
 template <class T> struct Row {
     const T *x;
@@ -168,36 +171,28 @@ template <class T> struct Row {
         if (infinite) return x == INFINITY ? 0.0f : -INFINITY;
         return x;
     }
-    __device__ typename Eight<T>::values_t raw(int v) const
-    {
-        return v < staged ? *reinterpret_cast<const typename Eight<T>::values_t *>(stage + v) : Eight<T>::load(x, v, vocabulary);
-    }
-    // the lane's logits of tile t; returns the first one's token
+    // the lane's logits of tile t, a scalar; returns the first one's token
     __device__ int tile(int t, float (&out)[kEach]) const
     {
         const int v = t * kTile + (threadIdx.x & 63) * kEach;
-        values(raw(v), out);
-        return v;
-    }
-    __device__ void values(const typename Eight<T>::values_t &e, float (&out)[kEach]) const
-    {
+        typename Eight<T>::values_t e;
+        if (t * kTile < staged) e = *reinterpret_cast<const typename Eight<T>::values_t *>(stage + v);
+        else e = Eight<T>::load(x, v, vocabulary);
 #pragma unroll
         for (int i = 0; i < kEach; ++i) out[i] = (float)e[i];
         if (infinite) {
 #pragma unroll
             for (int i = 0; i < kEach; ++i) out[i] = out[i] == INFINITY ? 0.0f : -INFINITY;
         }
+        return v;
     }
     // f(logits, first token) for the wave's tiles
     template <class F> __device__ void tiles(const F &f) const
     {
-        const int step = (blockDim.x >> 6) * kTile;
-        int v = (threadIdx.x >> 6) * kTile + (threadIdx.x & 63) * kEach;
-        auto next = raw(v);
-        for (int end = v - (threadIdx.x & 63) * kEach; end < vocabulary; end += step, v += step) {
+        const int waves = blockDim.x >> 6;
+        for (int t = wave_of_block(); t * kTile < vocabulary; t += waves) {
             float e[kEach];
-            values(next, e);
-            if (end + step < vocabulary) next = raw(v + step);
+            const int v = tile(t, e);
             f(e, v);
         }
     }
@@ -378,7 +373,7 @@ template <class S> __device__ Cut select(Shared &s, const S &source, const Weigh
     if constexpr (kListed) listed = source.count;
     uint32_t low = s.low, high = s.high, key = 0;
     bool numbers = false; // of the tokens with `key`
-    for (;;) {
+    while (low <= high) {
         if (low == high) {
             if (numbers) return Cut{logit_of(key), (int)low};
             key = low;
@@ -415,6 +410,7 @@ template <class S> __device__ Cut select(Shared &s, const S &source, const Weigh
         high = end < high ? end : high;
         __syncthreads();
     }
+    return cut; // not reached: the bin holds tokens
 }
 
 // Candidates of a small top-k.  The k-th best of the greatest logits of groups of tokens leaves k tokens before it at least, and few more where k is small beside the
@@ -550,7 +546,7 @@ template <class T, class P, int STAGE> __global__ __launch_bounds__(64 * kWaves)
 {
     __shared__ Shared s;
     __shared__ __attribute__((aligned(16))) T stage[STAGE / sizeof(T)];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, V = a.vocabulary, tiles = (V + kTile - 1) / kTile;
+    const int lane = threadIdx.x & 63, wave = wave_of_block(), waves = blockDim.x >> 6, V = a.vocabulary, tiles = (V + kTile - 1) / kTile;
     constexpr int kStaged = STAGE / (int)sizeof(T) / kTile * kTile;
     const int64_t r = blockIdx.x;
     Row<T> row{static_cast<const T *>(a.logits) + r * a.stride, stage, tiles * kTile < kStaged ? tiles * kTile : kStaged, V, false};
@@ -617,10 +613,11 @@ template <class T, class P, int STAGE> __global__ __launch_bounds__(64 * kWaves)
     // From a rate on the next logit below the greatest weighs 2^-512, nothing by any measure: a greater one would only take exponents out of their range
     const double next = (double)most - (double)logit_of(key_of(most) + 1);
     if (w.rate * next > 0x1p18 && next < (double)FLT_MAX) w.rate = 0x1p18 / next;
-    const double floor = (double)most - kSteps * (a.unit + 4) / w.rate;
+    const double octave = kSteps / w.rate; // in logits
+    const double floor = (double)most - (a.unit + 4) * octave;
     w.floor = floor >= -(double)FLT_MAX ? (float)floor : -FLT_MAX;
     if ((double)w.floor > floor) w.floor = w.floor > -FLT_MAX ? logit_of(key_of(w.floor) + 1) : -FLT_MAX;
-    const double far = (double)most - kSteps * 161 / w.rate;
+    const double far = (double)most - 161 * octave;
     w.far = far >= -(double)FLT_MAX ? (float)far : -FLT_MAX;
     if ((double)w.far > far) w.far = w.far > -FLT_MAX ? logit_of(key_of(w.far) + 1) : -FLT_MAX;
     const Even even{most, fmaxf(fminf((float)(w.rate * ((double)kBinsPerOctave / kSteps)), 1e30f), 1e-30f)};
@@ -693,14 +690,11 @@ template <class T, class P, int STAGE> __global__ __launch_bounds__(64 * kWaves)
         };
         for (int i = wave; i < groups; i += waves) {
             uint64_t sum = 0;
-            auto next = row.raw(i * group * kTile + lane * kEach);
 #pragma unroll 1
             for (int t = 0; t < group; ++t) {
-                const int v = (i * group + t) * kTile + lane * kEach;
                 float e[kEach];
                 uint64_t x[kEach];
-                row.values(next, e);
-                if (t + 1 < group) next = row.raw(v + kTile);
+                const int v = row.tile(i * group + t, e);
                 weigh(e, v, x);
 #pragma unroll
                 for (int j = 0; j < kEach; ++j) sum += x[j];
@@ -713,10 +707,10 @@ template <class T, class P, int STAGE> __global__ __launch_bounds__(64 * kWaves)
         all = s.all;
         const uint64_t wanted = s.wanted;
         uint64_t x[kEach], sum = 0, upto = 0;
-        const int v = (s.place * group + wave) * kTile + lane * kEach;
+        int v = 0;
         if (wave < group) {
             float e[kEach];
-            row.values(row.raw(v), e);
+            v = row.tile(__builtin_amdgcn_readfirstlane(s.place) * group + wave, e);
             weigh(e, v, x);
 #pragma unroll
             for (int j = 0; j < kEach; ++j) sum += x[j] -= kFixedBase;
