@@ -8,8 +8,258 @@ namespace apgemv {
 
 namespace {
 
+typedef float float16_t __attribute__((ext_vector_type(16)));
+typedef float float2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+
+constexpr int kWaveRows = 32;
+constexpr int kTileRows = kWaveRows * kWaves; // query rows of a workgroup
+constexpr int kTileKeys = 64;                 // keys in LDS, 16 from each wave
+constexpr int kPageKeys = 64 * 16;            // keys whose pages a wave holds
+// Weights are 2^7 e^(..): up to 2^15, and above the subnormal numbers of binary16 down to 2^-21 of the greatest
+constexpr float kRaise = 7.0f;
+
+// A tile of keys and values in LDS, as operands of v_mfma_f32_32x32x16_f16: 16 bytes per lane (column or row c = lane % 32, half h = lane / 32).
+// Keys: per block of 32 keys and part of 16 channels, key c's channels 8 h .. of the part.  Values: per 16 keys and block of 32 channels, channel c of keys
+// 4 h .. and 8 + 4 h ..  Padded so that neither the writers, who hold a key's or a chunk's channels, nor the readers meet a bank twice as often as they must.
+template <int D> struct Staged {
+    static constexpr int kParts = D / 16, kBlocks = D / 32, kN = D / 16; // kN: channels of a chunk
+    static constexpr int kPart = 64 * 16 + 32, kChunk = kN * 16 + 16, kHalf = 32 / kN * kChunk;
+    static constexpr int kKeyBytes = 2 * kParts * kPart, kValueBytes = 4 * kBlocks * 2 * kHalf;
+    static constexpr int kBytes = kKeyBytes + kValueBytes + kTileKeys * 4; // and the keys' (low, step) pairs
+    static constexpr int kSums = kTileRows * (D + 4) * 4;                   // the rows' sums, at the end
+    __device__ static int key(int block, int part, int h, int c) { return (block * kParts + part) * kPart + (h * 32 + c) * 16; }
+    __device__ static int value(int keys16, int block, int h, int c) { return kKeyBytes + ((keys16 * kBlocks + block) * 2 + h) * kHalf + c / kN * kChunk + c % kN * 16; }
+    __device__ static int pair(int t) { return kKeyBytes + kValueBytes + t * 4; }
+};
+
+// What a wave loads of a tile: 16 keys.  A lane has a quarter of key lane / 4's codes, chunk lane % 16 of the values of quad lane / 16 and that quad's pairs.
+template <int D> struct Raw {
+    typedef uint32_t words_t __attribute__((ext_vector_type(D / 32)));
+    words_t k, v;
+    uint4_t vp;
+    uint32_t kp; // key lane's, of the first 16 lanes
+};
+
+// The keys of a prefix for 128 rows of one key head: codes become operands once for all four waves.
+template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prefix_kernel(const SharedArgs a)
+{
+    typedef CacheLayout<D> L;
+    typedef Staged<D> T;
+    constexpr int kMost = 2 * T::kBytes > T::kSums ? 2 * T::kBytes : T::kSums;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kMost];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
+    const int kv = a.cache.kv_heads, group = a.heads / kv, head = blockIdx.x % kv, rest = blockIdx.x / kv, item = rest % a.prefix_items, split = rest / a.prefix_items;
+    Item it;
+    if (!find_prefix_item(a, kTileRows, item, &it)) return;
+    const int prefix = it.sequence, n = it.tokens, length = __builtin_amdgcn_readfirstlane(it.length), c0 = split * a.prefix_chunk;
+    if (split > 0 && length <= c0) return;
+    const int c1 = length < c0 + a.prefix_chunk ? length : c0 + a.prefix_chunk;
+
+    const int row = it.tile * kTileRows + wave * kWaveRows + c, token = row / group;
+    const bool valid = token < n;
+    half8_t q[T::kParts];
+    float q_sum = 0;
+    {
+        const _Float16 *p = a.q + (int64_t)(it.begin + (valid ? token : 0)) * a.q_token + (int64_t)(head * group + (valid ? row - token * group : 0)) * a.q_head + 8 * h;
+#pragma unroll
+        for (int i = 0; i < T::kParts; ++i) {
+            half8_t x = *reinterpret_cast<const half8_t *>(p + 16 * i);
+            if (a.scale < 0) x = -x;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) q_sum += (float)x[j];
+            q[i] = half8_t{x[0], x[4], x[1], x[5], x[2], x[6], x[3], x[7]}; // the order that codes come in
+        }
+        q_sum += __shfl_xor(q_sum, 32);
+        q_sum *= kCodeUnit;
+    }
+    const float scale = fabsf(a.scale) * kLog2e;
+    float16_t o[T::kBlocks];
+#pragma unroll
+    for (int b = 0; b < T::kBlocks; ++b)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[b][j] = 0;
+    float m = -INFINITY, l = 0;
+
+    // pages of 16 keys each, from `piece` on, and of the next piece
+    const auto pages_of = [&](int from) {
+        const int t = from + 16 * lane;
+        const int page = t < c1 ? a.prefix_tables[(int64_t)prefix * a.prefix_width + (t >> a.cache.log_page)] : -1;
+        return (int64_t)page < a.cache.pages ? page : -1;
+    };
+    int piece = c0, pages = pages_of(c0), later = pages_of(c0 + kPageKeys);
+    const int lp = a.cache.log_page, page_mask = (1 << lp) - 1;
+    // the tile's 16 keys of the wave; which of its four 16 keys are in the cache
+    const auto load = [&](int key, int *known) {
+        if (key - piece == kPageKeys) {
+            piece = key;
+            pages = later;
+            later = pages_of(piece + kPageKeys);
+        }
+        const int at = (key - piece) >> 4;
+        *known = (int)(__ballot(pages >= 0) >> at) & 15;
+        const int page = __builtin_amdgcn_readlane(pages, at + wave), t = (key + 16 * wave) & page_mask;
+        const uint8_t *section = L::block(a.cache, page < 0 ? 0 : page, head);
+        uintptr_t codes_at = reinterpret_cast<uintptr_t>(section + t * L::kRow), pairs_at = reinterpret_cast<uintptr_t>(section + (D << lp) + 4 * t);
+        asm("" : "+s"(codes_at), "+s"(pairs_at));
+        typedef const __attribute__((address_space(1))) uint8_t *global_t;
+        typedef typename Raw<D>::words_t words_t;
+        const global_t codes = (global_t)codes_at, pairs = (global_t)pairs_at;
+        Raw<D> r;
+        r.k = *(const __attribute__((address_space(1))) words_t *)(codes + lane * (D / 8));
+        r.v = *(const __attribute__((address_space(1))) words_t *)(codes + (L::kRow << lp) + lane * (D / 8));
+        r.vp = *(const __attribute__((address_space(1))) uint4_t *)(pairs + (4 << lp) + (lane >> 4) * 16);
+        r.kp = *(const __attribute__((address_space(1))) uint32_t *)(pairs + (lane & 15) * 4);
+        return r;
+    };
+    const uint32_t key_mask = in_vector(0x000f000fu), value_bits = in_vector(0x64006400u);
+    const auto stage = [&](uint8_t *to, const Raw<D> &r, int key, int known) {
+        const int of = lane >> 2, quarter = lane & 3;
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) {
+            const int eight = quarter * (D / 32) + j;
+            *reinterpret_cast<half8_t *>(to + T::key(wave >> 1, eight >> 1, eight & 1, (wave & 1) * 16 + of)) = key_operand(r.k[j], key_mask);
+        }
+        if (lane < 16) *reinterpret_cast<uint32_t *>(to + T::pair(16 * wave + lane)) = r.kp;
+        // values: low + step * code rounded once; 0 for keys that are not there
+        const int quad = lane >> 4, chunk = lane & 15, first = key + 16 * wave + 4 * quad;
+        const bool there = known >> wave & 1;
+        half2_t low[2], step[2];
+        bool over = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t pair = there && first + i < c1 ? r.vp[i] : 0;
+            low[i >> 1][i & 1] = low_of(pair);
+            step[i >> 1][i & 1] = step_of(pair);
+            over = over || (float)low_of(pair) + 15.0f * (float)step_of(pair) > 65504.0f;
+        }
+        constexpr int kH = D / 64;
+        uint8_t *const at = to + T::value(wave, chunk / (512 / D), quad & 1, chunk % (512 / D) * T::kN) + (quad >> 1) * 8;
+        const bool clamp = __any(over);
+#pragma unroll
+        for (int i = 0; i < T::kN; ++i) {
+            uint2_t x;
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                const half2_t code = __builtin_bit_cast(half2_t, r.v[p * kH + i / 4] >> 4 * (i & 3) & key_mask | value_bits) - half2_t{1024, 1024};
+                half2_t y = __builtin_elementwise_fma(code, step[p], low[p]);
+                if (clamp) { // 15 steps may pass the end of binary16 by the rounding of the step
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) y[e] = y[e] > (_Float16)65504 ? (_Float16)65504 : y[e];
+                }
+                x[p] = __builtin_bit_cast(uint32_t, y);
+            }
+            *reinterpret_cast<uint2_t *>(at + 16 * i) = x;
+        }
+    };
+
+    int known = 0, next_known = 0;
+    if (c0 < c1) {
+        const Raw<D> r = load(c0, &known);
+        stage(lds, r, c0, known);
+    }
+#pragma unroll 1
+    for (int key = c0, turn = 0; key < c1; key += kTileKeys, turn ^= 1) {
+        __syncthreads(); // this tile is there, the other one is free
+        const bool more = key + kTileKeys < c1;
+        Raw<D> r;
+        if (more) r = load(key + kTileKeys, &next_known);
+        const uint8_t *const tile = lds + turn * T::kBytes;
+        float16_t s[2];
+#pragma unroll
+        for (int i = 0; i < T::kParts; ++i)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const half8_t x = *reinterpret_cast<const half8_t *>(tile + T::key(b, i, h, c));
+                s[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, q[i], i == 0 ? float16_t{} : s[b], 0, 0, 0);
+            }
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const uint4_t pairs = *reinterpret_cast<const uint4_t *>(tile + T::pair(32 * b + 8 * g + 4 * h));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[b][4 * g + e] = __builtin_fmaf((float)step_of(pairs[e]), s[b][4 * g + e], times(low_of(pairs[e]), q_sum));
+            }
+        if (known != 15 || key + kTileKeys > c1) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (!(known >> (2 * b + (g >> 1)) & 1) || key + 32 * b + 8 * g + 4 * h + e >= c1) s[b][4 * g + e] = -INFINITY;
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) top = fmaxf(top, s[b][j]);
+        if (__any(top - m > a.slack)) { // also from -inf; a sum could round a difference of large scores away
+            const float next = fmaxf(m, fmaxf(top, __shfl_xor(top, 32))), keep = next == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - next) * scale);
+            m = next;
+            l *= keep;
+#pragma unroll
+            for (int b = 0; b < T::kBlocks; ++b) o[b] *= keep;
+        }
+        const float from = m == -INFINITY ? 0.0f : m;
+        float base = from * scale - kRaise;
+        if (__any(fabsf(base) > kFar)) { // the rounding of the product would be part of the exponent
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s[b][j] -= from;
+            base = -kRaise;
+        }
+        half8_t p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+                const float2_t x = {__builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 1][8 * (i & 1) + j], scale, -base)),
+                                    __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 1][8 * (i & 1) + j + 1], scale, -base))};
+                const half2_t y = __builtin_convertvector(x, half2_t);
+                l = __builtin_amdgcn_fdot2(y, half2_t{1, 1}, l, false); // the weights as they are used
+                p[i][j] = y[0];
+                p[i][j + 1] = y[1];
+            }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int b = 0; b < T::kBlocks; ++b) {
+                const half8_t x = *reinterpret_cast<const half8_t *>(tile + T::value(i, b, h, c));
+                o[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, p[i], o[b], 0, 0, 0);
+            }
+        if (more) {
+            stage(lds + (turn ^ 1) * T::kBytes, r, key + kTileKeys, next_known);
+            known = next_known;
+        }
+    }
+
+    // the rows' sums, in whole lines: through LDS, a wave its own rows
+    constexpr float kLower = 0.0078125f; // 2^-kRaise
+    l = (l + __shfl_xor(l, 32)) * kLower;
+    __syncthreads();
+    float *const sums = reinterpret_cast<float *>(lds) + wave * kWaveRows * (D + 4);
+#pragma unroll
+    for (int b = 0; b < T::kBlocks; ++b)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<float4_t *>(sums + c * (D + 4) + 32 * b + 8 * g + 4 * h) = float4_t{o[b][4 * g], o[b][4 * g + 1], o[b][4 * g + 2], o[b][4 * g + 3]} * kLower;
+    const int64_t range = (int64_t)(a.splits + split) * a.tokens * a.heads;
+    const auto place_of = [&](int r, int t) { return range + (int64_t)(it.begin + t) * a.heads + head * group + (r - t * group); };
+    if (valid && h == 0) a.stat[place_of(row, token)] = make_float2(m, l);
+    __syncthreads();
+#pragma unroll 4
+    for (int i = 0; i < kWaveRows * D / 256; ++i) {
+        const int at = i * 64 + lane, r = at / (D / 4), channel = at % (D / 4) * 4, of = it.tile * kTileRows + wave * kWaveRows + r, t = of / group;
+        if (t < n) *reinterpret_cast<float4_t *>(a.part + place_of(of, t) * D + channel) = *reinterpret_cast<const float4_t *>(sums + r * (D + 4) + channel);
+    }
+}
+
 struct Plan {
-    int rows; // 16-row tiles per workgroup
+    int rows;  // 16-row tiles per workgroup
+    bool wide; // a prefix's rows in tiles of 128, in a launch of their own
     int64_t items, prefix_items;
     int chunk, prefix_chunk, splits, prefix_splits;
 };
@@ -23,6 +273,23 @@ Plan plan_of(const ap_cache &c, const ap_shared &a)
     const auto items_of = [&](int64_t tile) { return o.q_starts ? o.tokens * group / tile + o.sequences : (each * group + tile - 1) / tile * o.sequences; };
     const auto prefix_items_of = [&](int64_t tile) { return a.prefixes > 0 ? o.tokens * group / tile + a.prefixes : 0; };
     const int64_t prefix_rows = a.prefixes > 0 ? (o.tokens + a.prefixes - 1) / a.prefixes * group : 0;
+    const auto round_up = [](int64_t x, int64_t to) { return (int)((x + to - 1) / to * to); };
+    p.wide = prefix_rows > 32;
+    if (p.wide) {
+        p.rows = each * group <= 16 && longest / kPiece * items_of(16) * c.kv_heads < 1 << 20 ? 1 : 2;
+        p.items = items_of(16 * p.rows);
+        p.prefix_items = prefix_items_of(kTileRows);
+        const int64_t units = p.items * c.kv_heads, prefix_units = p.prefix_items * c.kv_heads;
+        int64_t chunk = (longest * units + 511) / 512, prefix_chunk = (longest_prefix * prefix_units + 511) / 512;
+        if (p.rows == 1 && chunk > kPiece) chunk = kPiece;
+        chunk = chunk < 2 * kStep ? 2 * kStep : chunk;
+        prefix_chunk = prefix_chunk < 4 * kTileKeys ? 4 * kTileKeys : prefix_chunk;
+        p.chunk = round_up(chunk < longest ? chunk : longest, kStep);
+        p.prefix_chunk = round_up(prefix_chunk < longest_prefix ? prefix_chunk : longest_prefix, kTileKeys);
+        p.splits = (int)((longest + p.chunk - 1) / p.chunk);
+        p.prefix_splits = (int)((longest_prefix + p.prefix_chunk - 1) / p.prefix_chunk);
+        return p;
+    }
     p.rows = each * group <= 16 && prefix_rows <= 16 && most / kPiece * (items_of(16) + prefix_items_of(16)) * c.kv_heads < 1 << 20 ? 1 : 2;
     p.items = items_of(16 * p.rows);
     p.prefix_items = prefix_items_of(16 * p.rows);
@@ -31,9 +298,8 @@ Plan plan_of(const ap_cache &c, const ap_shared &a)
     int64_t chunk = (keys + 511) / 512;
     if (p.rows == 1 && chunk > kPiece) chunk = kPiece;
     if (chunk < 2 * kStep) chunk = 2 * kStep;
-    const auto round_up = [](int64_t x) { return (int)((x + kStep - 1) / kStep * kStep); };
-    p.chunk = round_up(chunk < longest ? chunk : longest);
-    p.prefix_chunk = round_up(chunk < longest_prefix ? chunk : longest_prefix);
+    p.chunk = round_up(chunk < longest ? chunk : longest, kStep);
+    p.prefix_chunk = round_up(chunk < longest_prefix ? chunk : longest_prefix, kStep);
     p.splits = (int)((longest + p.chunk - 1) / p.chunk);
     p.prefix_splits = a.prefixes > 0 ? (int)((longest_prefix + p.prefix_chunk - 1) / p.prefix_chunk) : 0;
     return p;
@@ -68,7 +334,13 @@ hipError_t launch_attention_shared(const ap_cache &c, const ap_shared &a, hipStr
     k.prefix_width = a.prefix_width;
     k.prefixes = a.prefixes, k.max_prefix = (int)a.max_prefix;
     k.prefix_items = (int)p.prefix_items, k.prefix_splits = p.prefix_splits, k.prefix_chunk = p.prefix_chunk;
-    const dim3 grid((unsigned)((p.items * p.splits + p.prefix_items * p.prefix_splits) * c.kv_heads)), join((unsigned)(o.tokens * o.heads));
+    if (p.wide) {
+        const dim3 grid((unsigned)(p.prefix_items * p.prefix_splits * c.kv_heads));
+        if (c.head_dim == 64) attention_prefix_kernel<64><<<grid, kThreads, 0, stream>>>(k);
+        else attention_prefix_kernel<128><<<grid, kThreads, 0, stream>>>(k);
+        k.prefix_items = 0; // of the launch below
+    }
+    const dim3 grid((unsigned)((p.items * p.splits + (int64_t)k.prefix_items * p.prefix_splits) * c.kv_heads)), join((unsigned)(o.tokens * o.heads));
     if (c.head_dim == 64) {
         if (p.rows == 1) attention_cached_kernel<64, 1, true><<<grid, kThreads, 0, stream>>>(k);
         else attention_cached_kernel<64, 2, true><<<grid, kThreads, 0, stream>>>(k);
