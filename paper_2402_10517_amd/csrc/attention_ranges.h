@@ -55,6 +55,7 @@ struct SharedArgs : CachedArgs {
     int64_t prefix_width;
     int prefixes, max_prefix;
     int prefix_items, prefix_splits, prefix_chunk;
+    bool wide; // the prefixes' rows are in tiles of their own (attention_shared.hip)
 };
 
 // The sequence and row tile of an item (64 lanes call together); false: there are fewer.  Where sequences have different numbers of tokens a lane
@@ -214,7 +215,13 @@ template <int D> __device__ __forceinline__ bf8_t value_operand(const Half<D> (&
 
 template <bool SHARED> using RangeArgs = std::conditional_t<SHARED, SharedArgs, CachedArgs>;
 
-template <int D, int NR, bool SHARED> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 64 ? 4 : 3 : 2) void attention_cached_kernel(const RangeArgs<SHARED> a)
+// The waves' sums of a row tile, where they meet
+template <int D> struct RangeSums {
+    float sums[kWaves][16][D + 4];
+    float4_t stats[kWaves][16];
+};
+
+template <int D, int NR, bool SHARED> __device__ __forceinline__ void attend_ranges(const RangeArgs<SHARED> &a, int block, RangeSums<D> &lds)
 {
     typedef CacheLayout<D> L;
     constexpr int kSteps = D / 32;    // products of 32 channels per score
@@ -222,13 +229,13 @@ template <int D, int NR, bool SHARED> __global__ __launch_bounds__(kThreads, NR 
     constexpr int kRows = 16 * NR;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
     const int kv = a.cache.kv_heads, group = a.heads / kv;
-    const int head = blockIdx.x % kv, rest = blockIdx.x / kv;
+    const int head = block % kv, rest = block / kv;
     int item, split, chunk = a.chunk, most = a.max_length, range;
     const int32_t *tables = a.tables;
     int64_t width = a.table_width;
     bool whole_prefix = false; // an item of a prefix: every row sees all keys
     if constexpr (SHARED) {
-        const int groups = a.prefix_items * a.prefix_splits; // the prefixes' come first: they are the longest
+        const int groups = a.wide ? 0 : a.prefix_items * a.prefix_splits; // the prefixes' come first: they are the longest
         whole_prefix = rest < groups;
         const int at = whole_prefix ? rest : rest - groups, items = whole_prefix ? a.prefix_items : a.items;
         item = at % items, split = at / items;
@@ -415,8 +422,8 @@ template <int D, int NR, bool SHARED> __global__ __launch_bounds__(kThreads, NR 
     }
 
     // join the waves: all sums to the common maximum, then every thread takes D / 16 channels of a row
-    __shared__ float sums[kWaves][16][D + 4];
-    __shared__ float4_t stats[kWaves][16];
+    auto &sums = lds.sums;
+    auto &stats = lds.stats;
     const int row_of = threadIdx.x >> 4, chunk_of = threadIdx.x & 15;
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
@@ -462,6 +469,12 @@ template <int D, int NR, bool SHARED> __global__ __launch_bounds__(kThreads, NR 
             }
         }
     }
+}
+
+template <int D, int NR, bool SHARED> __global__ __launch_bounds__(kThreads, NR == 1 ? D == 64 ? 4 : 3 : 2) void attention_cached_kernel(const RangeArgs<SHARED> a)
+{
+    __shared__ RangeSums<D> lds;
+    attend_ranges<D, NR, SHARED>(a, blockIdx.x, lds);
 }
 
 // Joins the ranges of a row that sees more than one: D / 4 lanes take every kParts-th range with a running maximum, and one in kParts of the

@@ -18,20 +18,30 @@ constexpr int kTileKeys = 64;                 // keys in LDS, 16 from each wave
 constexpr int kPageKeys = 64 * 16;            // keys whose pages a wave holds
 // Weights are 2^7 e^(..): up to 2^15, and above the subnormal numbers of binary16 down to 2^-21 of the greatest
 constexpr float kRaise = 7.0f;
+// instruction classes of the scheduler's groups
+constexpr int kProducts = 0x8, kLdsReads = 0x100;
 
-// A tile of keys and values in LDS, as operands of v_mfma_f32_32x32x16_f16: 16 bytes per lane (column or row c = lane % 32, half h = lane / 32).
-// Keys: per block of 32 keys and part of 16 channels, key c's channels 8 h .. of the part.  Values: per 16 keys and block of 32 channels, channel c of keys
-// 4 h .. and 8 + 4 h ..  Padded so that neither the writers, who hold a key's or a chunk's channels, nor the readers meet a bank twice as often as they must.
+// A tile of keys and values in LDS, as operands of v_mfma_f32_32x32x16_f16: 16 bytes per lane (column or row c = lane % 32, half h = lane / 32), in the order of the
+// lanes, so that reads meet every bank once.  Keys: per block of 32 keys and part of 16 channels, key c's channels 8 h .. of the part; padded between parts for those
+// who write.  Values: per 16 keys and block of 32 channels, channel c of keys 4 h .. and 8 + 4 h ..
 template <int D> struct Staged {
     static constexpr int kParts = D / 16, kBlocks = D / 32, kN = D / 16; // kN: channels of a chunk
-    static constexpr int kPart = 64 * 16 + 32, kChunk = kN * 16 + 16, kHalf = 32 / kN * kChunk;
-    static constexpr int kKeyBytes = 2 * kParts * kPart, kValueBytes = 4 * kBlocks * 2 * kHalf;
+    static constexpr int kPart = 64 * 16 + 32;
+    static constexpr int kKeyBytes = 2 * kParts * kPart, kValueBytes = 4 * kBlocks * 64 * 16;
     static constexpr int kBytes = kKeyBytes + kValueBytes + kTileKeys * 4; // and the keys' (low, step) pairs
     static constexpr int kSums = kTileRows * (D + 4) * 4;                   // the rows' sums, at the end
     __device__ static int key(int block, int part, int h, int c) { return (block * kParts + part) * kPart + (h * 32 + c) * 16; }
-    __device__ static int value(int keys16, int block, int h, int c) { return kKeyBytes + ((keys16 * kBlocks + block) * 2 + h) * kHalf + c / kN * kChunk + c % kN * 16; }
+    __device__ static int value(int keys16, int block, int h, int c) { return kKeyBytes + ((keys16 * kBlocks + block) * 64 + h * 32 + c) * 16; }
     __device__ static int pair(int t) { return kKeyBytes + kValueBytes + t * 4; }
 };
+
+// A barrier for LDS alone: loads from memory stay in flight
+__device__ __forceinline__ void lds_barrier()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
 
 // What a wave loads of a tile: 16 keys.  A lane has a quarter of key lane / 4's codes, chunk lane % 16 of the values of quad lane / 16 and that quad's pairs.
 template <int D> struct Raw {
@@ -42,14 +52,12 @@ template <int D> struct Raw {
 };
 
 // The keys of a prefix for 128 rows of one key head: codes become operands once for all four waves.
-template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prefix_kernel(const SharedArgs a)
+template <int D> __device__ __forceinline__ void attend_prefix(const SharedArgs &a, int block, uint8_t *lds)
 {
     typedef CacheLayout<D> L;
     typedef Staged<D> T;
-    constexpr int kMost = 2 * T::kBytes > T::kSums ? 2 * T::kBytes : T::kSums;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[kMost];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
-    const int kv = a.cache.kv_heads, group = a.heads / kv, head = blockIdx.x % kv, rest = blockIdx.x / kv, item = rest % a.prefix_items, split = rest / a.prefix_items;
+    const int kv = a.cache.kv_heads, group = a.heads / kv, head = block % kv, rest = block / kv, item = rest % a.prefix_items, split = rest / a.prefix_items;
     Item it;
     if (!find_prefix_item(a, kTileRows, item, &it)) return;
     const int prefix = it.sequence, n = it.tokens, length = __builtin_amdgcn_readfirstlane(it.length), c0 = split * a.prefix_chunk;
@@ -113,6 +121,11 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prefix
         return r;
     };
     const uint32_t key_mask = in_vector(0x000f000fu), value_bits = in_vector(0x64006400u);
+    // The lanes take the channels of their chunks in different orders, n ^ turned for n = 0, 1, ..: their writes then meet every bank equally often
+    const int turned = (lane & 15) / (D == 128 ? 2 : 4);
+    int shifts[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) shifts[i] = 4 * (i ^ (turned & 3));
     const auto stage = [&](uint8_t *to, const Raw<D> &r, int key, int known) {
         const int of = lane >> 2, quarter = lane & 3;
 #pragma unroll
@@ -123,47 +136,70 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prefix
         if (lane < 16) *reinterpret_cast<uint32_t *>(to + T::pair(16 * wave + lane)) = r.kp;
         // values: low + step * code rounded once; 0 for keys that are not there
         const int quad = lane >> 4, chunk = lane & 15, first = key + 16 * wave + 4 * quad;
-        const bool there = known >> wave & 1;
-        half2_t low[2], step[2];
-        bool over = false;
+        uint4_t pairs = r.vp;
+        if (known != 15 || key + kTileKeys > c1) {
+            int end = c1 - first, in = known >> wave & 1;
+            asm volatile("" : "+v"(end), "+s"(in)); // stays a branch: the compiler would select in every turn
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t pair = there && first + i < c1 ? r.vp[i] : 0;
-            low[i >> 1][i & 1] = low_of(pair);
-            step[i >> 1][i & 1] = step_of(pair);
-            over = over || (float)low_of(pair) + 15.0f * (float)step_of(pair) > 65504.0f;
+            for (int i = 0; i < 4; ++i) pairs[i] = in && i < end ? pairs[i] : 0;
         }
+        half2_t low[2], step[2], last[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            low[i] = half2_t{low_of(pairs[2 * i]), low_of(pairs[2 * i + 1])};
+            step[i] = half2_t{step_of(pairs[2 * i]), step_of(pairs[2 * i + 1])};
+            last[i] = __builtin_elementwise_fma(half2_t{15, 15}, step[i], low[i]);
+        }
+        const half2_t most = __builtin_elementwise_max(last[0], last[1]);
+        const bool over = most[0] > (_Float16)65504 || most[1] > (_Float16)65504;
         constexpr int kH = D / 64;
-        uint8_t *const at = to + T::value(wave, chunk / (512 / D), quad & 1, chunk % (512 / D) * T::kN) + (quad >> 1) * 8;
-        const bool clamp = __any(over);
+        const int at = T::value(wave, chunk / (512 / D), quad & 1, chunk % (512 / D) * T::kN + turned) + (quad >> 1) * 8;
+        uint32_t words[2][kH];
 #pragma unroll
-        for (int i = 0; i < T::kN; ++i) {
-            uint2_t x;
-#pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                const half2_t code = __builtin_bit_cast(half2_t, r.v[p * kH + i / 4] >> 4 * (i & 3) & key_mask | value_bits) - half2_t{1024, 1024};
-                half2_t y = __builtin_elementwise_fma(code, step[p], low[p]);
-                if (clamp) { // 15 steps may pass the end of binary16 by the rounding of the step
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) y[e] = y[e] > (_Float16)65504 ? (_Float16)65504 : y[e];
-                }
-                x[p] = __builtin_bit_cast(uint32_t, y);
+        for (int p = 0; p < 2; ++p) {
+            if constexpr (kH == 2) {
+                words[p][0] = turned & 4 ? r.v[2 * p + 1] : r.v[2 * p];
+                words[p][1] = turned & 4 ? r.v[2 * p] : r.v[2 * p + 1];
+            } else {
+                words[p][0] = r.v[p];
             }
-            *reinterpret_cast<uint2_t *>(at + 16 * i) = x;
+        }
+        const auto values = [&](const auto &last) {
+#pragma unroll
+            for (int i = 0; i < T::kN; ++i) {
+                uint2_t x;
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    const half2_t code = __builtin_bit_cast(half2_t, words[p][i / 4] >> shifts[i & 3] & key_mask | value_bits) - half2_t{1024, 1024};
+                    x[p] = __builtin_bit_cast(uint32_t, last(__builtin_elementwise_fma(code, step[p], low[p])));
+                }
+                *reinterpret_cast<uint2_t *>(to + (at ^ 16 * i)) = x;
+            }
+        };
+        if (__any(over)) { // 15 steps may pass the end of binary16 by the rounding of the step
+            asm volatile(""); // stays a branch: the compiler would take the greater of each value and its end, always
+            values([](half2_t y) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) y[e] = y[e] > (_Float16)65504 ? (_Float16)65504 : y[e];
+                return y;
+            });
+        } else {
+            values([](half2_t y) { return y; });
         }
     };
 
+    // Memory is asked for a tile two turns before its products, which leaves a turn for it to arrive; its codes become operands in the turn before, behind the
+    // products of the scores.  Behind the last tile it is asked for nothing new: what is loaded is not used.
     int known = 0, next_known = 0;
+    Raw<D> r;
     if (c0 < c1) {
-        const Raw<D> r = load(c0, &known);
+        r = load(c0, &known);
         stage(lds, r, c0, known);
+        r = load(c0 + kTileKeys, &next_known);
     }
 #pragma unroll 1
     for (int key = c0, turn = 0; key < c1; key += kTileKeys, turn ^= 1) {
-        __syncthreads(); // this tile is there, the other one is free
-        const bool more = key + kTileKeys < c1;
-        Raw<D> r;
-        if (more) r = load(key + kTileKeys, &next_known);
+        lds_barrier(); // this tile is there, the other one is free
         const uint8_t *const tile = lds + turn * T::kBytes;
         float16_t s[2];
 #pragma unroll
@@ -173,6 +209,19 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prefix
                 const half8_t x = *reinterpret_cast<const half8_t *>(tile + T::key(b, i, h, c));
                 s[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, q[i], i == 0 ? float16_t{} : s[b], 0, 0, 0);
             }
+        // operands kAhead reads ahead of their products
+        constexpr int kAhead = 6;
+        __builtin_amdgcn_sched_group_barrier(kLdsReads, kAhead, 0);
+#pragma unroll
+        for (int i = 0; i < 2 * T::kParts - kAhead; ++i) {
+            __builtin_amdgcn_sched_group_barrier(kProducts, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(kLdsReads, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(kProducts, kAhead, 0);
+        const int now = known;
+        stage(lds + (turn ^ 1) * T::kBytes, r, key + kTileKeys, next_known);
+        known = next_known;
+        r = load(key + 2 * kTileKeys, &next_known);
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -181,14 +230,16 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prefix
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[b][4 * g + e] = __builtin_fmaf((float)step_of(pairs[e]), s[b][4 * g + e], times(low_of(pairs[e]), q_sum));
             }
-        if (known != 15 || key + kTileKeys > c1) {
+        if (now != 15 || key + kTileKeys > c1) {
+            int end = c1 - key - 4 * h, there = now;
+            asm volatile("" : "+v"(end), "+s"(there)); // and so stays a branch
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int g = 0; g < 4; ++g)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (!(known >> (2 * b + (g >> 1)) & 1) || key + 32 * b + 8 * g + 4 * h + e >= c1) s[b][4 * g + e] = -INFINITY;
+                        if (!(there >> (2 * b + (g >> 1)) & 1) || 32 * b + 8 * g + e >= end) s[b][4 * g + e] = -INFINITY;
         }
         float top = s[0][0];
 #pragma unroll
@@ -230,10 +281,13 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prefix
                 const half8_t x = *reinterpret_cast<const half8_t *>(tile + T::value(i, b, h, c));
                 o[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, p[i], o[b], 0, 0, 0);
             }
-        if (more) {
-            stage(lds + (turn ^ 1) * T::kBytes, r, key + kTileKeys, next_known);
-            known = next_known;
+        __builtin_amdgcn_sched_group_barrier(kLdsReads, kAhead, 0);
+#pragma unroll
+        for (int i = 0; i < 4 * T::kBlocks - kAhead; ++i) {
+            __builtin_amdgcn_sched_group_barrier(kProducts, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(kLdsReads, 1, 0);
         }
+        __builtin_amdgcn_sched_group_barrier(kProducts, kAhead, 0);
     }
 
     // the rows' sums, in whole lines: through LDS, a wave its own rows
@@ -257,9 +311,19 @@ template <int D> __global__ __launch_bounds__(kThreads, 2) void attention_prefix
     }
 }
 
+// Both: workgroups of prefixes, then of the sequences' own keys, which wait for memory where the others wait for the matrix cores
+template <int D, int NR> __global__ __launch_bounds__(kThreads, 2) void attention_shared_kernel(const SharedArgs a)
+{
+    constexpr int kPrefix = 2 * Staged<D>::kBytes > Staged<D>::kSums ? 2 * Staged<D>::kBytes : Staged<D>::kSums, kOwn = sizeof(RangeSums<D>);
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kPrefix > kOwn ? kPrefix : kOwn];
+    const int groups = a.prefix_items * a.prefix_splits * a.cache.kv_heads;
+    if ((int)blockIdx.x < groups) attend_prefix<D>(a, blockIdx.x, lds);
+    else attend_ranges<D, NR, true>(a, blockIdx.x - groups, *reinterpret_cast<RangeSums<D> *>(lds));
+}
+
 struct Plan {
     int rows;  // 16-row tiles per workgroup
-    bool wide; // a prefix's rows in tiles of 128, in a launch of their own
+    bool wide; // a prefix's rows in tiles of 128
     int64_t items, prefix_items;
     int chunk, prefix_chunk, splits, prefix_splits;
 };
@@ -280,7 +344,7 @@ Plan plan_of(const ap_cache &c, const ap_shared &a)
         p.items = items_of(16 * p.rows);
         p.prefix_items = prefix_items_of(kTileRows);
         const int64_t units = p.items * c.kv_heads, prefix_units = p.prefix_items * c.kv_heads;
-        int64_t chunk = (longest * units + 511) / 512, prefix_chunk = (longest_prefix * prefix_units + 511) / 512;
+        int64_t chunk = (longest * units + 511) / 512, prefix_chunk = (longest_prefix * prefix_units + 255) / 256;
         if (p.rows == 1 && chunk > kPiece) chunk = kPiece;
         chunk = chunk < 2 * kStep ? 2 * kStep : chunk;
         prefix_chunk = prefix_chunk < 4 * kTileKeys ? 4 * kTileKeys : prefix_chunk;
@@ -334,20 +398,19 @@ hipError_t launch_attention_shared(const ap_cache &c, const ap_shared &a, hipStr
     k.prefix_width = a.prefix_width;
     k.prefixes = a.prefixes, k.max_prefix = (int)a.max_prefix;
     k.prefix_items = (int)p.prefix_items, k.prefix_splits = p.prefix_splits, k.prefix_chunk = p.prefix_chunk;
-    if (p.wide) {
-        const dim3 grid((unsigned)(p.prefix_items * p.prefix_splits * c.kv_heads));
-        if (c.head_dim == 64) attention_prefix_kernel<64><<<grid, kThreads, 0, stream>>>(k);
-        else attention_prefix_kernel<128><<<grid, kThreads, 0, stream>>>(k);
-        k.prefix_items = 0; // of the launch below
-    }
-    const dim3 grid((unsigned)((p.items * p.splits + (int64_t)k.prefix_items * p.prefix_splits) * c.kv_heads)), join((unsigned)(o.tokens * o.heads));
+    k.wide = p.wide;
+    const dim3 grid((unsigned)((p.items * p.splits + p.prefix_items * p.prefix_splits) * c.kv_heads)), join((unsigned)(o.tokens * o.heads));
+    const auto launch = [&](auto narrow, auto wide) {
+        if (p.wide) wide<<<grid, kThreads, 0, stream>>>(k);
+        else narrow<<<grid, kThreads, 0, stream>>>(k);
+    };
     if (c.head_dim == 64) {
-        if (p.rows == 1) attention_cached_kernel<64, 1, true><<<grid, kThreads, 0, stream>>>(k);
-        else attention_cached_kernel<64, 2, true><<<grid, kThreads, 0, stream>>>(k);
+        if (p.rows == 1) launch(attention_cached_kernel<64, 1, true>, attention_shared_kernel<64, 1>);
+        else launch(attention_cached_kernel<64, 2, true>, attention_shared_kernel<64, 2>);
         attention_join_kernel<64, true><<<join, kThreads, 0, stream>>>(k);
     } else {
-        if (p.rows == 1) attention_cached_kernel<128, 1, true><<<grid, kThreads, 0, stream>>>(k);
-        else attention_cached_kernel<128, 2, true><<<grid, kThreads, 0, stream>>>(k);
+        if (p.rows == 1) launch(attention_cached_kernel<128, 1, true>, attention_shared_kernel<128, 1>);
+        else launch(attention_cached_kernel<128, 2, true>, attention_shared_kernel<128, 2>);
         attention_join_kernel<128, true><<<join, kThreads, 0, stream>>>(k);
     }
     return hipGetLastError();
