@@ -55,8 +55,13 @@ struct SharedArgs : CachedArgs {
     int64_t prefix_width;
     int prefixes, max_prefix;
     int prefix_items, prefix_splits, prefix_chunk;
-    bool wide; // the prefixes' rows are in tiles of their own (attention_shared.hip)
+    // or the prefixes' rows are in tiles of kTileRows (attention_shared.hip), whose ranges are decided on the device: up to prefix_groups workgroups, whose
+    // sums lie behind those of the sequences' own keys
+    bool wide;
+    int prefix_groups;
+    int4 *shares; // of each prefix: its first workgroup, tiles, ranges
 };
+constexpr int kTileRows = 128;
 
 // The sequence and row tile of an item (64 lanes call together); false: there are fewer.  Where sequences have different numbers of tokens a lane
 // looks at one sequence, its length with it.
@@ -486,10 +491,13 @@ template <int D, bool SHARED> __global__ __launch_bounds__(kThreads) void attent
     const int64_t row = blockIdx.x, rows = (int64_t)a.tokens * a.heads;
     const float scale = fabsf(a.scale) * kLog2e;
     int own = 0, ranges = 0; // of its own keys, in all
+    int64_t sums_at = 0, sums_step = 0;
     // where range i of the row is: SHARED, the prefix's lie behind all sequences' own
     const auto place_of = [&](int i) {
-        if constexpr (SHARED) return (int64_t)(i < own ? i : i < ranges ? i - own + a.splits : 0) * rows + row;
-        else return (int64_t)(i < a.splits ? i : 0) * rows + row;
+        if constexpr (SHARED) {
+            if (i >= own && a.wide) return i < ranges ? sums_at + (int64_t)(i - own) * sums_step : row;
+            return (int64_t)(i < own ? i : i < ranges ? i - own + a.splits : 0) * rows + row;
+        } else return (int64_t)(i < a.splits ? i : 0) * rows + row;
     };
     const auto stat_of = [&](int i) { return a.stat[place_of(i)]; };
     const auto part_of = [&](int i) { return *reinterpret_cast<const float4_t *>(a.part + place_of(i) * D + lane * 4); };
@@ -505,9 +513,19 @@ template <int D, bool SHARED> __global__ __launch_bounds__(kThreads) void attent
         own = ranges = sees > a.chunk ? (sees + a.chunk - 1) / a.chunk : 1; // the first is there even where it holds no key
         const int p = a.prefixes > 0 ? sequence_of(a.prefix_starts, s, a.sequences, a.prefixes) : -1;
         if (p >= 0) {
+            int4 share;
+            if (a.wide) share = a.shares[p];
             prefix_tokens(a, p, &begin, &end);
-            const int length = prefix_length(a, p);
-            if (token >= begin && token < end) ranges += length > a.prefix_chunk ? (length + a.prefix_chunk - 1) / a.prefix_chunk : 1;
+            if (token < begin || token >= end) {
+            } else if (a.wide) {
+                const int kv = a.cache.kv_heads, group = a.heads / kv, head = (int)(row - (int64_t)token * a.heads), of = (int)(token - begin) * group + head % group;
+                ranges += share.z;
+                sums_at = a.splits * rows + ((int64_t)share.x + (int64_t)(of / kTileRows) * kv + head / group) * kTileRows + of % kTileRows;
+                sums_step = (int64_t)share.y * kv * kTileRows;
+            } else {
+                const int length = prefix_length(a, p);
+                ranges += length > a.prefix_chunk ? (length + a.prefix_chunk - 1) / a.prefix_chunk : 1;
+            }
         }
         st = stat_of(part), y = part_of(part);
     } else {

@@ -13,9 +13,17 @@ typedef float float2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 
 constexpr int kWaveRows = 32;
-constexpr int kTileRows = kWaveRows * kWaves; // query rows of a workgroup
+static_assert(kTileRows == kWaveRows * kWaves, "query rows of a workgroup");
 constexpr int kTileKeys = 64;                 // keys in LDS, 16 from each wave
 constexpr int kPageKeys = 64 * 16;            // keys whose pages a wave holds
+// The division of the prefixes among workgroups.  Steps (of 64 keys, for a tile of rows and a key head) of a workgroup, at least: us at 1 / 2 / 4, heads of 128,
+// 8 key heads: 96 rows over 2000 keys 22.1 / 19.1 / 20.4, 128 over 4096 25.7 / 25.7 / 23.5, over 8192 29.3 / 28.6 / 29.6.
+constexpr int kLeastSteps = 4;
+// Steps per CU from which on two workgroups for each share it, one at work while the other waits, at the price of twice as many sums.  us with one / two, 16 steps
+// (64 prefix rows of 16 prefixes, 2048 keys) 81.8 / 87.0, (256 rows, 16384 keys) 48.1 / 49.7; 32 steps (256 rows, 32768 keys) 68.9 / 66.1, (512, 16384) 76.4 / 74.7;
+// 64 steps (512, 32768) 123.3 / 111.4, 128 steps (1024, 32768) 232.7 / 205.6.
+constexpr int kStepsForTwo = 32;
+constexpr int kTried = 16; // prefixes
 // Weights are 2^7 e^(..): up to 2^15, and above the subnormal numbers of binary16 down to 2^-21 of the greatest
 constexpr float kRaise = 7.0f;
 // instruction classes of the scheduler's groups
@@ -51,18 +59,96 @@ template <int D> struct Raw {
     uint32_t kp; // key lane's, of the first 16 lanes
 };
 
+// What a workgroup does: a row tile of a prefix and key head, and a range of its keys
+struct Share {
+    Item item;
+    int head, from, to;
+};
+
+// The prefixes' tiles of keys (of 64, for each tile of rows and key head) are divided evenly among the workgroups that the card has room for: what they really hold is known
+// on the device alone.  (64 lanes call together.)  The first workgroup leaves for the join how.  False: there is nothing left for this one.
+__device__ __forceinline__ bool find_share(const SharedArgs &a, int block, Share *out)
+{
+    const int lane = threadIdx.x & 63, kv = a.cache.kv_heads, group = a.heads / kv;
+    struct Prefix {
+        int64_t begin, tokens;
+        int length, tiles, steps;
+    };
+    const auto prefix_of = [&](int first) {
+        Prefix x{0, 0, 0, 0, 0};
+        if (first + lane < a.prefixes) {
+            int64_t end;
+            x.length = prefix_length(a, first + lane);
+            prefix_tokens(a, first + lane, &x.begin, &end);
+            x.tokens = end - x.begin;
+            x.tiles = (int)((x.tokens * group + kTileRows - 1) / kTileRows);
+            x.steps = (x.length + kTileKeys - 1) / kTileKeys;
+        }
+        return x;
+    };
+    Prefix x = prefix_of(0);
+    int64_t steps = 0, units = 0;
+    for (int first = 0; first < a.prefixes; first += 64) {
+        if (first > 0) x = prefix_of(first);
+        int64_t s = (int64_t)x.tiles * kv * x.steps, u = x.steps > 0 ? (int64_t)x.tiles * kv : 0;
+        for (int m = 1; m < 64; m <<= 1) s += __shfl_xor(s, m), u += __shfl_xor(u, m);
+        steps += s;
+        units += u;
+    }
+    if (a.prefixes > 64) x = prefix_of(0);
+    // Each unit's last range may be short: with as many workgroups less there is no second round.  Few prefixes are tried at 64 lengths from there down.
+    const int64_t slots = steps >= 256 * kStepsForTwo ? 512 : 256, divided = units < slots / 2 ? slots - units : slots / 2, each = (steps + divided - 1) / divided,
+                  all = ((int64_t)a.max_prefix + kTileKeys - 1) / kTileKeys;
+    int chunk = (int)(each < kLeastSteps ? kLeastSteps : each > all ? all : each);
+    if (a.prefixes <= kTried && chunk > kLeastSteps) {
+        const int least = (int)((steps + slots - 1) / slots), from = least < kLeastSteps ? kLeastSteps : least;
+        if (from < chunk) {
+            const int mine = from + (int)((int64_t)(chunk - from) * lane >> 6);
+            int64_t groups = 0;
+            for (int i = 0; i < a.prefixes; ++i) groups += (int64_t)__builtin_amdgcn_readlane(x.tiles, i) * kv * ((__builtin_amdgcn_readlane(x.steps, i) + mine - 1) / mine);
+            const uint64_t fit = __ballot(groups <= slots);
+            if (fit) chunk = __builtin_amdgcn_readlane(mine, __builtin_ctzll(fit));
+        }
+    }
+    int before = 0;
+    bool found = false;
+    for (int first = 0; first < a.prefixes; first += 64) {
+        if (first > 0) x = prefix_of(first);
+        const int ranges = (x.steps + chunk - 1) / chunk, mine = x.tiles * kv * ranges;
+        int upto = mine;
+        for (int d = 1; d < 64; d <<= 1) {
+            const int other = __shfl_up(upto, d);
+            if (lane >= d) upto += other;
+        }
+        if (block == 0 && threadIdx.x < 64 && first + lane < a.prefixes) a.shares[first + lane] = make_int4(before + upto - mine, x.tiles, before + upto <= a.prefix_groups ? ranges : 0, 0);
+        const uint64_t here = __ballot(before + upto > block);
+        if (!found && here) {
+            found = true;
+            const int l = __builtin_ctzll(here), at = block - before - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l)),
+                      tiles = __builtin_amdgcn_readlane(x.tiles, l), rest = at / kv, split = rest / tiles, length = __builtin_amdgcn_readlane(x.length, l);
+            out->head = at - rest * kv;
+            out->item = Item{first + l, rest - split * tiles, __builtin_amdgcn_readlane((int)x.begin, l), __builtin_amdgcn_readlane((int)x.tokens, l), length};
+            out->from = split * chunk * kTileKeys;
+            out->to = length - out->from > (int64_t)chunk * kTileKeys ? out->from + chunk * kTileKeys : length;
+        }
+        // there are more than prefix_groups only where starts descend and prefixes overlap: those behind have no workgroup then
+        before += __builtin_amdgcn_readlane(upto, 63);
+        before = before < a.prefix_groups ? before : a.prefix_groups;
+    }
+    return found;
+}
+
 // The keys of a prefix for 128 rows of one key head: codes become operands once for all four waves.
 template <int D> __device__ __forceinline__ void attend_prefix(const SharedArgs &a, int block, uint8_t *lds)
 {
     typedef CacheLayout<D> L;
     typedef Staged<D> T;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
-    const int kv = a.cache.kv_heads, group = a.heads / kv, head = block % kv, rest = block / kv, item = rest % a.prefix_items, split = rest / a.prefix_items;
-    Item it;
-    if (!find_prefix_item(a, kTileRows, item, &it)) return;
-    const int prefix = it.sequence, n = it.tokens, length = __builtin_amdgcn_readfirstlane(it.length), c0 = split * a.prefix_chunk;
-    if (split > 0 && length <= c0) return;
-    const int c1 = length < c0 + a.prefix_chunk ? length : c0 + a.prefix_chunk;
+    Share share;
+    if (!find_share(a, block, &share)) return;
+    const Item it = share.item;
+    const int group = a.heads / a.cache.kv_heads, head = __builtin_amdgcn_readfirstlane(share.head), prefix = it.sequence, n = it.tokens,
+              c0 = __builtin_amdgcn_readfirstlane(share.from), c1 = __builtin_amdgcn_readfirstlane(share.to);
 
     const int row = it.tile * kTileRows + wave * kWaveRows + c, token = row / group;
     const bool valid = token < n;
@@ -300,14 +386,14 @@ template <int D> __device__ __forceinline__ void attend_prefix(const SharedArgs 
 #pragma unroll
         for (int g = 0; g < 4; ++g)
             *reinterpret_cast<float4_t *>(sums + c * (D + 4) + 32 * b + 8 * g + 4 * h) = float4_t{o[b][4 * g], o[b][4 * g + 1], o[b][4 * g + 2], o[b][4 * g + 3]} * kLower;
-    const int64_t range = (int64_t)(a.splits + split) * a.tokens * a.heads;
-    const auto place_of = [&](int r, int t) { return range + (int64_t)(it.begin + t) * a.heads + head * group + (r - t * group); };
-    if (valid && h == 0) a.stat[place_of(row, token)] = make_float2(m, l);
+    const int64_t place = (int64_t)a.splits * a.tokens * a.heads + (int64_t)block * kTileRows + wave * kWaveRows;
+    if (h == 0) a.stat[place + c] = make_float2(m, l);
     __syncthreads();
+    // rows that are not there as well: the join does not look at them
 #pragma unroll 4
     for (int i = 0; i < kWaveRows * D / 256; ++i) {
-        const int at = i * 64 + lane, r = at / (D / 4), channel = at % (D / 4) * 4, of = it.tile * kTileRows + wave * kWaveRows + r, t = of / group;
-        if (t < n) *reinterpret_cast<float4_t *>(a.part + place_of(of, t) * D + channel) = *reinterpret_cast<const float4_t *>(sums + r * (D + 4) + channel);
+        const int at = i * 64 + lane, r = at / (D / 4), channel = at % (D / 4) * 4;
+        *reinterpret_cast<float4_t *>(a.part + (place + r) * D + channel) = *reinterpret_cast<const float4_t *>(sums + r * (D + 4) + channel);
     }
 }
 
@@ -316,16 +402,20 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, 2) void attentio
 {
     constexpr int kPrefix = 2 * Staged<D>::kBytes > Staged<D>::kSums ? 2 * Staged<D>::kBytes : Staged<D>::kSums, kOwn = sizeof(RangeSums<D>);
     __shared__ __attribute__((aligned(16))) uint8_t lds[kPrefix > kOwn ? kPrefix : kOwn];
-    const int groups = a.prefix_items * a.prefix_splits * a.cache.kv_heads;
-    if ((int)blockIdx.x < groups) attend_prefix<D>(a, blockIdx.x, lds);
-    else attend_ranges<D, NR, true>(a, blockIdx.x - groups, *reinterpret_cast<RangeSums<D> *>(lds));
+    if ((int)blockIdx.x < a.prefix_groups) attend_prefix<D>(a, blockIdx.x, lds);
+    else attend_ranges<D, NR, true>(a, blockIdx.x - a.prefix_groups, *reinterpret_cast<RangeSums<D> *>(lds));
 }
 
 struct Plan {
     int rows;  // 16-row tiles per workgroup
     bool wide; // a prefix's rows in tiles of 128
-    int64_t items, prefix_items;
-    int chunk, prefix_chunk, splits, prefix_splits;
+    int64_t items, prefix_items = 0;
+    int chunk, prefix_chunk = 0, splits, prefix_splits = 0;
+    int64_t prefix_groups;
+    int64_t sums(const ap_shared &a) const // rows' sums in the workspace
+    {
+        return (int64_t)(splits + prefix_splits) * a.own.tokens * a.own.heads + prefix_groups * kTileRows;
+    }
 };
 
 Plan plan_of(const ap_cache &c, const ap_shared &a)
@@ -338,22 +428,25 @@ Plan plan_of(const ap_cache &c, const ap_shared &a)
     const auto prefix_items_of = [&](int64_t tile) { return a.prefixes > 0 ? o.tokens * group / tile + a.prefixes : 0; };
     const int64_t prefix_rows = a.prefixes > 0 ? (o.tokens + a.prefixes - 1) / a.prefixes * group : 0;
     const auto round_up = [](int64_t x, int64_t to) { return (int)((x + to - 1) / to * to); };
-    p.wide = prefix_rows > 32;
+    // Tiles of 128 rows read and prepare a key once where the others do so for every 32 rows, and wait longer before their first.  us with tiles of 32 / 128, 8 key
+    // heads of 128: 48 rows over 2000 keys 14.7 / 19.5, over 32768 36.1 / 39.4, 64 over 8192 22.8 / 23.4, 128 over 8192 28.0 / 28.3, over 32768 58.1 / 45.1,
+    // 256 over 1000 20.5 / 22.9, over 32768 92.0 / 65.6, 1024 over 8192 170.6 / 136.1.
+    p.wide = prefix_rows > 64;
     if (p.wide) {
         p.rows = each * group <= 16 && longest / kPiece * items_of(16) * c.kv_heads < 1 << 20 ? 1 : 2;
         p.items = items_of(16 * p.rows);
-        p.prefix_items = prefix_items_of(kTileRows);
-        const int64_t units = p.items * c.kv_heads, prefix_units = p.prefix_items * c.kv_heads;
-        int64_t chunk = (longest * units + 511) / 512, prefix_chunk = (longest_prefix * prefix_units + 255) / 256;
+        const int64_t units = p.items * c.kv_heads;
+        int64_t chunk = (longest * units + 511) / 512;
         if (p.rows == 1 && chunk > kPiece) chunk = kPiece;
         chunk = chunk < 2 * kStep ? 2 * kStep : chunk;
-        prefix_chunk = prefix_chunk < 4 * kTileKeys ? 4 * kTileKeys : prefix_chunk;
         p.chunk = round_up(chunk < longest ? chunk : longest, kStep);
-        p.prefix_chunk = round_up(prefix_chunk < longest_prefix ? prefix_chunk : longest_prefix, kTileKeys);
         p.splits = (int)((longest + p.chunk - 1) / p.chunk);
-        p.prefix_splits = (int)((longest_prefix + p.prefix_chunk - 1) / p.prefix_chunk);
+        // at most as many workgroups as find_share divides the prefixes among: slots, and a short range of each row tile and key head
+        const int64_t prefix_units = prefix_items_of(kTileRows) * c.kv_heads, ranges = (longest_prefix + kLeastSteps * kTileKeys - 1) / (kLeastSteps * kTileKeys);
+        p.prefix_groups = ranges * prefix_units < 512 + prefix_units ? ranges * prefix_units : 512 + prefix_units;
         return p;
     }
+    p.prefix_groups = 0;
     p.rows = each * group <= 16 && prefix_rows <= 16 && most / kPiece * (items_of(16) + prefix_items_of(16)) * c.kv_heads < 1 << 20 ? 1 : 2;
     p.items = items_of(16 * p.rows);
     p.prefix_items = prefix_items_of(16 * p.rows);
@@ -374,7 +467,7 @@ Plan plan_of(const ap_cache &c, const ap_shared &a)
 size_t attention_shared_work(const ap_cache &c, const ap_shared &a)
 {
     const Plan p = plan_of(c, a);
-    return (size_t)(p.splits + p.prefix_splits) * a.own.tokens * a.own.heads * (c.head_dim * sizeof(float) + sizeof(float2));
+    return (size_t)p.sums(a) * (c.head_dim * sizeof(float) + sizeof(float2)) + (p.wide ? a.prefixes * sizeof(int4) + 16 : 0);
 }
 
 hipError_t launch_attention_shared(const ap_cache &c, const ap_shared &a, hipStream_t stream)
@@ -393,13 +486,14 @@ hipError_t launch_attention_shared(const ap_cache &c, const ap_shared &a, hipStr
     k.slack = kSlack / (fabsf(k.scale) * kLog2e);
     k.out = static_cast<_Float16 *>(o.out);
     k.part = static_cast<float *>(o.work);
-    k.stat = reinterpret_cast<float2 *>(k.part + (size_t)(p.splits + p.prefix_splits) * o.tokens * o.heads * c.head_dim);
+    k.stat = reinterpret_cast<float2 *>(k.part + p.sums(a) * c.head_dim);
+    k.shares = reinterpret_cast<int4 *>((reinterpret_cast<uintptr_t>(k.stat + p.sums(a)) + 15) & ~(uintptr_t)15);
     k.prefix_starts = a.prefix_starts, k.prefix_lengths = a.prefix_lengths, k.prefix_tables = a.prefix_tables;
     k.prefix_width = a.prefix_width;
     k.prefixes = a.prefixes, k.max_prefix = (int)a.max_prefix;
     k.prefix_items = (int)p.prefix_items, k.prefix_splits = p.prefix_splits, k.prefix_chunk = p.prefix_chunk;
-    k.wide = p.wide;
-    const dim3 grid((unsigned)((p.items * p.splits + p.prefix_items * p.prefix_splits) * c.kv_heads)), join((unsigned)(o.tokens * o.heads));
+    k.wide = p.wide, k.prefix_groups = (int)p.prefix_groups;
+    const dim3 grid((unsigned)((p.items * p.splits + p.prefix_items * p.prefix_splits) * c.kv_heads + p.prefix_groups)), join((unsigned)(o.tokens * o.heads));
     const auto launch = [&](auto narrow, auto wide) {
         if (p.wide) wide<<<grid, kThreads, 0, stream>>>(k);
         else narrow<<<grid, kThreads, 0, stream>>>(k);

@@ -220,7 +220,7 @@ def test_values_at_the_end_of_the_range(B, sequences):
     shared_case(B, [400], [sequences], [2] * sequences, [1] * sequences, 4, 2, 128, 16, spoil=small)
 
 
-@pytest.mark.parametrize("sequences", [1, 30])
+@pytest.mark.parametrize("sequences", [1, 30, 70])
 def test_pages_outside_the_cache_hold_nothing(B, sequences):
     G, D, page = 2, 128, 16
     cache = B.KVCache(4, G, D, page_tokens=page)
@@ -252,6 +252,38 @@ def test_starts_that_make_no_sense(B):
     call([0, 3, 6], q_starts=int32([0, 1, 2, 3, 4, 5, 70]), out=out)
     assert close(out[:3], good[:3]) and close(out[3:5], alone[3:5]) and (out[5:] == 7).all()
     call([0, 3, 6], q_starts=int32([-9, 5, 2, 2 ** 31 - 1, -2 ** 31, 6, 6]), out=out)
+
+
+def test_starts_that_make_no_sense_with_many_rows(B):
+    n = 40
+    cache, prefix_table, table, k, v = filled(B, [300, 700, 90], [20] * n, 2, 64, 16, 5)
+    q, own = normal(1, n, 16, 64), int32([20] * n)
+    call = lambda starts, **kw: B.ap_attention_shared(cache, q, prefix_table, int32([300, 700, 90]), table, own, prefix_starts=int32(starts), **kw)  # noqa: E731
+    alone = B.ap_attention_cached(cache, q, table, own)
+    close = lambda a, b: (a.float() - b.float()).abs().max() <= 2.0 ** -9 * b.abs().max()  # noqa: E731
+    for starts in ([0, -1, 2 ** 31 - 1, 0], [70, 70, 90, 90], [-5, -3, -1, -1], [3, 3, 3, 3]):
+        assert close(call(starts), alone), starts
+    good = call([0, 10, 30, 40])
+    assert not close(good, alone)
+    assert close(call([0, 10, 30, 41])[:30], good[:30])
+    assert torch.isfinite(call([0, 40, 0, 40])).all()           # prefixes that overlap
+    out = torch.full_like(q, 7.0)
+    call([0, 10, 30, 40], q_starts=int32(list(range(n)) + [70]), out=out)
+    assert close(out[:30], good[:30]) and close(out[30:-1], alone[30:-1]) and (out[-1] == 7).all()
+    # more of overlapping prefixes than there are workgroups for
+    many = 300
+    tables, lengths = prefix_table[:1].expand(many, -1).contiguous(), int32([300] * many)
+    q, own, table = normal(2, many * 3, 44, 64), int32([20] * many * 3), table[:1].expand(many * 3, -1).contiguous()
+    starts = [0] + [many * 3 if i % 2 else 0 for i in range(1, many)] + [many * 3]
+    out = B.ap_attention_shared(cache, q, tables, lengths, table, own, prefix_starts=int32(starts))
+    assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_many_row_tiles_and_prefixes(B, D):
+    # more tiles than workgroups, and prefixes of every share of them: none, one range, several
+    shared_case(B, [0, 64, 2000, 1, 129, 3000], [3, 30, 4, 90, 1, 60], [1 + i % 7 for i in range(188)], [1 + i % 3 for i in range(188)], 24, 2, D, 16)
+    shared_case(B, [70] * 20, [9] * 20, [1 + i % 7 for i in range(180)], [1] * 180, 32, 4, D, 32)
 
 
 def test_offsets_beyond_32_bits(B):
