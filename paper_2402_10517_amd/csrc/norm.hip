@@ -1,7 +1,12 @@
 // The norms around a block of a decoder layer, fused with the block's gate, scale and residual.
 //
+// r = residual + scale * gate * norm(x) (the norm of the block's output only with `post`), out = norm(r); norm(v) = weight * (v - mean) / sqrt(mean square + eps) + bias.
+//
 // A workgroup holds a row in registers, `PER` chunks of 8 columns per thread: each input is read and each output written once, and the norm after the
-// residual needs no second pass over memory. Bound by HBM; a single row by its launch, its loads and a reduction per norm.
+// residual needs no second pass over memory.  Large ones are bound by HBM: 8192 x 8192 with a post norm, a gate per value and a binary32 residual 170 us (940 MB, 5.5 TB/s),
+// with no post norm, binary16, 101 us (537 MB, 5.3 TB/s).  Smaller ones are bound by what a row does one after the other, of which a CU has two or three at a time: loads
+// from HBM, two sums over the workgroup for a centred norm and one for another, weights from the L2, stores.  1531 x 5121 centred with a post norm 30 us (63 MB, 2.1 TB/s); the
+// rows' odd starts are 5 us of that.  One row of 4096: 4.4 us, a launch that does nothing 3.5.
 #include "decode_device.h"
 
 namespace apgemv {
@@ -18,6 +23,7 @@ struct NormArgs {
     int64_t tokens;
     int columns, post, centred;
     float scale, eps;
+    double each; // 1 / columns
 };
 
 constexpr int kEach = 8; // adjacent columns of a chunk
@@ -53,28 +59,53 @@ template <bool TAIL, class T> __device__ __forceinline__ void store(T *row, int 
         if (c + i < columns) row[c + i] = e.x[i];
 }
 
-// The sum over the workgroup, the same bits in all threads.  `place` alternates, so that one barrier is enough.
-__device__ __forceinline__ double block_sum(double x, double *place)
+// x of the lane that a data-parallel primitive names, 0 without one
+template <int CTRL, int ROWS> __device__ __forceinline__ double moved(double x)
 {
-    for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
-    if (blockDim.x == 64) return x;
-    if ((threadIdx.x & 63) == 0) place[threadIdx.x >> 6] = x;
+    const uint64_t bits = __builtin_bit_cast(uint64_t, x);
+    const uint32_t low = __builtin_amdgcn_update_dpp(0, (int)bits, CTRL, ROWS, 0xf, true), high = __builtin_amdgcn_update_dpp(0, (int)(bits >> 32), CTRL, ROWS, 0xf, true);
+    return __builtin_bit_cast(double, (uint64_t)high << 32 | low);
+}
+
+__device__ __forceinline__ double from_lane(double x, int lane)
+{
+    const uint64_t bits = __builtin_bit_cast(uint64_t, x);
+    const uint32_t low = __builtin_amdgcn_readlane((int)bits, lane), high = __builtin_amdgcn_readlane((int)(bits >> 32), lane);
+    return __builtin_bit_cast(double, (uint64_t)high << 32 | low);
+}
+
+// The sum over the workgroup, the same bits in all threads.  `place` alternates, so that one barrier is enough.
+template <int WAVES> __device__ __forceinline__ double block_sum(double x, double *place)
+{
+    x += moved<0x111, 0xf>(x); // row_shr:1, 2, 4, 8: lane 15 of each row has the row's
+    x += moved<0x112, 0xf>(x);
+    x += moved<0x114, 0xf>(x);
+    x += moved<0x118, 0xf>(x);
+    x += moved<0x142, 0xa>(x); // row_bcast:15, 31: lane 63 has all
+    x += moved<0x143, 0xc>(x);
+    const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+    if (waves == 1) return from_lane(x, 63);
+    if (lane == 63) place[threadIdx.x >> 6] = x;
     __syncthreads();
-    x = 0;
-    for (int w = 0; w < (int)(blockDim.x >> 6); ++w) x += place[w];
-    return x;
+    const int of = lane & (WAVES - 1);
+    x = of < waves ? place[of] : 0;
+    x += moved<0x111, 0xf>(x);
+    x += moved<0x112, 0xf>(x);
+    if constexpr (WAVES > 4) x += moved<0x114, 0xf>(x);
+    if constexpr (WAVES > 8) x += moved<0x118, 0xf>(x);
+    return from_lane(x, WAVES - 1);
 }
 
 // The square of a sum's range: sums of squares beyond it are taken again of values times 2^-64 or 2^64
 constexpr float kLeastSum = 0x1p-80f, kMostSum = 0x1p120f;
 
 // TAIL: the last chunk of a row is not whole
-template <class R, int PER, bool POST, bool CENTRED, bool TAIL> __global__ __launch_bounds__(1024) void norm_kernel(const NormArgs a)
+template <class R, int THREADS, int PER, bool TAIL> __global__ __launch_bounds__(THREADS) void norm_kernel(const NormArgs a)
 {
     __shared__ double places[2][16];
-    constexpr bool LATE = PER >= 4; // registers do not hold all of a wide row's inputs
+    constexpr bool LATE = THREADS * PER > 2048; // registers do not hold all of a wide row's inputs
     int turn = 0;
-    const auto sum = [&](double x) { return block_sum(x, places[turn++ & 1]); };
+    const auto sum = [&](double x) { return block_sum<THREADS / 64>(x, places[turn++ & 1]); };
     const int columns = a.columns, first = threadIdx.x * kEach, step = blockDim.x * kEach;
     for (int64_t row = blockIdx.x; row < a.tokens; row += gridDim.x) {
         float v[PER][kEach]; // 0 in columns that do not exist
@@ -84,20 +115,29 @@ template <class R, int PER, bool POST, bool CENTRED, bool TAIL> __global__ __lau
             asm("" : "+v"(n));
             return n;
         };
+        // 0 in the columns that chunk p does not have
+        const auto cut = [&](int p) {
+            int n = left(p);
+            if (n >= (TAIL ? kEach : 1)) return;
+            asm volatile("" : "+v"(n)); // stays a branch
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) v[p][i] = TAIL && i < n ? v[p][i] : 0.0f;
+        };
         // normalises v: sums of up to 8 (the mean) or 32 values in binary32, of those in binary64.  The mean may be far above the differences from it: 48 bits.
         const auto norm = [&](const _Float16 *weight, const _Float16 *bias) {
-            if constexpr (CENTRED) {
+            asm("" : "+s"(weight), "+s"(bias)); // not in registers for the next row
+            if (a.centred) {
                 double s = 0;
 #pragma unroll
                 for (int p = 0; p < PER; ++p)
                     s += (double)(((v[p][0] + v[p][1]) + (v[p][2] + v[p][3])) + ((v[p][4] + v[p][5]) + (v[p][6] + v[p][7])));
-                const double mean = sum(s) / columns;
+                const double mean = sum(s) * a.each;
                 const float high = (float)mean, low = (float)(mean - (double)high);
 #pragma unroll
                 for (int p = 0; p < PER; ++p) {
-                    const int n = TAIL ? left(p) : left(p) > 0 ? kEach : 0;
 #pragma unroll
-                    for (int i = 0; i < kEach; ++i) v[p][i] = i < n ? (v[p][i] - high) - low : 0.0f;
+                    for (int i = 0; i < kEach; ++i) v[p][i] = (v[p][i] - high) - low;
+                    cut(p);
                 }
             }
             const auto squares = [&](float by) {
@@ -108,17 +148,26 @@ template <class R, int PER, bool POST, bool CENTRED, bool TAIL> __global__ __lau
                     for (int i = 0; i < kEach; ++i) s = __builtin_fmaf(v[p][i] * by, v[p][i] * by, s);
                 return sum((double)s);
             };
-            double mean = squares(1.0f);
+            float s = 0;
+#pragma unroll
+            for (int p = 0; p < PER; ++p)
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) s = __builtin_fmaf(v[p][i], v[p][i], s);
+            double mean = sum((double)s);
             if (mean > (double)kMostSum) mean = squares(0x1p-64f) * 0x1p128;
             else if (mean < (double)kLeastSum) mean = squares(0x1p64f) * 0x1p-128;
-            const double inverse = 1.0 / sqrt(mean / columns + (double)a.eps);
-            // as two factors, of which neither leaves binary32 where their product does not
-            const float f = (float)__builtin_sqrt(inverse);
-            const float g = f > 0 ? (float)(inverse / (double)f) : 0.0f; // of a row with an infinity 0: its finite values become 0
+            mean = mean * a.each + (double)a.eps;
+            // 1 / sqrt as two factors, an inverse root of 1/4 .. 1 (to 1 ulp) and a power of two, of which neither leaves binary32.  Of a row with an infinity both are 0
+            // and its finite values become 0.
+            const int power = (__builtin_amdgcn_frexp_exp(mean) + 1) >> 1;
+            const bool finite = mean < (double)INFINITY;
+            const float f = finite ? __builtin_amdgcn_rsqf((float)__builtin_ldexp(mean, -2 * power)) : mean == (double)INFINITY ? 0.0f : NAN,
+                        g = finite ? __builtin_ldexpf(1.0f, -power) : f;
 #pragma unroll
             for (int p = 0; p < PER; ++p) {
                 const int c = first + p * step;
                 if (c < columns) {
+                    if (LATE) asm volatile("" ::: "memory");
                     Eight<_Float16> w, b;
 #pragma unroll
                     for (int i = 0; i < kEach; ++i) w.x[i] = (_Float16)1, b.x[i] = (_Float16)0;
@@ -149,27 +198,25 @@ template <class R, int PER, bool POST, bool CENTRED, bool TAIL> __global__ __lau
 #pragma unroll
                 for (int i = 0; i < kEach; ++i) v[p][i] = there ? x[p][i] : 0.0f;
             }
-            if constexpr (POST) norm(a.post_weight, a.post_bias);
+            if (a.post) norm(a.post_weight, a.post_bias);
         }
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
             const int c = first + p * step;
             if (c < columns) {
+                if (LATE) asm volatile("" ::: "memory"); // a chunk's after the one before
                 if (LATE && a.residual) r[p] = load<TAIL>(from, c, columns);
                 if (LATE && a.gate) g[p] = load<TAIL>(a.gate + row * a.gate_stride, c, columns);
                 Eight<R> y;
-                const int n = TAIL ? left(p) : left(p) > 0 ? kEach : 0;
 #pragma unroll
                 for (int i = 0; i < kEach; ++i) {
                     const float gated = a.gate ? v[p][i] * g[p][i] : v[p][i];
                     y.x[i] = !a.x ? r[p].x[i] : (R)(a.residual ? __builtin_fmaf(a.scale, gated, r[p][i]) : a.scale * gated);
-                    v[p][i] = i < n ? (float)y.x[i] : 0.0f;
+                    v[p][i] = (float)y.x[i];
                 }
                 if (a.residual_out) store<TAIL>(to, c, columns, y);
-            } else {
-#pragma unroll
-                for (int i = 0; i < kEach; ++i) v[p][i] = 0;
             }
+            cut(p);
         }
         if (!a.out) continue;
         norm(a.weight, a.bias);
@@ -186,25 +233,19 @@ template <class R, int PER, bool POST, bool CENTRED, bool TAIL> __global__ __lau
     }
 }
 
-template <class R, int PER, bool TAIL> void launch(const NormArgs &k, int threads, hipStream_t stream)
-{
-    const dim3 grid((unsigned)(k.tokens < 1 << 20 ? k.tokens : 1 << 20));
-    if (k.post) {
-        if (k.centred) norm_kernel<R, PER, true, true, TAIL><<<grid, threads, 0, stream>>>(k);
-        else norm_kernel<R, PER, true, false, TAIL><<<grid, threads, 0, stream>>>(k);
-    } else {
-        if (k.centred) norm_kernel<R, PER, false, true, TAIL><<<grid, threads, 0, stream>>>(k);
-        else norm_kernel<R, PER, false, false, TAIL><<<grid, threads, 0, stream>>>(k);
-    }
-}
-
 template <class R, bool TAIL> void launch(const NormArgs &k, hipStream_t stream)
 {
     const int chunks = (k.columns + kEach - 1) / kEach;
+    const dim3 grid((unsigned)(k.tokens < 1 << 20 ? k.tokens : 1 << 20));
     const auto threads = [&](int per) { return (chunks + 64 * per - 1) / (64 * per) * 64; };
-    if (chunks <= 1024) launch<R, 1, TAIL>(k, threads(1), stream);
-    else if (chunks <= 2048) launch<R, 2, TAIL>(k, threads(2), stream);
-    else launch<R, 4, TAIL>(k, threads(4), stream);
+    // A chunk per thread up to 8192 columns, as a row's time is that of its loads, sums and stores one after the other; of more rows than CUs with a binary16 residual two
+    // (three workgroups of 8192 columns on a CU instead of two).  us with one / two, binary16 residual, 8192 columns: 256 rows 6.1 / 6.6, 1024 19.5 / 17.1, 8192
+    // 106 / 101, with a centred post norm 170 / 132; 4096 columns, 4096 rows 27.1 / 28.9; binary32 residual, 8192 x 8192 140 / 148, with a post norm and a gate 170 / 181.
+    if (chunks <= 256) norm_kernel<R, 256, 1, TAIL><<<grid, threads(1), 0, stream>>>(k);
+    else if (sizeof(R) == 2 && chunks > 512 && chunks <= 1024 && k.tokens > 256) norm_kernel<R, 512, 2, TAIL><<<grid, threads(2), 0, stream>>>(k);
+    else if (chunks <= 1024) norm_kernel<R, 1024, 1, TAIL><<<grid, threads(1), 0, stream>>>(k);
+    else if (chunks <= 2048) norm_kernel<R, 1024, 2, TAIL><<<grid, threads(2), 0, stream>>>(k);
+    else norm_kernel<R, 1024, 4, TAIL><<<grid, threads(4), 0, stream>>>(k);
 }
 
 template <class R> void launch(const NormArgs &k, hipStream_t stream)
@@ -227,7 +268,7 @@ hipError_t launch_norm(const ap_normed &a, hipStream_t stream)
     k.weight = static_cast<const _Float16 *>(a.weight), k.bias = static_cast<const _Float16 *>(a.bias);
     k.post_weight = static_cast<const _Float16 *>(a.post_weight), k.post_bias = static_cast<const _Float16 *>(a.post_bias);
     k.tokens = a.tokens, k.columns = (int)a.columns, k.post = a.post, k.centred = a.centred;
-    k.scale = a.scale, k.eps = a.eps;
+    k.scale = a.scale, k.eps = a.eps, k.each = 1.0 / (double)(a.columns > 0 ? a.columns : 1);
     if (a.half) launch<_Float16>(k, stream);
     else launch<float>(k, stream);
     return hipGetLastError();

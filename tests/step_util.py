@@ -47,8 +47,8 @@ def shared_attention(q, k, v, scale, sees, low_k, low_v):
 def norm(v, weight, bias, eps, centred):
     """64-bit norm of rows, and the bound of the kernel's error against it where the rows are exact.
 
-    Sums over a row: a mean of squares from binary32 sums of up to 32 products is off by 33 EPS32 of itself, the inverse of its root by half of that; two factors of the
-    inverse, two products and the sum with the bias round once each.  A mean is off by 4 EPS32 of the mean magnitude, and so is each difference from it, whose
+    Sums over a row: a mean of squares from binary32 sums of up to 32 products is off by 33 EPS32 of itself, the inverse of its root by half of that; its rounding to
+    binary32 is half an EPS32 more, the inverse root 2 (one in the last place), and a product and the sum with the bias round once each.  A mean is off by 4 EPS32 of the mean magnitude, and so is each difference from it, whose
     square adds twice the relative error."""
     v = v.double()
     slack = torch.zeros_like(v[:, :1])

@@ -84,6 +84,15 @@ def test_columns(B, columns, centred, half):
     norm_case(B, None, residual, w, centred=centred)
 
 
+@pytest.mark.parametrize("half", [False, True])
+@pytest.mark.parametrize("centred", [False, True])
+@pytest.mark.parametrize("tokens,columns", [(256, 4104), (257, 4096), (257, 4097), (257, 4104), (300, 5121), (261, 6201), (258, 8192)])
+def test_many_rows_of_many_columns(B, tokens, columns, centred, half):
+    x, r = normal(columns, tokens, columns), normal(1, tokens, columns, size=3, dtype=torch.float16 if half else torch.float32)
+    w, b, pw, pb = (normal(i, columns) for i in range(2, 6))
+    norm_case(B, x, r, w, b, pw, pb, normal(6, tokens, columns), centred=centred)
+
+
 @pytest.mark.parametrize("tokens", [1, 2, 5, 64, 300, 2049])
 @pytest.mark.parametrize("half", [False, True])
 def test_tokens(B, tokens, half):
