@@ -226,7 +226,7 @@ struct Shared {
     uint64_t before, amount, all, wanted;
     float wave_most[kWaves];
     uint32_t low, high;
-    int count, place, kept;
+    int count, place, kept, zeroed;
 };
 
 // Where in the sum of kept weights a uniform number draws: the first token up to which they reach it.  At least 1, at most the sum.
@@ -322,7 +322,7 @@ struct Even {
 //
 // The tokens of the even bin that reaches it are listed.  Their interval of keys is divided into bins until one key is left; where it has more tokens than
 // are wanted, an interval of token numbers is, for the first ones.  A bin that holds more than the list is looked for in the row.
-template <class S> __device__ Cut select(Shared &s, const S &source, const Weights &w, const Cut cut, const Even even, bool weigh, int count, float p)
+template <class S> __device__ __forceinline__ Cut select(Shared &s, const S &source, const Weights &w, const Cut cut, const Even even, bool weigh, int count, float p)
 {
     constexpr bool kListed = std::is_same_v<S, List>;
     clear_bins(s);
@@ -415,7 +415,7 @@ template <class S> __device__ Cut select(Shared &s, const S &source, const Weigh
 
 // Candidates of a small top-k.  The k-th best of the greatest logits of groups of tokens leaves k tokens before it at least, and few more where k is small beside the
 // groups: those are listed.  Groups are the tokens of a lane (groups = false: of 1024) or 8 adjacent ones.  Returns their number, -1 where the place is not to be had.
-template <class T> __device__ int candidates(Shared &s, const Row<T> &row, const Even even, float lane_most, int k, bool groups)
+template <class T> __device__ __forceinline__ int candidates(Shared &s, const Row<T> &row, const Even even, float lane_most, int k, bool groups)
 {
     const auto top_of = [](const float(&e)[kEach]) {
         float top = e[0];
@@ -467,7 +467,7 @@ template <class T> __device__ int candidates(Shared &s, const Row<T> &row, const
 // Ranks the n listed tokens among each other.  *token, and the kept ones' *cut and the sum of their weights.
 //
 // The sum of the weights ahead of a token is that over all others: their number is divided among the waves, whose parts meet in LDS.
-__device__ void rank(Shared &s, const Weights &w, int n, int k, float p, float least, float u, int64_t *token, Cut *cut, uint64_t *all)
+__device__ __forceinline__ void rank(Shared &s, const Weights &w, int n, int k, float p, float least, float u, int64_t *token, Cut *cut, uint64_t *all)
 {
     const uint64_t *const orders = reinterpret_cast<const uint64_t *>(s.list); // (token, key): the key is the high half
     uint64_t *const weights = s.bins, *const aheads = s.bins + kRanked;
@@ -572,6 +572,7 @@ template <class T, class P, int STAGE> __global__ __launch_bounds__(64 * kWaves)
     for (int m = 1; m < 16; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
 
     P *const kept = a.probabilities ? static_cast<P *>(a.probabilities) + r * V : nullptr;
+    typedef typename Eight<P>::values_t out_t;
     const auto write = [&](const auto &probability) {
         if (!kept) return;
 #pragma unroll 1
@@ -580,7 +581,15 @@ template <class T, class P, int STAGE> __global__ __launch_bounds__(64 * kWaves)
             Eight<P>::store(kept, v, V, probability(tile, v));
         }
     };
-    typedef typename Eight<P>::values_t out_t;
+    // Where few tokens can be kept all probabilities are 0 first, while the search goes on, and those of the kept ones follow at the end
+    const bool few = !(t > 0) || most == -INFINITY || (k > 0 && k < V && k <= kMostListed && ((4 * k <= (int)blockDim.x && k <= kFew) || 32 * k <= V));
+    if (few) write([&](int, int) { return out_t{}; });
+    if (threadIdx.x == 0) s.zeroed = few;
+    const auto zeros_are_there = [&] {
+        if (!kept) return;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    };
     if (!(t > 0) || most == -INFINITY) { // the first token alone, or none
         if (most != -INFINITY && lane_most == most) {
             row.tiles([&](const float(&e)[kEach], int v) {
@@ -592,12 +601,8 @@ template <class T, class P, int STAGE> __global__ __launch_bounds__(64 * kWaves)
         __syncthreads();
         const int first = most == -INFINITY ? -1 : s.place;
         if (threadIdx.x == 0) a.tokens[r] = first;
-        write([&](int, int v) {
-            out_t y;
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) y[i] = (P)(v + i == first ? 1.0f : 0.0f);
-            return y;
-        });
+        zeros_are_there();
+        if (kept && threadIdx.x == 0 && first >= 0) kept[first] = (P)1.0f;
         return;
     }
     if (most == INFINITY) {
@@ -645,11 +650,49 @@ template <class T, class P, int STAGE> __global__ __launch_bounds__(64 * kWaves)
         if (least > cut.x) cut = Cut{least, 0x7fffffff};
         __syncthreads();
     };
-    if (listed >= 0 && listed <= kRanked && listed <= (int)blockDim.x) {
+    const bool sorted = listed >= 0 && listed <= kRanked && listed <= (int)blockDim.x;
+    if (sorted) {
         rank(s, w, listed, k, p, least, u, a.tokens + r, &cut, &all);
     } else if (listed >= 0) {
+        cuts(List{s.list, listed, V});
+    } else {
+        cuts(row);
+        // The kept tokens are listed where they are few, until a tile has many: the passes that are left evaluate no others then
+        if (cut.x > -INFINITY) {
+            if (threadIdx.x == 0) s.count = 0;
+            __syncthreads();
+            for (int tile = wave; tile < tiles && s.count <= kList; tile += waves) {
+                float e[kEach];
+                const int v = row.tile(tile, e);
+                bool keep[kEach];
+                cut.keeps(e, v, keep);
+                uint64_t lanes[kEach];
+                int total = 0;
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) {
+                    lanes[j] = __ballot(keep[j]);
+                    total += __builtin_popcountll(lanes[j]);
+                }
+                if (total == 0) continue;
+                int at = 0;
+                if (lane == 0) at = atomicAdd(&s.count, total > kTile / 16 ? kList + 1 : total);
+                at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) {
+                    const int mine = at + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(lanes[j] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes[j], 0));
+                    if (keep[j] && mine < kList) s.list[mine] = make_uint2(v + j, key_of(e[j]));
+                    at += __builtin_popcountll(lanes[j]);
+                }
+            }
+            __syncthreads();
+            if (s.count <= kList) listed = s.count;
+            __syncthreads();
+            if (listed >= 0 && !s.zeroed) write([&](int, int) { return out_t{}; });
+        }
+    }
+    if (sorted) {
+    } else if (listed >= 0) {
         const List list{s.list, listed, V};
-        cuts(list);
         clear_bins(s);
         list.tiles([&](const auto &e, int v) {
             if (cut.keeps(e[0], v)) add(s, v / kTile, w.fixed(e[0]));
@@ -674,7 +717,6 @@ template <class T, class P, int STAGE> __global__ __launch_bounds__(64 * kWaves)
             if (before < wanted && wanted <= before + weights[i]) a.tokens[r] = numbers[i];
         }
     } else {
-        cuts(row);
         // Sums of groups of up to 4 tiles, a wave each; then a wave for each tile of the group that the random number meets
         const int group = tiles >= 4 * waves ? 4 : tiles >= 2 * waves ? 2 : 1, groups = (tiles + group - 1) / group;
         // a logit that is not kept is taken as one that weighs nothing
@@ -732,6 +774,17 @@ template <class T, class P, int STAGE> __global__ __launch_bounds__(64 * kWaves)
         }
     }
     const double share = __builtin_ldexp(1.0, a.unit) / (double)all;
+    if (listed >= 0 || s.zeroed) zeros_are_there();
+    if (listed >= 0) {
+        if (kept) {
+            for (int i = threadIdx.x; i < listed; i += blockDim.x) {
+                const float x = logit_of(s.list[i].y);
+                const int v = (int)s.list[i].x;
+                if (cut.keeps(x, v)) kept[v] = (P)(float)(w.exact(x) * share);
+            }
+        }
+        return;
+    }
     write([&](int tile, int) {
         float e[kEach];
         const int v = row.tile(tile, e);
