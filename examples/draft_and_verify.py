@@ -4,7 +4,7 @@ A small decoder with random weights (quantised once by ap_quantize, so that its 
 operators as a server would:
 
   prompt   ap_gemm, ap_cache_append (rotation and 4-bit cache), ap_attention_prompt over packed prompts of different lengths
-  draft    one token per sequence and step at `draft_bits`: ap_gemv, ap_cache_append, ap_attention_cached
+  draft    one token per sequence and step at `draft_bits`: ap_gemm, ap_cache_append, ap_attention_cached, ap_norm between the products, ap_sample
   verify   the drafts of all sequences at once at 8 bits, several tokens per sequence; their keys and values replace those of the
            draft in the cache; ap_verify says how many stand and draws the token after them
 
@@ -43,24 +43,17 @@ class Decoder:
         self.rotary = B.rotary_table(positions, HEAD_DIM)
 
     def forward(self, bits, tokens, positions, slots, attend):
-        """Probabilities after each of `tokens`; attend(layer's cache, q, k, v) is the attention of the call."""
+        """Token and probabilities after each of `tokens`; attend(layer's cache, q, k, v) is the attention of the call."""
         x = self.embedding[tokens].float()
+        h, _ = B.ap_norm(None, x)
         for layer in self.layers:
-            h = B.ap_gemm(layer["qkv"], bits, norm(x)).view(len(tokens), HEADS + 2 * KV_HEADS, HEAD_DIM)
+            h = B.ap_gemm(layer["qkv"], bits, h).view(len(tokens), HEADS + 2 * KV_HEADS, HEAD_DIM)
             q, k, v = h[:, :HEADS], h[:, HEADS:HEADS + KV_HEADS], h[:, HEADS + KV_HEADS:]
             q, k = B.ap_cache_append(layer["cache"], k, v, slots, q=q, positions=positions, rotary=self.rotary)
-            x = x + B.ap_gemm(layer["out"], bits, attend(layer["cache"], q, k, v).view(len(tokens), HIDDEN)).float()
-            gate, up = B.ap_gemm(layer["up"], bits, norm(x)).float().chunk(2, dim=1)
-            x = x + B.ap_gemm(layer["down"], bits, (torch.nn.functional.silu(gate) * up).half()).float()
-        return torch.softmax(B.ap_gemm(self.head, bits, norm(x)).float(), dim=1)
-
-
-def norm(x):
-    return (x * torch.rsqrt(x.square().mean(dim=1, keepdim=True) + 1e-6)).half()
-
-
-def sample(p):
-    return (p / torch.empty_like(p).exponential_()).argmax(dim=1)
+            h, x = B.ap_norm(B.ap_gemm(layer["out"], bits, attend(layer["cache"], q, k, v).view(len(tokens), HIDDEN)), x)
+            gate, up = B.ap_gemm(layer["up"], bits, h).float().chunk(2, dim=1)
+            h, x = B.ap_norm(B.ap_gemm(layer["down"], bits, (torch.nn.functional.silu(gate) * up).half()), x)
+        return B.ap_sample(B.ap_gemm(self.head, bits, h), torch.rand(len(tokens), device="cuda"), probabilities=torch.float32)
 
 
 class Session:
@@ -76,34 +69,34 @@ class Session:
         starts = torch.cat([torch.zeros(1, dtype=torch.int32), counts.cumsum(0).int()]).cuda()
         positions = torch.cat([torch.arange(len(p)) for p in prompts]).cuda()
         sequence = torch.repeat_interleave(torch.arange(n), counts.long()).cuda()
-        p = decoder.forward(8, torch.cat([torch.as_tensor(p) for p in prompts]).cuda(), positions, self.slots(sequence, positions),
-                            lambda cache, q, k, v: B.ap_attention_prompt(q, k, v, starts))
+        new, _ = decoder.forward(8, torch.cat([torch.as_tensor(p) for p in prompts]).cuda(), positions, self.slots(sequence, positions),
+                                 lambda cache, q, k, v: B.ap_attention_prompt(q, k, v, starts))
         self.lengths = counts.cuda()
-        self.last = sample(p[starts[1:].long() - 1])
+        self.last = new[starts[1:].long() - 1]
         self.tokens = [list(t) + [int(x)] for t, x in zip(prompts, self.last)]
 
     def slots(self, sequence, positions):
         return self.tables[sequence, positions // PAGE].long() * PAGE + positions % PAGE
 
     def run(self, bits, tokens):
-        """The model over the next tokens (sequences, n), whose keys and values go to the cache behind `lengths`."""
+        """The model over the next tokens (sequences, n), whose keys and values go to the cache behind `lengths`: tokens and probabilities after each."""
         sequences, n = tokens.shape
         positions = (self.lengths.long()[:, None] + torch.arange(n, device="cuda")).flatten()
         slots = self.slots(torch.arange(sequences, device="cuda").repeat_interleave(n), positions)
-        p = self.decoder.forward(bits, tokens.flatten(), positions, slots,
-                                 lambda cache, q, k, v: B.ap_attention_cached(cache, q, self.tables, self.lengths + n, max_length=self.room))
-        return p.view(sequences, n, VOCABULARY)
+        new, p = self.decoder.forward(bits, tokens.flatten(), positions, slots,
+                                      lambda cache, q, k, v: B.ap_attention_cached(cache, q, self.tables, self.lengths + n, max_length=self.room))
+        return new.view(sequences, n), p.view(sequences, n, VOCABULARY)
 
     def step(self, draft_bits, drafts):
         """Drafts, verifies and keeps what stands; returns the number of accepted drafts of each sequence."""
         tokens, draft, lengths = [self.last], [], self.lengths
         for _ in range(drafts):
-            p = self.run(draft_bits, tokens[-1][:, None])[:, 0]
-            draft.append(p)
-            tokens.append(sample(p))
+            new, p = self.run(draft_bits, tokens[-1][:, None])
+            draft.append(p[:, 0])
+            tokens.append(new[:, 0])
             self.lengths = self.lengths + 1
         self.lengths = lengths                                  # the draft's keys and values are written over
-        target = self.run(8, torch.stack(tokens, dim=1))
+        _, target = self.run(8, torch.stack(tokens, dim=1))
         drafted = torch.stack(tokens[1:], dim=1)
         new, accepted = B.ap_verify(target, torch.stack(draft, dim=1), drafted, torch.rand(drafted.shape, device="cuda"),
                                     torch.empty((len(drafted), VOCABULARY), device="cuda").exponential_())
