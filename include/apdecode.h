@@ -172,7 +172,7 @@ ap_status ap_verify(const ap_verification *a, void *stream);
  * sequence's prefix and its own.  A prefix is read once for all rows of its sequences.
  *   own        as for ap_attention_cached: q, the sequences' own keys (lengths and tables count from the first one behind the prefix), max_length
  *              the bound of their number, out, work (ap_attention_shared_size bytes).  tables may be NULL where max_length is 0
- *   prefixes   up to 2^20, (tokens * heads / 8 + (sequences + prefixes) * kv_heads) < 2^24, tokens * heads < 2^24
+ *   prefixes   up to 2^20, (tokens * heads / 8 + (sequences + prefixes + 512) * kv_heads) < 2^24, tokens * heads < 2^24
  *   prefix_starts device, prefixes + 1: prefix p belongs to the sequences prefix_starts[p] .. prefix_starts[p + 1] - 1; not descending (a prefix
  *              whose two starts descend or leave 0 .. sequences has no sequences, nor has one whose sequences' tokens do in q_starts).  Sequences
  *              before the first and behind the last have no prefix.  NULL: sequences / prefixes each
@@ -180,8 +180,8 @@ ap_status ap_verify(const ap_verification *a, void *stream);
  *   prefix_tables  device, prefixes x prefix_width page numbers; may be NULL where max_prefix is 0
  *   max_prefix host's bound of prefix_lengths, up to prefix_width * page_tokens and 2^30: decides how the work is divided
  * A token that sees no key at all gets zeros.  A prefix need not fill its last page; pages may be shared in any way.  Scores, softmax and sums are
- * binary32.  Where a prefix has more than 32 rows per key head, its values enter the products as ap_cache_read gives them and its weights rounded
- * to binary16; else, and for the sequences' own keys, as in ap_attention_cached.
+ * binary32.  Where prefixes have more than 64 rows per key head on average, their values enter the products as ap_cache_read gives them, rounded to
+ * binary16; else, and for the sequences' own keys, as in ap_attention_cached.
  */
 typedef struct {
     ap_cached own;
@@ -231,7 +231,7 @@ ap_status ap_norm(const ap_normed *a, void *stream);
  *              from row to row
  *   uniform, temperature, top_p, min_p  device, rows binary32;  top_k  device, rows int32;  each but uniform may be NULL: 1, 1, 0 and 0
  *   tokens     device, rows
- *   probabilities device, rows x vocabulary contiguous binary32, or binary16 where half_probabilities != 0; NULL = not wanted
+ *   probabilities device, rows x vocabulary contiguous binary32, or binary16 where half_probabilities != 0; not in the logits' memory; NULL = not wanted
  *   work       device, ap_sample_size bytes, 16-byte aligned; may be NULL where that is 0
  * Weights are binary64 and their sums 64-bit fixed point, exact in any order: what is kept and which token is drawn does not depend on how the work is
  * divided.  A weight below 2^-42 of the greatest (2^-62 of it times the vocabulary) may count as nothing in the sums.

@@ -202,7 +202,8 @@ static ap_status check_shared(const ap_cache *c, const ap_shared *a)
     if (a->own.tokens * a->own.heads >= (int64_t)1 << 24) return AP_ERR_SHAPE; // a workgroup of 256 threads joins the ranges of a row
     if (a->prefixes < 0 || a->prefixes > (1 << 20)) return AP_ERR_SHAPE;
     if (!a->prefix_starts && a->prefixes > 0 && a->own.sequences % a->prefixes) return AP_ERR_SHAPE;
-    if (!groups_ok(a->own.tokens * a->own.heads, 8, (int64_t)a->own.sequences + a->prefixes, c->kv_heads)) return AP_ERR_SHAPE;
+    // besides the row tiles' workgroups there are up to 512 for the prefixes
+    if (!groups_ok(a->own.tokens * a->own.heads, 8, (int64_t)a->own.sequences + a->prefixes + 512, c->kv_heads)) return AP_ERR_SHAPE;
     if (a->prefix_width < 0 || a->prefix_width >= (int64_t)1 << 31 || a->max_prefix < 0 || a->max_prefix > kMaxKeys ||
         a->max_prefix > a->prefix_width * c->page_tokens)
         return AP_ERR_SHAPE;
@@ -272,6 +273,24 @@ extern "C" ap_status ap_sample_size(const ap_sampling *a, size_t *bytes)
     return AP_OK;
 }
 
+// Whether a row of logits lies in the probabilities' memory, which is written before the last logit is read
+static bool overlaps(const ap_sampling *a)
+{
+    if (!a->probabilities) return false;
+    typedef __int128 wide_t; // |rows * stride| is up to 2^63 bytes
+    const wide_t element = a->half ? 2 : 4, row = a->vocabulary * element, begin = reinterpret_cast<uintptr_t>(a->probabilities),
+                 end = begin + (wide_t)a->rows * a->vocabulary * (a->half_probabilities ? 2 : 4);
+    wide_t first = reinterpret_cast<uintptr_t>(a->logits), stride = a->stride * element;
+    if (stride < 0) first += (a->rows - 1) * stride, stride = -stride;
+    // the first row that ends behind the beginning
+    wide_t i = 0;
+    if (first + row <= begin) {
+        if (stride == 0) return false;
+        i = (begin - row - first) / stride + 1;
+    }
+    return i < a->rows && first + i * stride < end;
+}
+
 extern "C" ap_status ap_sample(const ap_sampling *a, void *stream)
 {
     const ap_status s = check_sample(a);
@@ -279,7 +298,7 @@ extern "C" ap_status ap_sample(const ap_sampling *a, void *stream)
     if (a->rows == 0) return AP_OK;
     if (!a->logits || !aligned(a->logits, a->half ? 2 : 4) || !a->uniform || !aligned(a->uniform, 4) || !a->tokens || !aligned(a->tokens, 8) ||
         !aligned(a->temperature, 4) || !aligned(a->top_p, 4) || !aligned(a->min_p, 4) || !aligned(a->top_k, 4) ||
-        !aligned(a->probabilities, a->half_probabilities ? 2 : 4))
+        !aligned(a->probabilities, a->half_probabilities ? 2 : 4) || overlaps(a))
         return AP_ERR_INVALID_ARG;
     const size_t need = sample_work(*a);
     if (need && (!a->work || !aligned(a->work, 16))) return AP_ERR_INVALID_ARG;

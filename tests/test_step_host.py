@@ -41,7 +41,7 @@ def normed(**kw):
 
 def sampling(**kw):
     return Sampling(**dict(dict(logits=P, stride=100, half=0, half_probabilities=0, rows=2, vocabulary=100, uniform=P, temperature=P, top_p=P, min_p=P, top_k=P, tokens=P,
-                                probabilities=P, work=P, work_bytes=1 << 40), **kw))
+                                probabilities=P + (1 << 20), work=P, work_bytes=1 << 40), **kw))
 
 
 def test_shared_refusals():
@@ -124,6 +124,19 @@ def test_sample_refusals():
         if size.value:
             assert ask(sampling(rows=rows_, vocabulary=vocabulary, work_bytes=size.value - 1)) == SMALL
             assert ask(sampling(rows=rows_, vocabulary=vocabulary, work=None, work_bytes=size.value)) == INVALID
+
+
+def test_probabilities_in_the_logits_memory_are_refused():
+    def ask(first, stride, at, rows=3, half=0, half_probabilities=0, V=8):
+        return of(B.lib.ap_sample, sampling(logits=P + first, stride=stride, rows=rows, vocabulary=V, half=half, half_probabilities=half_probabilities, probabilities=P + at))
+    size = 8 * 4
+    for first, stride, at in ((0, 8, 0), (0, 8, 3 * size - 4), (3 * size - 4, 8, 0), (0, 8, size), (0, 0, 0), (size, 0, 0), (4 * size, -8, 0), (4 * size, -8, 4 * size), (0, 1000, 4000),
+                              (0, 1000, 4000 + size - 4), (0, 1000, 8000), (0, 1000, 4004 - 3 * size), ((1 << 39) * 8, -(1 << 40) + 1, (1 << 39) * 8)):
+        assert ask(first, stride, at) == INVALID, (first, stride, at)
+    if not torch.cuda.is_available():                            # (asked for in earnest these addresses would be written)
+        for first, stride, at in ((0, 8, 3 * size), (3 * size, 8, 0), (0, 0, size), (3 * size, 0, 0), (0, 1000, size), (0, 1000, 4000 - 3 * size), (4 * size, -8, 5 * size), (0, 1000, 8000 + size)):
+            assert ask(first, stride, at) not in (0, INVALID, SHAPE), (first, stride, at)
+    assert ask(0, 8, 3 * 16 - 2, half=1, half_probabilities=1) == INVALID
 
 
 def test_binding_refuses_tensors_that_do_not_fit():
