@@ -94,7 +94,7 @@ struct Weights {
     int unit;
     float floor, far; // logits that weigh less than 2^-3 in fixed point, and less than 2^-160; not infinite
     // 2^scale times the weight of x
-    __device__ double of(float x, int scale) const
+    __device__ __forceinline__ double of(float x, int scale) const
     {
         const double magic = 0x1.8p52 + (double)kSteps * scale, y = (double)x - most, t = __builtin_fma(y, rate, magic), f = __builtin_fma(y, rate, magic - t);
         const int k = (int)(uint32_t)__double_as_longlong(t);
@@ -116,9 +116,9 @@ static_assert(kSteps == 1 << 9, "the shift of Weights::of");
 struct Cut {
     float x;
     int last;
-    __device__ bool keeps(float y, int v) const { return y > x || (y == x && v <= last); }
+    __device__ __forceinline__ bool keeps(float y, int v) const { return y > x || (y == x && v <= last); }
     // of n adjacent tokens; mostly all that are equal to x are kept
-    template <int n> __device__ void keeps(const float (&y)[n], int v, bool (&out)[n]) const
+    template <int n> __device__ __forceinline__ void keeps(const float (&y)[n], int v, bool (&out)[n]) const
     {
 #pragma unroll
         for (int i = 0; i < n; ++i) out[i] = y[i] >= x && y[i] > -INFINITY;
@@ -172,7 +172,7 @@ template <class T> struct Row {
         return x;
     }
     // the lane's logits of tile t, a scalar; returns the first one's token
-    __device__ int tile(int t, float (&out)[kEach]) const
+    __device__ __forceinline__ int tile(int t, float (&out)[kEach]) const
     {
         const int v = t * kTile + (threadIdx.x & 63) * kEach;
         typename Eight<T>::values_t e;
@@ -187,7 +187,7 @@ template <class T> struct Row {
         return v;
     }
     // f(logits, first token) for the wave's tiles
-    template <class F> __device__ void tiles(const F &f) const
+    template <class F> __device__ __forceinline__ void tiles(const F &f) const
     {
         const int waves = blockDim.x >> 6;
         for (int t = wave_of_block(); t * kTile < vocabulary; t += waves) {
@@ -197,7 +197,7 @@ template <class T> struct Row {
         }
     }
     // f(logit, token), in little code for what is seldom run
-    template <class F> __device__ void each(const F &f) const
+    template <class F> __device__ __forceinline__ void each(const F &f) const
     {
 #pragma unroll 1
         for (int v = threadIdx.x; v < vocabulary; v += blockDim.x) f(value(v < staged ? stage[v] : x[v]), v);
@@ -208,7 +208,7 @@ template <class T> struct Row {
 struct List {
     const uint2 *list;
     int count, vocabulary;
-    template <class F> __device__ void tiles(const F &f) const
+    template <class F> __device__ __forceinline__ void tiles(const F &f) const
     {
         for (int i = threadIdx.x; i < count; i += blockDim.x) {
             const uint2 x = list[i];
@@ -244,7 +244,7 @@ __device__ __forceinline__ uint64_t share_of(float p, uint64_t sum)
 
 // The first of `count` numbers in LDS at which the sum up to it reaches the target that target(sum of all) gives: s.place, s.before (the sum before it), s.amount
 // (it), s.all and s.wanted, the target.  count <= kBins.  A target is 1 at least; one beyond the sum leaves s.place at -1.
-template <class F> __device__ void find(Shared &s, int count, const F &target)
+template <class F> __device__ __forceinline__ void find(Shared &s, int count, const F &target)
 {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, finders = blockDim.x >> 6 < kFinders ? blockDim.x >> 6 : kFinders;
     const int per = (count + 64 * finders - 1) / (64 * finders), first = threadIdx.x * per;
@@ -320,7 +320,7 @@ struct Even {
 
 // Where the tokens that `cut` keeps, in order, reach `count` (weigh = false), or their weights the share p of their sum.
 //
-// The tokens of the even bin that reaches it are listed.  Their interval of keys is divided into bins until one key is left; where it has more tokens than
+// The tokens of the even bin that reaches it are listed.  Few are ranked among each other; else their interval of keys is divided into bins until one key is left; where it has more tokens than
 // are wanted, an interval of token numbers is, for the first ones.  A bin that holds more than the list is looked for in the row.
 template <class S> __device__ __forceinline__ Cut select(Shared &s, const S &source, const Weights &w, const Cut cut, const Even even, bool weigh, int count, float p)
 {
@@ -354,22 +354,43 @@ template <class S> __device__ __forceinline__ Cut select(Shared &s, const S &sou
         const float at = even.place(x);
         return at >= from && !(at >= to) && cut.keeps(x, v);
     };
+    uint64_t *const orders = s.bins; // of the bin's tokens
     source.tiles([&](const auto &e, int v) {
         constexpr int n = sizeof(e) / sizeof(e[0]);
 #pragma unroll
         for (int i = 0; i < n; ++i)
             if (inside(e[i], v + i)) {
                 const uint32_t key = key_of(e[i]);
-                if (!kListed) {
-                    const int at = atomicAdd(&s.count, 1);
-                    if (at < kList) s.list[at] = make_uint2(v + i, key);
-                }
+                const int at = atomicAdd(&s.count, 1);
+                if (at < kRanked) orders[at] = (uint64_t)key << 32 | (uint32_t)(v + i);
+                if (!kListed && at < kList) s.list[at] = make_uint2(v + i, key);
                 atomicMin(&s.low, key);
                 atomicMax(&s.high, key);
             }
     });
     __syncthreads();
     int listed = s.count;
+    if (const int columns = (listed + 63) & ~63; listed <= kRanked && columns <= (int)blockDim.x) {
+        // few: each one's sum of those ahead of it, in parts of the others
+        uint64_t *const weights = s.bins + kRanked, *const aheads = s.bins + 2 * kRanked;
+        const int i = threadIdx.x, column = i % columns, part = i / columns, parts = blockDim.x / columns;
+        if (i < columns) weights[i] = i >= listed ? 0 : weigh ? w.fixed(logit_of((uint32_t)(orders[i] >> 32))) : 1, aheads[i] = 0;
+        if (threadIdx.x == 0) s.place = 0;
+        __syncthreads();
+        const uint64_t order = orders[column < listed ? column : 0];
+        if (column < listed && part < parts) {
+            uint64_t ahead = 0;
+            for (int j = part; j < listed; j += parts) ahead += orders[j] < order ? weights[j] : 0;
+            atomicAdd((unsigned long long *)&aheads[column], (unsigned long long)ahead);
+        }
+        __syncthreads();
+        if (i < listed && aheads[i] < wanted && wanted <= aheads[i] + weights[i]) s.low = (uint32_t)(order >> 32), s.high = (uint32_t)order;
+        __syncthreads();
+        if (i < listed && (uint32_t)(order >> 32) == s.low && (uint32_t)order > s.high) s.place = 1; // one with the same logit is not kept
+        __syncthreads();
+        const float x = logit_of(s.low);
+        return Cut{x, s.place ? (int)s.high : x == cut.x ? cut.last : 0x7fffffff};
+    }
     if constexpr (kListed) listed = source.count;
     uint32_t low = s.low, high = s.high, key = 0;
     bool numbers = false; // of the tokens with `key`
