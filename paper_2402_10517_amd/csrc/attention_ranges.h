@@ -59,7 +59,12 @@ struct SharedArgs : CachedArgs {
     // sums lie behind those of the sequences' own keys
     bool wide;
     int prefix_groups;
-    int4 *shares; // of each prefix: its first workgroup, tiles, ranges
+    struct Share {
+        int first, tiles, ranges; // its first workgroup, tiles of rows, ranges of keys
+        int begin, end;           // tokens
+        int unused[3];
+    };
+    Share *shares; // of each prefix, for the join
 };
 constexpr int kTileRows = 128;
 
@@ -513,18 +518,18 @@ template <int D, bool SHARED> __global__ __launch_bounds__(kThreads) void attent
         own = ranges = sees > a.chunk ? (sees + a.chunk - 1) / a.chunk : 1; // the first is there even where it holds no key
         const int p = a.prefixes > 0 ? sequence_of(a.prefix_starts, s, a.sequences, a.prefixes) : -1;
         if (p >= 0) {
-            int4 share;
-            if (a.wide) share = a.shares[p];
-            prefix_tokens(a, p, &begin, &end);
-            if (token < begin || token >= end) {
-            } else if (a.wide) {
-                const int kv = a.cache.kv_heads, group = a.heads / kv, head = (int)(row - (int64_t)token * a.heads), of = (int)(token - begin) * group + head % group;
-                ranges += share.z;
-                sums_at = a.splits * rows + ((int64_t)share.x + (int64_t)(of / kTileRows) * kv + head / group) * kTileRows + of % kTileRows;
-                sums_step = (int64_t)share.y * kv * kTileRows;
+            if (a.wide) {
+                const SharedArgs::Share share = a.shares[p];
+                if (token >= share.begin && token < share.end) {
+                    const int kv = a.cache.kv_heads, group = a.heads / kv, head = (int)(row - (int64_t)token * a.heads), of = (token - share.begin) * group + head % group;
+                    ranges += share.ranges;
+                    sums_at = a.splits * rows + ((int64_t)share.first + (int64_t)(of / kTileRows) * kv + head / group) * kTileRows + of % kTileRows;
+                    sums_step = (int64_t)share.tiles * kv * kTileRows;
+                }
             } else {
+                prefix_tokens(a, p, &begin, &end);
                 const int length = prefix_length(a, p);
-                ranges += length > a.prefix_chunk ? (length + a.prefix_chunk - 1) / a.prefix_chunk : 1;
+                if (token >= begin && token < end) ranges += length > a.prefix_chunk ? (length + a.prefix_chunk - 1) / a.prefix_chunk : 1;
             }
         }
         st = stat_of(part), y = part_of(part);

@@ -63,14 +63,14 @@ template <int D> struct Raw {
 };
 
 // What a workgroup does: a row tile of a prefix and key head, and a range of its keys
-struct Share {
+struct Part {
     Item item;
     int head, from, to;
 };
 
 // The prefixes' tiles of keys (of 64, for each tile of rows and key head) are divided evenly among the workgroups that the card has room for: what they really hold is known
 // on the device alone.  (64 lanes call together.)  The first workgroup leaves for the join how.  False: there is nothing left for this one.
-__device__ __forceinline__ bool find_share(const SharedArgs &a, int block, Share *out)
+__device__ __forceinline__ bool find_part(const SharedArgs &a, int block, Part *out)
 {
     const int lane = threadIdx.x & 63, kv = a.cache.kv_heads, group = a.heads / kv;
     struct Prefix {
@@ -123,7 +123,8 @@ __device__ __forceinline__ bool find_share(const SharedArgs &a, int block, Share
             const int other = __shfl_up(upto, d);
             if (lane >= d) upto += other;
         }
-        if (block == 0 && threadIdx.x < 64 && first + lane < a.prefixes) a.shares[first + lane] = make_int4(before + upto - mine, x.tiles, before + upto <= a.prefix_groups ? ranges : 0, 0);
+        if (block == 0 && threadIdx.x < 64 && first + lane < a.prefixes) 
+            a.shares[first + lane] = {before + upto - mine, x.tiles, before + upto <= a.prefix_groups ? ranges : 0, (int)x.begin, (int)(x.begin + x.tokens), {}};
         const uint64_t here = __ballot(before + upto > block);
         if (!found && here) {
             found = true;
@@ -147,11 +148,11 @@ template <int D> __device__ __forceinline__ void attend_prefix(const SharedArgs 
     typedef CacheLayout<D> L;
     typedef Staged<D> T;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
-    Share share;
-    if (!find_share(a, block, &share)) return;
-    const Item it = share.item;
-    const int group = a.heads / a.cache.kv_heads, head = __builtin_amdgcn_readfirstlane(share.head), prefix = it.sequence, n = it.tokens,
-              c0 = __builtin_amdgcn_readfirstlane(share.from), c1 = __builtin_amdgcn_readfirstlane(share.to);
+    Part part;
+    if (!find_part(a, block, &part)) return;
+    const Item it = part.item;
+    const int group = a.heads / a.cache.kv_heads, head = __builtin_amdgcn_readfirstlane(part.head), prefix = it.sequence, n = it.tokens,
+              c0 = __builtin_amdgcn_readfirstlane(part.from), c1 = __builtin_amdgcn_readfirstlane(part.to);
 
     const int row = it.tile * kTileRows + wave * kWaveRows + c, token = row / group;
     const bool valid = token < n;
@@ -450,7 +451,7 @@ Plan plan_of(const ap_cache &c, const ap_shared &a)
         chunk = chunk < 2 * kStep ? 2 * kStep : chunk;
         p.chunk = round_up(chunk < longest ? chunk : longest, kStep);
         p.splits = (int)((longest + p.chunk - 1) / p.chunk);
-        // at most as many workgroups as find_share divides the prefixes among: slots, and a short range of each row tile and key head
+        // at most as many workgroups as find_part divides the prefixes among: slots, and a short range of each row tile and key head
         const int64_t prefix_units = prefix_items_of(kTileRows) * c.kv_heads, ranges = (longest_prefix + kLeastSteps * kTileKeys - 1) / (kLeastSteps * kTileKeys);
         p.prefix_groups = ranges * prefix_units < 512 + prefix_units ? ranges * prefix_units : 512 + prefix_units;
         return p;
@@ -476,7 +477,7 @@ Plan plan_of(const ap_cache &c, const ap_shared &a)
 size_t attention_shared_work(const ap_cache &c, const ap_shared &a)
 {
     const Plan p = plan_of(c, a);
-    return (size_t)p.sums(a) * (c.head_dim * sizeof(float) + sizeof(float2)) + (p.wide ? a.prefixes * sizeof(int4) + 16 : 0);
+    return (size_t)p.sums(a) * (c.head_dim * sizeof(float) + sizeof(float2)) + (p.wide ? a.prefixes * sizeof(SharedArgs::Share) + 32 : 0);
 }
 
 hipError_t launch_attention_shared(const ap_cache &c, const ap_shared &a, hipStream_t stream)
@@ -496,7 +497,7 @@ hipError_t launch_attention_shared(const ap_cache &c, const ap_shared &a, hipStr
     k.out = static_cast<_Float16 *>(o.out);
     k.part = static_cast<float *>(o.work);
     k.stat = reinterpret_cast<float2 *>(k.part + p.sums(a) * c.head_dim);
-    k.shares = reinterpret_cast<int4 *>((reinterpret_cast<uintptr_t>(k.stat + p.sums(a)) + 15) & ~(uintptr_t)15);
+    k.shares = reinterpret_cast<SharedArgs::Share *>((reinterpret_cast<uintptr_t>(k.stat + p.sums(a)) + 31) & ~(uintptr_t)31);
     k.prefix_starts = a.prefix_starts, k.prefix_lengths = a.prefix_lengths, k.prefix_tables = a.prefix_tables;
     k.prefix_width = a.prefix_width;
     k.prefixes = a.prefixes, k.max_prefix = (int)a.max_prefix;
