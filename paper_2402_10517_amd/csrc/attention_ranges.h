@@ -487,6 +487,44 @@ template <int D, int NR, bool SHARED> __global__ __launch_bounds__(kThreads, NR 
     attend_ranges<D, NR, SHARED>(a, blockIdx.x, lds);
 }
 
+// Where the sums of a row's ranges are (64 lanes call together; false: the row has no sequence): its own keys', then its prefix's behind those of all sequences
+struct RowRanges {
+    int64_t row, rows, at, step;
+    int own, all, splits;
+    bool wide;
+    __device__ int64_t place(int i) const // beyond the last any place
+    {
+        if (i >= own && wide) return i < all ? at + (int64_t)(i - own) * step : row;
+        return (int64_t)(i < own ? i : i < all ? i - own + splits : 0) * rows + row;
+    }
+};
+__device__ __forceinline__ bool ranges_of_row(const SharedArgs &a, int token, int head, RowRanges *out)
+{
+    RowRanges r{(int64_t)token * a.heads + head, (int64_t)a.tokens * a.heads, 0, 0, 0, 0, a.splits, a.wide};
+    const int s = sequence_of(a.q_starts, token, a.tokens, a.sequences);
+    if (s < 0) return false;
+    int64_t begin, end;
+    token_range(a.q_starts, s, a.tokens, a.sequences, &begin, &end);
+    const int sees = length_of(a, s) - (int)(end - 1 - token);
+    r.own = r.all = sees > a.chunk ? (sees + a.chunk - 1) / a.chunk : 1; // the first is there even where it holds no key
+    const int p = a.prefixes > 0 ? sequence_of(a.prefix_starts, s, a.sequences, a.prefixes) : -1;
+    if (p >= 0 && a.wide) {
+        const SharedArgs::Share share = a.shares[p];
+        if (token >= share.begin && token < share.end) {
+            const int kv = a.cache.kv_heads, group = a.heads / kv, of = (token - share.begin) * group + head % group;
+            r.all += share.ranges;
+            r.at = a.splits * r.rows + ((int64_t)share.first + (int64_t)(of / kTileRows) * kv + head / group) * kTileRows + of % kTileRows;
+            r.step = (int64_t)share.tiles * kv * kTileRows;
+        }
+    } else if (p >= 0) {
+        prefix_tokens(a, p, &begin, &end);
+        const int length = prefix_length(a, p);
+        if (token >= begin && token < end) r.all += length > a.prefix_chunk ? (length + a.prefix_chunk - 1) / a.prefix_chunk : 1;
+    }
+    *out = r;
+    return true;
+}
+
 // Joins the ranges of a row that sees more than one: D / 4 lanes take every kParts-th range with a running maximum, and one in kParts of the
 // workgroup the rest. The sums are asked for before it is known how many ranges the row has; what is beyond them is dropped.
 template <int D, bool SHARED> __global__ __launch_bounds__(kThreads) void attention_join_kernel(const RangeArgs<SHARED> a)
@@ -495,45 +533,27 @@ template <int D, bool SHARED> __global__ __launch_bounds__(kThreads) void attent
     const int token = blockIdx.x / a.heads, lane = threadIdx.x % kLanes, part = threadIdx.x / kLanes;
     const int64_t row = blockIdx.x, rows = (int64_t)a.tokens * a.heads;
     const float scale = fabsf(a.scale) * kLog2e;
-    int own = 0, ranges = 0; // of its own keys, in all
-    int64_t sums_at = 0, sums_step = 0;
-    // where range i of the row is: SHARED, the prefix's lie behind all sequences' own
+    int ranges = 0;
+    RowRanges found{};
     const auto place_of = [&](int i) {
-        if constexpr (SHARED) {
-            if (i >= own && a.wide) return i < ranges ? sums_at + (int64_t)(i - own) * sums_step : row;
-            return (int64_t)(i < own ? i : i < ranges ? i - own + a.splits : 0) * rows + row;
-        } else return (int64_t)(i < a.splits ? i : 0) * rows + row;
+        if constexpr (SHARED) return found.place(i);
+        else return (int64_t)(i < a.splits ? i : 0) * rows + row;
     };
     const auto stat_of = [&](int i) { return a.stat[place_of(i)]; };
     const auto part_of = [&](int i) { return *reinterpret_cast<const float4_t *>(a.part + place_of(i) * D + lane * 4); };
     float2 st;
     float4_t y;
-    if constexpr (!SHARED) st = stat_of(part), y = part_of(part);
-    const int s = sequence_of(a.q_starts, token, a.tokens, a.sequences);
-    if (s < 0) return;
-    int64_t begin, end;
-    token_range(a.q_starts, s, a.tokens, a.sequences, &begin, &end);
-    const int sees = length_of(a, s) - (int)(end - 1 - token);
     if constexpr (SHARED) {
-        own = ranges = sees > a.chunk ? (sees + a.chunk - 1) / a.chunk : 1; // the first is there even where it holds no key
-        const int p = a.prefixes > 0 ? sequence_of(a.prefix_starts, s, a.sequences, a.prefixes) : -1;
-        if (p >= 0) {
-            if (a.wide) {
-                const SharedArgs::Share share = a.shares[p];
-                if (token >= share.begin && token < share.end) {
-                    const int kv = a.cache.kv_heads, group = a.heads / kv, head = (int)(row - (int64_t)token * a.heads), of = (token - share.begin) * group + head % group;
-                    ranges += share.ranges;
-                    sums_at = a.splits * rows + ((int64_t)share.first + (int64_t)(of / kTileRows) * kv + head / group) * kTileRows + of % kTileRows;
-                    sums_step = (int64_t)share.tiles * kv * kTileRows;
-                }
-            } else {
-                prefix_tokens(a, p, &begin, &end);
-                const int length = prefix_length(a, p);
-                if (token >= begin && token < end) ranges += length > a.prefix_chunk ? (length + a.prefix_chunk - 1) / a.prefix_chunk : 1;
-            }
-        }
+        if (!ranges_of_row(a, token, (int)(row - (int64_t)token * a.heads), &found)) return;
+        ranges = found.all;
         st = stat_of(part), y = part_of(part);
     } else {
+        st = stat_of(part), y = part_of(part);
+        const int s = sequence_of(a.q_starts, token, a.tokens, a.sequences);
+        if (s < 0) return;
+        int64_t begin, end;
+        token_range(a.q_starts, s, a.tokens, a.sequences, &begin, &end);
+        const int sees = length_of(a, s) - (int)(end - 1 - token);
         if (sees <= a.chunk) return;
         ranges = (sees + a.chunk - 1) / a.chunk;
     }

@@ -24,6 +24,9 @@ constexpr int kLeastSteps = 4;
 // 64 steps (512, 32768) 123.3 / 111.4, 128 steps (1024, 32768) 232.7 / 205.6.
 constexpr int kStepsForTwo = 32;
 constexpr int kTried = 16; // prefixes
+// Rows (token and head) from which on the join takes a wave for each instead of a workgroup.  us of the whole call with workgroups / waves: 64 rows 26.9 / 28.7 (36 ranges
+// each), 256 20.1 / 20.8, 512 18.7 / 18.5 and 42.2 / 41.7, 1024 23.8 / 21.2, 29.9 / 29.0 and 49.8 / 49.5, 1920 24.1 / 21.7, 4096 (the join alone) 11.2 / 7.4.
+constexpr int kRowsForWaves = 1024;
 // Weights are 2^7 e^(..): up to 2^15, and above the subnormal numbers of binary16 down to 2^-21 of the greatest.  They go in as two binary16 parts, at twice the products
 // for the values: what is left is the rounding of the values, low + step * code, to binary16.  One part, whose roundings are as large as the result's own: relative error
 // 3.4e-4 against 3.0e-4 with two and 2.1e-4 of the result's rounding alone; 1024 rows over 32768 keys, 8 key heads of 128, 214 us against 258.  Their sum is that of the
@@ -416,6 +419,53 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, 2) void attentio
     else attend_ranges<D, NR, true>(a, blockIdx.x - a.prefix_groups, *reinterpret_cast<RangeSums<D> *>(lds));
 }
 
+// The join where rows are many and their ranges few: a wave for a row, whose ranges go to its 64 / (D / 4) parts, kAtOnce of each asked for at once.
+template <int D> __global__ __launch_bounds__(kThreads) void join_rows_kernel(const SharedArgs a)
+{
+    constexpr int kLanes = D / 4, kParts = 64 / kLanes, kAtOnce = 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & (kLanes - 1), part = (threadIdx.x & 63) / kLanes;
+    const int64_t row = (int64_t)blockIdx.x * kWaves + wave;
+    if (row >= (int64_t)a.tokens * a.heads) return;
+    const int token = (int)row / a.heads;
+    RowRanges r;
+    if (!ranges_of_row(a, token, (int)row - token * a.heads, &r)) return;
+    const float scale = fabsf(a.scale) * kLog2e;
+    // a range without a finite maximum has no key that the row sees, or only NaN: its sums are 0 or NaN and go in as they are
+    const auto keep_of = [&](float from, float to) { return from == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((from - to) * scale); };
+    float top = -INFINITY, total = 0;
+    float4_t x = {0, 0, 0, 0};
+    for (int first = part; first - part < r.all; first += kAtOnce * kParts) {
+        float2 st[kAtOnce];
+        float4_t y[kAtOnce];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            const int64_t place = r.place(first + j * kParts);
+            st[j] = a.stat[place];
+            y[j] = *reinterpret_cast<const float4_t *>(a.part + place * D + lane * 4);
+        }
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j)
+            if (first + j * kParts < r.all) {
+                const float next = fmaxf(top, st[j].x), old = keep_of(top, next), keep = keep_of(st[j].x, next);
+                total = total * old + st[j].y * keep;
+                x = x * old + y[j] * keep;
+                top = next;
+            }
+    }
+#pragma unroll
+    for (int m = kLanes; m < 64; m <<= 1) {
+        const float other = __shfl_xor(top, m), next = fmaxf(top, other), keep = keep_of(top, next), keep_other = keep_of(other, next);
+        total = total * keep + __shfl_xor(total, m) * keep_other;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = x[k] * keep + __shfl_xor(x[k], m) * keep_other;
+        top = next;
+    }
+    half4_t out;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) out[k] = (_Float16)(total == 0.0f ? 0.0f : x[k] / total);
+    if (part == 0) *reinterpret_cast<half4_t *>(a.out + row * D + lane * 4) = out;
+}
+
 struct Plan {
     int rows;  // 16-row tiles per workgroup
     bool wide; // a prefix's rows in tiles of 128
@@ -503,7 +553,10 @@ hipError_t launch_attention_shared(const ap_cache &c, const ap_shared &a, hipStr
     k.prefixes = a.prefixes, k.max_prefix = (int)a.max_prefix;
     k.prefix_items = (int)p.prefix_items, k.prefix_splits = p.prefix_splits, k.prefix_chunk = p.prefix_chunk;
     k.wide = p.wide, k.prefix_groups = (int)p.prefix_groups;
-    const dim3 grid((unsigned)((p.items * p.splits + p.prefix_items * p.prefix_splits) * c.kv_heads + p.prefix_groups)), join((unsigned)(o.tokens * o.heads));
+    const dim3 grid((unsigned)((p.items * p.splits + p.prefix_items * p.prefix_splits) * c.kv_heads + p.prefix_groups));
+    const int64_t rows = o.tokens * o.heads;
+    const bool waves = rows >= kRowsForWaves;
+    const dim3 join((unsigned)(waves ? (rows + kWaves - 1) / kWaves : rows));
     const auto launch = [&](auto narrow, auto wide) {
         if (p.wide) wide<<<grid, kThreads, 0, stream>>>(k);
         else narrow<<<grid, kThreads, 0, stream>>>(k);
@@ -511,11 +564,13 @@ hipError_t launch_attention_shared(const ap_cache &c, const ap_shared &a, hipStr
     if (c.head_dim == 64) {
         if (p.rows == 1) launch(attention_cached_kernel<64, 1, true>, attention_shared_kernel<64, 1>);
         else launch(attention_cached_kernel<64, 2, true>, attention_shared_kernel<64, 2>);
-        attention_join_kernel<64, true><<<join, kThreads, 0, stream>>>(k);
+        if (waves) join_rows_kernel<64><<<join, kThreads, 0, stream>>>(k);
+        else attention_join_kernel<64, true><<<join, kThreads, 0, stream>>>(k);
     } else {
         if (p.rows == 1) launch(attention_cached_kernel<128, 1, true>, attention_shared_kernel<128, 1>);
         else launch(attention_cached_kernel<128, 2, true>, attention_shared_kernel<128, 2>);
-        attention_join_kernel<128, true><<<join, kThreads, 0, stream>>>(k);
+        if (waves) join_rows_kernel<128><<<join, kThreads, 0, stream>>>(k);
+        else attention_join_kernel<128, true><<<join, kThreads, 0, stream>>>(k);
     }
     return hipGetLastError();
 }

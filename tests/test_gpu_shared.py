@@ -148,6 +148,18 @@ def test_large_batches(B):
     shared_case(B, [1500, 2600], [70, 61], [1 + (i * 31) % 200 for i in range(131)], [1 + i % 3 for i in range(131)], 8, 2, 64, 32)
 
 
+def test_joins_of_many_rows(B):
+    # rows from which on a wave joins each, with few and with many ranges, some of them empty, and tokens of no sequence
+    shared_case(B, [5000], [33], [1 + (i * 97) % 900 for i in range(33)], [1] * 33, 32, 4, 128, 64)
+    shared_case(B, [20000, 0, 700], [3, 2, 6], [5 + (i * 517) % 3000 for i in range(13)], [1 + i % 5 for i in range(13)], 40, 40, 64, 16)
+    cache, prefix_table, table, k, v = filled(B, [300], [9] * 40, 2, 64, 16, 5)
+    q, out = normal(1, 80, 16, 64), torch.full((80, 16, 64), 7.0, dtype=torch.float16, device="cuda")
+    starts = int32([3 + i for i in range(41)])
+    B.ap_attention_shared(cache, q, prefix_table, int32([300]), table, int32([9] * 40), q_starts=starts, out=out)
+    want = B.ap_attention_shared(cache, q[3:43].contiguous(), prefix_table, int32([300]), table, int32([9] * 40))
+    assert (out[:3] == 7).all() and (out[43:] == 7).all() and (out[3:43].float() - want.float()).abs().max() <= 2.0 ** -9 * want.abs().max()
+
+
 def test_long_prefixes(B):
     shared_case(B, [70001], [20], [3] * 20, [1] * 20, 8, 1, 128, 64)
     shared_case(B, [33000, 5], [1, 1], [3, 700], [1, 1], 8, 2, 64, 16)
