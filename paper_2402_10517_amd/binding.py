@@ -479,7 +479,7 @@ def ap_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=N
 
     temperature, top_p, min_p: float32 (rows,), top_k: int32 (rows,), None = 1, 1, 0 and 0, which keep every token; a temperature of 0 takes the greatest.
     probabilities: torch.float32 or torch.float16 = those that the token was drawn from, 0 for tokens that were not kept (what ap_verify takes); a
-    tensor (rows, vocabulary) = written there; None = not wanted.  `stream` and work as in ap_attention_cached."""
+    tensor (rows, vocabulary) = written there (not the logits); None = not wanted.  `stream` and work as in ap_attention_cached."""
     if probabilities is None or isinstance(probabilities, torch.dtype):
         kinds = {None: 0, torch.float32: 1, torch.float16: 2}
         assert probabilities in kinds, "probabilities are float32 or float16"

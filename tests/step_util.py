@@ -10,8 +10,8 @@ def shared_attention(q, k, v, scale, sees, low_k, low_v):
     """One sequence over its prefix and its own keys: q (n, heads, D), k, v (m, kv_heads, D), 64-bit, query i sees the first sees[i] keys.  (out, bound).
 
     The bound is of a kernel with binary32 scores and sums (a sum of products is off by 16 EPS32 of the magnitudes that enter it, low_k and low_v with
-    offsets), with weights and values rounded to binary16 each, that rounds its result to binary16.  A weight below 2^-21 of the greatest is a subnormal number
-    of binary16: off by 2^-25 2^-7 of the greatest at least, which is a share of at most 2^-32 of the sum of weights per key."""
+    offsets), with values rounded to binary16 and weights kept to 16 bits (2^-17), that rounds its result to binary16.  A weight below 2^-21 of the greatest is a subnormal
+    number of binary16: off by 2^-25 2^-7 of the greatest at least, which is a share of at most 2^-32 of the sum of weights per key."""
     n, H, D = q.shape
     m, G, _ = k.shape
     if m == 0 or n == 0:
@@ -37,7 +37,7 @@ def shared_attention(q, k, v, scale, sees, low_k, low_v):
     size = torch.where(seen, size, torch.zeros_like(size)).amax(2, keepdim=True)
     magnitude = torch.nan_to_num(low_v).abs()
     mass = torch.matmul(torch.nan_to_num(p), magnitude)
-    rel = 2 * (16 + 4) * EPS32 * size + 2 * HALF_EPS16 + 64 * EPS32
+    rel = 2 * (16 + 4) * EPS32 * size + HALF_EPS16 + 2 * 2.0 ** -17 + 64 * EPS32
     small = 2.0 ** -32 * torch.matmul(seen.double().expand(G, -1, -1).contiguous(), magnitude)
     bound = HALF_EPS16 * torch.nan_to_num(out).abs() + rel * mass + small + SUBNORMAL16
     back = lambda x: x.view(G, group, n, D).permute(2, 0, 1, 3).reshape(n, H, D)  # noqa: E731

@@ -143,6 +143,13 @@ def test_many_prefixes(B):
     shared_case(B, [1 + (i * 37) % 90 for i in range(P)], sizes, [1 + (i * 13) % 40 for i in range(n)], [i % 3 for i in range(n)], 4, 2, 64, 16)
 
 
+def test_many_prefixes_of_many_rows(B):
+    sizes = [i % 5 for i in range(70)]
+    n = sum(sizes)
+    shared_case(B, [(i * 37) % 290 for i in range(70)], sizes, [1 + (i * 13) % 40 for i in range(n)], [1 + i % 2 for i in range(n)], 40, 1, 64, 16)
+    shared_case(B, [2000 + i for i in range(17)], [3] * 17, [1 + (i * 13) % 40 for i in range(51)], [1] * 51, 66, 3, 64, 32)
+
+
 def test_large_batches(B):
     shared_case(B, [1500, 2600], [70, 61], [1 + (i * 31) % 200 for i in range(131)], [1] * 131, 16, 2, 128, 64)
     shared_case(B, [1500, 2600], [70, 61], [1 + (i * 31) % 200 for i in range(131)], [1 + i % 3 for i in range(131)], 8, 2, 64, 32)
