@@ -197,7 +197,7 @@ ap_status ap_attention_shared(const ap_cache *c, const ap_shared *a, void *strea
  *   y = post ? norm(x) * post_weight + post_bias : x,   r = residual + scale * gate * y rounded to the residual's type,   out = norm(r) * weight + bias
  * with norm(a) = a / sqrt(mean(a^2) + eps), or (centred) (a - mean(a)) / sqrt(mean((a - mean(a))^2) + eps).
  *   tokens, columns  up to 2^31 - 256 rows of up to 32768 values, which are contiguous; rows may have any stride (in elements; 0 = the same row for all, of
- *              what is read)
+ *              what is read; |stride| >= columns of what is written)
  *   x          binary16, the block's output; NULL = none (r = residual; gate, post and scale are not looked at)
  *   residual   binary32, or binary16 where half != 0; NULL = none (r = scale * gate * y); x and residual are not both NULL
  *   gate       binary16; NULL = 1.  A gate per channel has stride 0

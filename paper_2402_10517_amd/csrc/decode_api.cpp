@@ -251,6 +251,9 @@ extern "C" ap_status ap_norm(const ap_normed *a, void *stream)
         return AP_ERR_INVALID_ARG;
     if (!aligned(a->weight, 2) || !aligned(a->bias, 2) || !aligned(a->post_weight, 2) || !aligned(a->post_bias, 2)) return AP_ERR_INVALID_ARG;
     if (!std::isfinite(a->scale) || !(a->eps >= 0) || !std::isfinite(a->eps)) return AP_ERR_INVALID_ARG;
+    // rows that are written lie apart
+    const auto apart = [&](const ap_rows &r) { return !r.data || a->tokens < 2 || r.stride >= a->columns || -r.stride >= a->columns; };
+    if (!apart(a->out) || !apart(a->residual_out)) return AP_ERR_INVALID_ARG;
     if (!a->out.data && !a->residual_out.data) return AP_OK;
     return done(launch_norm(*a, static_cast<hipStream_t>(stream)));
 }

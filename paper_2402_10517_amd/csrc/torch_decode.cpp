@@ -479,7 +479,7 @@ PyObject *sample(PyObject *, PyObject *const *args, Py_ssize_t n)
             if (kind) probabilities = allocate({S, V}, kind == 2 ? at::kHalf : at::kFloat, c.device, c.stream, true);
         } else {
             probabilities = c.tensor(args[6], "probabilities");
-            if (probabilities.dim() != 2 || (probabilities.scalar_type() != at::kHalf && probabilities.scalar_type() != at::kFloat))
+            if (probabilities.dim() != 2 || probabilities.size(0) != S || probabilities.size(1) != V || (probabilities.scalar_type() != at::kHalf && probabilities.scalar_type() != at::kFloat))
                 refuse("probabilities", "must be a float32 or float16 tensor (rows, vocabulary)");
             c.array(args[6], "probabilities", probabilities.scalar_type(), S * V);
         }

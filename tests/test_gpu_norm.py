@@ -213,3 +213,11 @@ def test_tensors_that_do_not_fit_are_refused(B):
         B.ap_norm(normal(1, 2, 32769), None)
     with pytest.raises(TypeError):
         B.ap_norm(None, None)
+
+
+def test_rows_that_are_written_lie_apart(B):
+    x, r = normal(1, 3, 64), normal(2, 3, 64, dtype=torch.float32)
+    for bad in (dict(out=x[:1].expand(3, -1)), dict(residual_out=r[:1].expand(3, -1)), dict(out=torch.empty(256, dtype=torch.float16, device="cuda").as_strided((3, 64), (32, 1)))):
+        with pytest.raises(B.ApError):
+            B.ap_norm(x, r, **bad)
+    assert B.ap_norm(x[:1], r[:1], out=torch.empty_like(x)[:1].expand(1, -1))[0].shape == (1, 64)

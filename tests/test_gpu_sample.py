@@ -242,3 +242,18 @@ def test_tensors_that_do_not_fit_are_refused(B):
     with pytest.raises(TypeError):
         call(uniform=None)
     assert call(logits=logits[:0], uniform=u[:0])[0].shape == (0,)
+
+
+def test_probabilities_that_do_not_fit_are_refused(B):
+    x, u = logits_of(1, 4, 100, False), uniform_of(1, 4)
+    before = x.clone()
+    with pytest.raises(AssertionError):
+        B.ap_sample(x, u, probabilities=torch.empty((100, 4), device="cuda"))
+    with pytest.raises(B.ApError):                              # the logits themselves
+        B.ap_sample(x, u, probabilities=x)
+    both = torch.empty(1000, device="cuda")
+    both[:400] = x.flatten()
+    with pytest.raises(B.ApError):                              # the last row
+        B.ap_sample(both[:400].view(4, 100), u, probabilities=both[399:799].view(4, 100))
+    tokens, p = B.ap_sample(both[:400].view(4, 100), u, probabilities=both[400:800].view(4, 100))
+    assert torch.equal(x, before) and torch.equal(tokens, B.ap_sample(x, u)[0]) and torch.equal(p, B.ap_sample(x, u, probabilities=torch.float32)[1])

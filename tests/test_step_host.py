@@ -98,7 +98,7 @@ def test_norm_refusals():
     none = Rows(None, 0)
     for bad in (dict(x=none, residual=none), dict(x=Rows(P + 1, 64)), dict(residual=Rows(P + 2, 64)), dict(residual_out=Rows(P + 2, 64)), dict(gate=Rows(P + 1, 0)),
                 dict(out=Rows(P + 1, 64)), dict(weight=P + 1), dict(bias=P + 1), dict(post_weight=P + 1), dict(post_bias=P + 1), dict(x=Rows(P, 1 << 40)),
-                dict(out=Rows(P, -(1 << 40))), dict(scale=float("nan")), dict(eps=-1e-6), dict(eps=float("nan")), dict(eps=float("inf")), dict(half=1, residual=Rows(P + 1, 64))):
+                dict(out=Rows(P, -(1 << 40))), dict(out=Rows(P, 63)), dict(out=Rows(P, 0)), dict(residual_out=Rows(P, -63)), dict(scale=float("nan")), dict(eps=-1e-6), dict(eps=float("nan")), dict(eps=float("inf")), dict(half=1, residual=Rows(P + 1, 64))):
         assert ask(normed(**bad)) == INVALID, bad
     for bad in (dict(tokens=-1), dict(tokens=1 << 31), dict(columns=0), dict(columns=32769), dict(columns=-64)):
         assert ask(normed(**bad)) == SHAPE, bad
