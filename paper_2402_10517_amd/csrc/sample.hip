@@ -608,7 +608,16 @@ template <class T, class P, int STAGE> __global__ __launch_bounds__(64 * kWaves)
     };
     // Where few tokens can be kept all probabilities are 0 first, while the search goes on, and those of the kept ones follow at the end
     const bool few = !(t > 0) || most == -INFINITY || (k > 0 && k < V && k <= kMostListed && ((4 * k <= (int)blockDim.x && k <= kFew) || 32 * k <= V));
-    if (few) write([&](int, int) { return out_t{}; });
+    // zeros in whole 16 bytes, adjacent lanes side by side
+    const auto clear = [&] {
+        if (!kept) return;
+        constexpr int kWide = 16 / sizeof(P);
+        const int ahead = (int)(-reinterpret_cast<uintptr_t>(kept) / sizeof(P) & (kWide - 1)), head = ahead < V ? ahead : V, wide = (V - head) / kWide, tail = head + wide * kWide;
+        if ((int)threadIdx.x < head) kept[threadIdx.x] = (P)0.0f;
+        if ((int)threadIdx.x < V - tail) kept[tail + threadIdx.x] = (P)0.0f;
+        for (int i = threadIdx.x; i < wide; i += blockDim.x) reinterpret_cast<uint4_t *>(kept + head)[i] = uint4_t{0, 0, 0, 0};
+    };
+    if (few) clear();
     if (threadIdx.x == 0) s.zeroed = few;
     const auto zeros_are_there = [&] {
         if (!kept) return;
@@ -675,6 +684,25 @@ template <class T, class P, int STAGE> __global__ __launch_bounds__(64 * kWaves)
         if (least > cut.x) cut = Cut{least, 0x7fffffff};
         __syncthreads();
     };
+    // The kept logits of a tile one behind the other, in the list's memory: weights are evaluated for these alone.  at: the lane's places, -1 for others; returns their
+    // number, of which kGathered are there.
+    constexpr int kGathered = kList * sizeof(uint2) / sizeof(float) / kWaves;
+    float *const gathered = reinterpret_cast<float *>(s.list) + wave * kGathered;
+    const auto gather = [&](const float(&e)[kEach], int v, int (&at)[kEach]) {
+        bool keep[kEach];
+        cut.keeps(e, v, keep);
+        int n = 0;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const uint64_t lanes = __ballot(keep[j]);
+            const int mine = n + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0));
+            if (keep[j] && mine < kGathered) gathered[mine] = e[j];
+            at[j] = keep[j] ? mine : -1;
+            n += __builtin_popcountll(lanes);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); // other lanes of the wave read them
+        return n;
+    };
     const bool sorted = listed >= 0 && listed <= kRanked && listed <= (int)blockDim.x;
     if (sorted) {
         rank(s, w, listed, k, p, least, u, a.tokens + r, &cut, &all);
@@ -712,7 +740,7 @@ template <class T, class P, int STAGE> __global__ __launch_bounds__(64 * kWaves)
             __syncthreads();
             if (s.count <= kList) listed = s.count;
             __syncthreads();
-            if (listed >= 0 && !s.zeroed) write([&](int, int) { return out_t{}; });
+            if (listed >= 0 && !s.zeroed) clear();
         }
     }
     if (sorted) {
@@ -762,11 +790,20 @@ template <class T, class P, int STAGE> __global__ __launch_bounds__(64 * kWaves)
                 float e[kEach];
                 uint64_t x[kEach];
                 const int v = row.tile(i * group + t, e);
+                if (cut.x > -INFINITY) {
+                    int at[kEach];
+                    const int n = gather(e, v, at);
+                    if (n <= kGathered) {
+                        for (int q = lane; q < n; q += 64) sum += w.fixed(gathered[q]);
+                        continue;
+                    }
+                }
                 weigh(e, v, x);
 #pragma unroll
                 for (int j = 0; j < kEach; ++j) sum += x[j];
+                sum -= kEach * kFixedBase;
             }
-            sum = wave_scan(sum - (uint64_t)(group * kEach) * kFixedBase);
+            sum = wave_scan(sum);
             if (lane == 63) s.bins[i] = sum;
         }
         __syncthreads();
@@ -814,6 +851,21 @@ template <class T, class P, int STAGE> __global__ __launch_bounds__(64 * kWaves)
         float e[kEach];
         const int v = row.tile(tile, e);
         out_t y;
+        if (cut.x > -INFINITY) {
+            int at[kEach];
+            const int n = gather(e, v, at);
+            if (n <= kGathered) {
+                for (int q = lane; q < n; q += 64) gathered[q] = (float)(w.exact(gathered[q]) * share);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) {
+                    const float x = gathered[at[i] < 0 ? 0 : at[i]];
+                    y[i] = (P)(at[i] < 0 ? 0.0f : x);
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                return y;
+            }
+        }
         bool keep[kEach], some = false;
         cut.keeps(e, v, keep);
 #pragma unroll
