@@ -174,8 +174,8 @@ ap_status ap_verify(const ap_verification *a, void *stream);
  *              the bound of their number, out, work (ap_attention_shared_size bytes).  tables may be NULL where max_length is 0
  *   prefixes   up to 2^20, (tokens * heads / 8 + (sequences + prefixes + 512) * kv_heads) < 2^24, tokens * heads < 2^24
  *   prefix_starts device, prefixes + 1: prefix p belongs to the sequences prefix_starts[p] .. prefix_starts[p + 1] - 1; not descending (a prefix
- *              whose two starts descend or leave 0 .. sequences has no sequences, nor has one whose sequences' tokens do in q_starts).  Sequences
- *              before the first and behind the last have no prefix.  NULL: sequences / prefixes each
+ *              whose two starts descend or leave 0 .. sequences has no sequences, nor has one whose sequences' tokens do in q_starts, or begin before the end
+ *              of an earlier prefix's).  Sequences before the first and behind the last have no prefix.  NULL: sequences / prefixes each
  *   prefix_lengths device, prefixes: their keys, all of which every token of their sequences sees; above max_prefix taken as max_prefix
  *   prefix_tables  device, prefixes x prefix_width page numbers; may be NULL where max_prefix is 0
  *   max_prefix host's bound of prefix_lengths, up to prefix_width * page_tokens and 2^30: decides how the work is divided

@@ -62,7 +62,8 @@ struct SharedArgs : CachedArgs {
     struct Share {
         int first, tiles, ranges; // its first workgroup, tiles of rows, ranges of keys
         int begin, end;           // tokens
-        int unused[3];
+        int from, to;             // sequences
+        int unused;
     };
     Share *shares; // of each prefix, for the join
 };
@@ -104,18 +105,21 @@ __device__ __forceinline__ bool find_item(const CachedArgs &a, int rows_per_tile
     return false;
 }
 
-// The tokens [begin, end) of a prefix's sequences; none where starts descend or leave their range
-__device__ __forceinline__ void prefix_tokens(const SharedArgs &a, int p, int64_t *begin, int64_t *end)
+// The sequences [from, to) of a prefix and their tokens [begin, end); none, and false, where starts descend or leave their range
+__device__ __forceinline__ bool prefix_tokens(const SharedArgs &a, int p, int64_t *begin, int64_t *end, int64_t *from, int64_t *to)
 {
+    const bool ok = token_range(a.prefix_starts, p, a.sequences, a.prefixes, from, to);
     int64_t first, last;
-    token_range(a.prefix_starts, p, a.sequences, a.prefixes, &first, &last);
-    *begin = *end = 0;
-    if (first >= last) return;
-    const int64_t each = a.q_starts ? 0 : a.tokens / a.sequences, from = a.q_starts ? a.q_starts[first] : first * each,
-                  to = a.q_starts ? a.q_starts[last] : last * each;
-    if (from < 0 || from > to || to > a.tokens) return;
-    *begin = from;
-    *end = to;
+    if (a.q_starts) {
+        first = a.q_starts[*from], last = a.q_starts[*to]; // up to a.sequences
+    } else {
+        const int64_t each = a.tokens / a.sequences;
+        first = *from * each, last = *to * each;
+    }
+    const bool some = *from < *to, there = first >= 0 && first <= last && last <= a.tokens;
+    *begin = some && there ? first : 0;
+    *end = some && there ? last : 0;
+    return ok && (there || !some);
 }
 
 __device__ __forceinline__ int prefix_length(const SharedArgs &a, int p)
@@ -129,14 +133,17 @@ __device__ __forceinline__ bool find_prefix_item(const SharedArgs &a, int rows_p
 {
     const int lane = threadIdx.x & 63, group = a.heads / a.cache.kv_heads;
     int before = 0;
+    Apart apart;
     for (int first = 0; first < a.prefixes; first += 64) {
-        int tiles = 0, length = 0;
-        int64_t begin = 0, end = 0;
+        int length = 0;
+        int64_t begin = 0, end = 0, from, to;
+        bool ok = true;
         if (first + lane < a.prefixes) {
             length = prefix_length(a, first + lane);
-            prefix_tokens(a, first + lane, &begin, &end);
-            tiles = (int)(((end - begin) * group + rows_per_tile - 1) / rows_per_tile);
+            ok = prefix_tokens(a, first + lane, &begin, &end, &from, &to);
         }
+        if (a.prefix_starts || a.q_starts) apart.cut(ok, &begin, &end);
+        const int tiles = (int)(((end - begin) * group + rows_per_tile - 1) / rows_per_tile);
         int upto = tiles;
         for (int d = 1; d < 64; d <<= 1) {
             const int other = __shfl_up(upto, d);
@@ -488,53 +495,95 @@ template <int D, int NR, bool SHARED> __global__ __launch_bounds__(kThreads, NR 
 }
 
 // Where the sums of a row's ranges are (64 lanes call together; false: the row has no sequence): its own keys', then its prefix's behind those of all sequences
-struct RowRanges {
+template <bool WIDE> struct RowRanges {
     int64_t row, rows, at, step;
     int own, all, splits;
-    bool wide;
     __device__ int64_t place(int i) const // beyond the last any place
     {
-        if (i >= own && wide) return i < all ? at + (int64_t)(i - own) * step : row;
+        if (WIDE && i >= own) return i < all ? at + (int64_t)(i - own) * step : row;
         return (int64_t)(i < own ? i : i < all ? i - own + splits : 0) * rows + row;
     }
 };
-__device__ __forceinline__ bool ranges_of_row(const SharedArgs &a, int token, int head, RowRanges *out)
+// What a lane knows of a prefix: its tokens, its sequences and its keys, or its share as find_part has left it
+struct PrefixLane {
+    int64_t begin = 0, end = 0, from = 0, to = 0;
+    int length = 0;
+    bool ok = true;
+    __device__ __forceinline__ PrefixLane(const SharedArgs &a, int p)
+    {
+        if (p >= a.prefixes) return;
+        length = prefix_length(a, p);
+        ok = prefix_tokens(a, p, &begin, &end, &from, &to);
+    }
+};
+struct ShareLane : SharedArgs::Share {
+    __device__ __forceinline__ ShareLane(const SharedArgs &a, int p) : Share{}
+    {
+        if (p < a.prefixes) static_cast<Share &>(*this) = a.shares[p];
+    }
+};
+template <bool WIDE> __device__ __forceinline__ bool ranges_of_row(const SharedArgs &a, int token, int head, RowRanges<WIDE> *out)
 {
-    RowRanges r{(int64_t)token * a.heads + head, (int64_t)a.tokens * a.heads, 0, 0, 0, 0, a.splits, a.wide};
-    const int s = sequence_of(a.q_starts, token, a.tokens, a.sequences);
+    RowRanges<WIDE> r{(int64_t)token * a.heads + head, (int64_t)a.tokens * a.heads, 0, 0, 0, 0, a.splits};
+    const int lane = threadIdx.x & 63;
+    // the first 64 sequences' numbers and prefixes' are asked for together
+    int starts = 0, ends = 0, lengths = 0;
+    const auto ask = [&](int first) {
+        const int i = first + lane < a.sequences ? first + lane : a.sequences - 1;
+        starts = a.q_starts[i], ends = a.q_starts[i + 1], lengths = a.lengths[i];
+    };
+    if (a.q_starts) ask(0);
+    std::conditional_t<WIDE, ShareLane, PrefixLane> prefix(a, lane);
+    int s = -1, sees = 0;
+    if (!a.q_starts) {
+        const int each = a.tokens / a.sequences;
+        s = token / each;
+        sees = length_of(a, s) - ((s + 1) * each - 1 - token);
+    }
+    for (int first = 0; a.q_starts && first < a.sequences; first += 64) {
+        if (first > 0) ask(first);
+        const uint64_t found = __ballot(starts >= 0 && starts <= token && token < ends && ends <= a.tokens && first + lane < a.sequences);
+        if (!found) continue;
+        const int l = __builtin_ctzll(found), length = __builtin_amdgcn_readlane(lengths, l);
+        s = first + l;
+        sees = (length < 0 ? 0 : length > a.max_length ? a.max_length : length) - (__builtin_amdgcn_readlane(ends, l) - 1 - token);
+        break;
+    }
     if (s < 0) return false;
-    int64_t begin, end;
-    token_range(a.q_starts, s, a.tokens, a.sequences, &begin, &end);
-    const int sees = length_of(a, s) - (int)(end - 1 - token);
     r.own = r.all = sees > a.chunk ? (sees + a.chunk - 1) / a.chunk : 1; // the first is there even where it holds no key
-    const int p = a.prefixes > 0 ? sequence_of(a.prefix_starts, s, a.sequences, a.prefixes) : -1;
-    if (p >= 0 && a.wide) {
-        const SharedArgs::Share share = a.shares[p];
-        if (token >= share.begin && token < share.end) {
-            const int kv = a.cache.kv_heads, group = a.heads / kv, of = (token - share.begin) * group + head % group;
-            r.all += share.ranges;
-            r.at = a.splits * r.rows + ((int64_t)share.first + (int64_t)(of / kTileRows) * kv + head / group) * kTileRows + of % kTileRows;
-            r.step = (int64_t)share.tiles * kv * kTileRows;
+    Apart apart;
+    for (int first = 0; first < a.prefixes; first += 64) {
+        if (first > 0) prefix = decltype(prefix)(a, first + lane);
+        if constexpr (!WIDE) apart.cut(prefix.ok, &prefix.begin, &prefix.end);
+        const uint64_t found = __ballot(token >= prefix.begin && token < prefix.end && s >= prefix.from && s < prefix.to);
+        if (!found) continue;
+        const int l = __builtin_ctzll(found);
+        const auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+        if constexpr (WIDE) {
+            const int kv = a.cache.kv_heads, group = a.heads / kv, row = (token - of(prefix.begin)) * group + head % group;
+            r.all += of(prefix.ranges);
+            r.at = a.splits * r.rows + ((int64_t)of(prefix.first) + (int64_t)(row / kTileRows) * kv + head / group) * kTileRows + row % kTileRows;
+            r.step = (int64_t)of(prefix.tiles) * kv * kTileRows;
+        } else {
+            const int length = of(prefix.length);
+            r.all += length > a.prefix_chunk ? (length + a.prefix_chunk - 1) / a.prefix_chunk : 1;
         }
-    } else if (p >= 0) {
-        prefix_tokens(a, p, &begin, &end);
-        const int length = prefix_length(a, p);
-        if (token >= begin && token < end) r.all += length > a.prefix_chunk ? (length + a.prefix_chunk - 1) / a.prefix_chunk : 1;
+        break;
     }
     *out = r;
     return true;
 }
 
 // Joins the ranges of a row that sees more than one: D / 4 lanes take every kParts-th range with a running maximum, and one in kParts of the
-// workgroup the rest. The sums are asked for before it is known how many ranges the row has; what is beyond them is dropped.
-template <int D, bool SHARED> __global__ __launch_bounds__(kThreads) void attention_join_kernel(const RangeArgs<SHARED> a)
+// workgroup the rest. The sums are asked for before it is known how many ranges the row has; what is beyond them is dropped.  WIDE: of SharedArgs that say so
+template <int D, bool SHARED, bool WIDE = false> __global__ __launch_bounds__(kThreads) void attention_join_kernel(const RangeArgs<SHARED> a)
 {
     constexpr int kLanes = D / 4, kParts = kThreads / kLanes;
     const int token = blockIdx.x / a.heads, lane = threadIdx.x % kLanes, part = threadIdx.x / kLanes;
     const int64_t row = blockIdx.x, rows = (int64_t)a.tokens * a.heads;
     const float scale = fabsf(a.scale) * kLog2e;
     int ranges = 0;
-    RowRanges found{};
+    RowRanges<WIDE> found{};
     const auto place_of = [&](int i) {
         if constexpr (SHARED) return found.place(i);
         else return (int64_t)(i < a.splits ? i : 0) * rows + row;

@@ -83,31 +83,34 @@ __device__ __forceinline__ bool find_part(const SharedArgs &a, int block, Part *
 {
     const int lane = threadIdx.x & 63, kv = a.cache.kv_heads, group = a.heads / kv;
     struct Prefix {
-        int64_t begin, tokens;
+        int64_t begin, tokens, from, to;
         int length, tiles, steps;
     };
-    const auto prefix_of = [&](int first) {
-        Prefix x{0, 0, 0, 0, 0};
+    const auto prefix_at = [&](int first, Apart &apart) {
+        Prefix x{};
+        int64_t end = 0;
+        bool ok = true;
         if (first + lane < a.prefixes) {
-            int64_t end;
             x.length = prefix_length(a, first + lane);
-            prefix_tokens(a, first + lane, &x.begin, &end);
-            x.tokens = end - x.begin;
-            x.tiles = (int)((x.tokens * group + kTileRows - 1) / kTileRows);
-            x.steps = (x.length + kTileKeys - 1) / kTileKeys;
+            ok = prefix_tokens(a, first + lane, &x.begin, &end, &x.from, &x.to);
         }
+        apart.cut(ok, &x.begin, &end);
+        x.tokens = end - x.begin;
+        x.tiles = (int)((x.tokens * group + kTileRows - 1) / kTileRows);
+        x.steps = (x.length + kTileKeys - 1) / kTileKeys;
         return x;
     };
-    Prefix x = prefix_of(0);
+    Apart apart, again;
+    Prefix x = prefix_at(0, apart);
     int64_t steps = 0, units = 0;
     for (int first = 0; first < a.prefixes; first += 64) {
-        if (first > 0) x = prefix_of(first);
+        if (first > 0) x = prefix_at(first, apart);
         int64_t s = (int64_t)x.tiles * kv * x.steps, u = x.steps > 0 ? (int64_t)x.tiles * kv : 0;
         for (int m = 1; m < 64; m <<= 1) s += __shfl_xor(s, m), u += __shfl_xor(u, m);
         steps += s;
         units += u;
     }
-    if (a.prefixes > 64) x = prefix_of(0);
+    if (a.prefixes > 64) x = prefix_at(0, again);
     // Each unit's last range may be short: with as many workgroups less there is no second round.  Few prefixes are tried at 64 lengths from there down.
     const int64_t slots = steps >= 256 * kStepsForTwo ? 512 : 256, divided = units < slots / 2 ? slots - units : slots / 2, each = (steps + divided - 1) / divided,
                   all = ((int64_t)a.max_prefix + kTileKeys - 1) / kTileKeys;
@@ -125,15 +128,15 @@ __device__ __forceinline__ bool find_part(const SharedArgs &a, int block, Part *
     int before = 0;
     bool found = false;
     for (int first = 0; first < a.prefixes; first += 64) {
-        if (first > 0) x = prefix_of(first);
+        if (first > 0) x = prefix_at(first, again);
         const int ranges = (x.steps + chunk - 1) / chunk, mine = x.tiles * kv * ranges;
         int upto = mine;
         for (int d = 1; d < 64; d <<= 1) {
             const int other = __shfl_up(upto, d);
             if (lane >= d) upto += other;
         }
-        if (block == 0 && threadIdx.x < 64 && first + lane < a.prefixes) 
-            a.shares[first + lane] = {before + upto - mine, x.tiles, before + upto <= a.prefix_groups ? ranges : 0, (int)x.begin, (int)(x.begin + x.tokens), {}};
+        if (block == 0 && threadIdx.x < 64 && first + lane < a.prefixes)
+            a.shares[first + lane] = {before + upto - mine, x.tiles, ranges, (int)x.begin, (int)(x.begin + x.tokens), (int)x.from, (int)x.to, 0};
         const uint64_t here = __ballot(before + upto > block);
         if (!found && here) {
             found = true;
@@ -144,9 +147,7 @@ __device__ __forceinline__ bool find_part(const SharedArgs &a, int block, Part *
             out->from = split * chunk * kTileKeys;
             out->to = length - out->from > (int64_t)chunk * kTileKeys ? out->from + chunk * kTileKeys : length;
         }
-        // there are more than prefix_groups only where starts descend and prefixes overlap: those behind have no workgroup then
         before += __builtin_amdgcn_readlane(upto, 63);
-        before = before < a.prefix_groups ? before : a.prefix_groups;
     }
     return found;
 }
@@ -426,14 +427,14 @@ template <int D, int NR> __global__ __launch_bounds__(kThreads, 2) void attentio
 }
 
 // The join where rows are many and their ranges few: a wave for a row, whose ranges go to its 64 / (D / 4) parts, kAtOnce of each asked for at once.
-template <int D> __global__ __launch_bounds__(kThreads) void join_rows_kernel(const SharedArgs a)
+template <int D, bool WIDE> __global__ __launch_bounds__(kThreads) void join_rows_kernel(const SharedArgs a)
 {
     constexpr int kLanes = D / 4, kParts = 64 / kLanes, kAtOnce = 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & (kLanes - 1), part = (threadIdx.x & 63) / kLanes;
     const int64_t row = (int64_t)blockIdx.x * kWaves + wave;
     if (row >= (int64_t)a.tokens * a.heads) return;
     const int token = (int)row / a.heads;
-    RowRanges r;
+    RowRanges<WIDE> r;
     if (!ranges_of_row(a, token, (int)row - token * a.heads, &r)) return;
     const float scale = fabsf(a.scale) * kLog2e;
     // a range without a finite maximum has no key that the row sees, or only NaN: its sums are 0 or NaN and go in as they are
@@ -567,16 +568,20 @@ hipError_t launch_attention_shared(const ap_cache &c, const ap_shared &a, hipStr
         if (p.wide) wide<<<grid, kThreads, 0, stream>>>(k);
         else narrow<<<grid, kThreads, 0, stream>>>(k);
     };
+    const auto launch_join = [&](auto narrow, auto wide) {
+        if (p.wide) wide<<<join, kThreads, 0, stream>>>(k);
+        else narrow<<<join, kThreads, 0, stream>>>(k);
+    };
     if (c.head_dim == 64) {
         if (p.rows == 1) launch(attention_cached_kernel<64, 1, true>, attention_shared_kernel<64, 1>);
         else launch(attention_cached_kernel<64, 2, true>, attention_shared_kernel<64, 2>);
-        if (waves) join_rows_kernel<64><<<join, kThreads, 0, stream>>>(k);
-        else attention_join_kernel<64, true><<<join, kThreads, 0, stream>>>(k);
+        if (waves) launch_join(join_rows_kernel<64, false>, join_rows_kernel<64, true>);
+        else launch_join(attention_join_kernel<64, true>, attention_join_kernel<64, true, true>);
     } else {
         if (p.rows == 1) launch(attention_cached_kernel<128, 1, true>, attention_shared_kernel<128, 1>);
         else launch(attention_cached_kernel<128, 2, true>, attention_shared_kernel<128, 2>);
-        if (waves) join_rows_kernel<128><<<join, kThreads, 0, stream>>>(k);
-        else attention_join_kernel<128, true><<<join, kThreads, 0, stream>>>(k);
+        if (waves) launch_join(join_rows_kernel<128, false>, join_rows_kernel<128, true>);
+        else launch_join(attention_join_kernel<128, true>, attention_join_kernel<128, true, true>);
     }
     return hipGetLastError();
 }

@@ -33,20 +33,46 @@ template <int D> struct CacheLayout {
     }
 };
 
-// Tokens [begin, end) of sequence s; none where the two starts descend or leave [0, tokens]
-__device__ __forceinline__ void token_range(const int32_t *starts, int s, int64_t tokens, int sequences, int64_t *begin, int64_t *end)
+// Tokens [begin, end) of sequence s; none, and false, where the two starts descend or leave [0, tokens]
+__device__ __forceinline__ bool token_range(const int32_t *starts, int s, int64_t tokens, int sequences, int64_t *begin, int64_t *end)
 {
     if (!starts) {
         const int64_t each = tokens / sequences;
         *begin = s * each;
         *end = *begin + each;
-        return;
+        return true;
     }
     const int64_t a = starts[s], b = starts[s + 1];
     const bool ok = a >= 0 && a <= b && b <= tokens;
     *begin = ok ? a : 0;
     *end = ok ? b : 0;
+    return ok;
 }
+
+// Ranges of rows that begin before the end of an earlier one are none: no row has two owners, and all row tiles together are as many as the host has counted.  64 lanes call
+// together, for 64 adjacent ranges after the other; ok: the lane's is as its starts say, or there is none for the lane.  Starts that do not descend have no such ranges, and
+// cost a vote of the wave.
+struct Apart {
+    int upto = 0; // the greatest end so far
+    bool ordered = true;
+    __device__ __forceinline__ void cut(bool ok, int64_t *begin, int64_t *end)
+    {
+        ordered = ordered && __all(ok);
+        const bool filled = *begin < *end;
+        if (ordered) {
+            const uint64_t lanes = __ballot(filled);
+            if (lanes) upto = __builtin_amdgcn_readlane((int)*end, 63 - __builtin_clzll(lanes));
+            return;
+        }
+        const int lane = threadIdx.x & 63;
+#pragma unroll 1
+        for (int i = 0; i < 64; ++i) {
+            const int from = __builtin_amdgcn_readlane((int)*begin, i), to = __builtin_amdgcn_readlane((int)*end, i);
+            if (from < upto && lane == i) *begin = *end = 0;
+            if (from < to && to > upto) upto = to;
+        }
+    }
+};
 
 // The sequence of token i (all 64 lanes call together); -1 for a token of none
 __device__ __forceinline__ int sequence_of(const int32_t *starts, int64_t i, int64_t tokens, int sequences)

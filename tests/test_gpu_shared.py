@@ -359,3 +359,43 @@ def test_tensors_that_do_not_fit_are_refused(B):
     with pytest.raises(TypeError):
         call(prefix_tables=None)
     assert call(q=q[:0], tables=table[:0], lengths=own[:0], prefix_tables=prefix_table[:0], prefix_lengths=lens[:0]).shape == (0, 8, 64)
+
+
+@pytest.mark.parametrize("heads,group", [(8, 4), (32, 16)])       # prefixes of few rows on average, and of many
+def test_overlapping_prefixes_go_to_the_first(B, heads, group):
+    # a prefix that begins before the end of an earlier one has no sequences: the same bits as with starts that say so
+    n = 20
+    cache, prefix_table, table, k, v = filled(B, [300, 700, 90, 400], [20 + i for i in range(n)], heads // group, 64, 16, 5)
+    q, own, lengths = normal(1, n, heads, 64), int32([20 + i for i in range(n)]), int32([300, 700, 90, 400])
+    work = torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
+
+    def call(starts, lengths=lengths, **kw):
+        work.fill_(255)                                          # sums that nobody has written are NaN
+        return B.ap_attention_shared(cache, q, prefix_table, lengths, table, own, prefix_starts=int32(starts), work=work, out=torch.full_like(q, 7.0), **kw)
+    for starts, same in (([0, 8, 0, 12, 12], [0, 8, 8, 8, 8]), ([0, n, 0, n, n], [0, n, n, n, n]), ([0, n, 0, n, 0], [0, n, n, n, n]),
+                         ([3, 8, 2, 8, n], [3, 8, 8, 8, n]), ([99, 0, 5, 5, 9], [0, 0, 5, 5, 9])):
+        want = call(same)
+        assert torch.equal(call(starts), want) and torch.isfinite(want).all(), starts
+        assert torch.equal(call(starts, q_starts=int32(list(range(n + 1)))), call(same, q_starts=int32(list(range(n + 1))))), starts
+    # the third, 7 .. 15, begins in the first, 4 .. 9; the fourth begins at its end
+    got, want = call([4, 9, 7, 15, n]), call([4, 9, 9, 15, n], lengths=int32([300, 700, 0, 400]))
+    assert (got.float() - want.float()).abs().max() <= 2.0 ** -9 * want.abs().max()
+
+
+@pytest.mark.parametrize("heads", [2, 66])
+def test_many_overlapping_prefixes(B, heads):
+    # more than a wave looks at at once, of which every other one overlaps all before it: row tiles of the live ones only
+    n, P = 90, 150
+    prefix = [40 + (i * 37) % 300 for i in range(P)]
+    cache, prefix_table, table, k, v = filled(B, prefix, [5 + i % 30 for i in range(n)], 1, 64, 16, 5)
+    q, own = normal(1, n, heads, 64), int32([5 + i % 30 for i in range(n)])
+    work = torch.empty(256 << 20, dtype=torch.uint8, device="cuda")
+
+    def call(starts):
+        work.fill_(255)
+        return B.ap_attention_shared(cache, q, prefix_table, int32(prefix), table, own, prefix_starts=int32(starts), work=work)
+    owners = [min(i * n // 60, n) for i in range(61)]
+    starts = owners[:60] + [n if i % 2 else 0 for i in range(60, P + 1)]
+    same = owners[:60] + [owners[59]] * (P + 1 - 60)             # from there on starts descend, or begin at 0
+    got, want = call(starts), call(same)
+    assert torch.equal(got, want) and torch.isfinite(got).all()
