@@ -86,7 +86,8 @@ ap_status ap_cache_read(const ap_cache *c, const int64_t *slots, int64_t tokens,
  * Attention of new tokens (tokens * heads / 16 + sequences * kv_heads < 2^24) over the cache: out[i] = sum_j softmax_j(scale * q[i] . k[j]) v[j].
  *   q          tokens rows of heads heads; the tokens of a sequence are adjacent
  *   q_starts   device, sequences + 1: sequence s has the tokens q_starts[s] .. q_starts[s + 1] - 1; not descending (a sequence
- *              whose two starts descend or leave 0 .. tokens has no tokens).  NULL: tokens / sequences each
+ *              whose two starts descend or leave 0 .. tokens has no tokens, nor has one that begins before the end of an earlier
+ *              one).  NULL: tokens / sequences each
  *   lengths    device, sequences: the keys of a sequence, its new tokens included (they have been appended): token i of n sees the
  *              first lengths[s] - n + 1 + i keys.  A token that sees none gets zeros.  Lengths above max_length are taken as
  *              max_length
@@ -113,8 +114,8 @@ ap_status ap_attention_cached(const ap_cache *c, const ap_cached *a, void *strea
 
 /*
  * Causal attention over packed sequences: sequence s has the queries q_starts[s] .. q_starts[s + 1] - 1 and the keys k_starts[s] ..
- * k_starts[s + 1] - 1 (device, sequences + 1 each, not descending; a sequence whose two starts descend or leave the rows has none);
- * its last query sees its last key.  Query i of n sees the first m - n + 1 + i of m keys; one that sees none gets zeros, as does
+ * k_starts[s + 1] - 1 (device, sequences + 1 each, not descending; a sequence whose two starts descend or leave the rows has none, nor
+ * has one any queries that begins in q_starts before the end of an earlier one); its last query sees its last key.  Query i of n sees the first m - n + 1 + i of m keys; one that sees none gets zeros, as does
  * one whose scores are all -inf.  What a query does not see does not reach it, NaN and infinities included.
  *   q; k, v    tokens rows of heads heads (tokens * heads < 2^31 - 256, tokens * heads / 128 + sequences * kv_heads < 2^24); keys (up to
  *              2^30) rows of kv_heads heads, their token strides in 0 .. 2^24 (AP_ERR_SHAPE otherwise)

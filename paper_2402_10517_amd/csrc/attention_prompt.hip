@@ -137,13 +137,12 @@ __device__ __forceinline__ bool find_tile(const PromptArgs &a, int item, int *se
 {
     const int lane = threadIdx.x & 63, group = a.heads / a.kv_heads;
     int before = 0;
+    Apart apart;
     for (int first = 0; first < a.sequences; first += 64) {
-        int tiles = 0;
-        if (first + lane < a.sequences) {
-            int64_t begin, end;
-            token_range(a.q_starts, first + lane, a.tokens, a.sequences, &begin, &end);
-            tiles = (int)(((end - begin) * group + kRows - 1) / kRows);
-        }
+        int64_t begin = 0, end = 0;
+        const bool ok = first + lane >= a.sequences || token_range(a.q_starts, first + lane, a.tokens, a.sequences, &begin, &end);
+        apart.cut(ok, &begin, &end);
+        const int tiles = (int)(((end - begin) * group + kRows - 1) / kRows);
         int upto = tiles;
         for (int d = 1; d < 64; d <<= 1) {
             const int other = __shfl_up(upto, d);

@@ -80,14 +80,17 @@ __device__ __forceinline__ bool find_item(const CachedArgs &a, int rows_per_tile
         return true;
     }
     int before = 0;
+    Apart apart;
     for (int first = 0; first < a.sequences; first += 64) {
-        int tiles = 0, length = 0;
+        int length = 0;
         int64_t begin = 0, end = 0;
+        bool ok = true;
         if (first + lane < a.sequences) {
             length = length_of(a, first + lane);
-            token_range(a.q_starts, first + lane, a.tokens, a.sequences, &begin, &end);
-            tiles = (int)(((end - begin) * group + rows_per_tile - 1) / rows_per_tile);
+            ok = token_range(a.q_starts, first + lane, a.tokens, a.sequences, &begin, &end);
         }
+        apart.cut(ok, &begin, &end);
+        const int tiles = (int)(((end - begin) * group + rows_per_tile - 1) / rows_per_tile);
         int upto = tiles;
         for (int d = 1; d < 64; d <<= 1) {
             const int other = __shfl_up(upto, d);
@@ -540,9 +543,13 @@ template <bool WIDE> __device__ __forceinline__ bool ranges_of_row(const SharedA
         s = token / each;
         sees = length_of(a, s) - ((s + 1) * each - 1 - token);
     }
+    Apart own;
     for (int first = 0; a.q_starts && first < a.sequences; first += 64) {
         if (first > 0) ask(first);
-        const uint64_t found = __ballot(starts >= 0 && starts <= token && token < ends && ends <= a.tokens && first + lane < a.sequences);
+        const bool there = first + lane < a.sequences, ok = starts >= 0 && starts <= ends && ends <= a.tokens;
+        int64_t begin = there && ok ? starts : 0, end = there && ok ? ends : 0;
+        own.cut(ok || !there, &begin, &end);
+        const uint64_t found = __ballot(token >= begin && token < end);
         if (!found) continue;
         const int l = __builtin_ctzll(found), length = __builtin_amdgcn_readlane(lengths, l);
         s = first + l;

@@ -74,19 +74,17 @@ struct Apart {
     }
 };
 
-// The sequence of token i (all 64 lanes call together); -1 for a token of none
+// The sequence of token i (all 64 lanes call together); -1 for a token of none, as those of a sequence that begins in an earlier one are
 __device__ __forceinline__ int sequence_of(const int32_t *starts, int64_t i, int64_t tokens, int sequences)
 {
     if (!starts) return (int)(i / (tokens / sequences));
     const int lane = threadIdx.x & 63;
+    Apart apart;
     for (int first = 0; first < sequences; first += 64) {
-        bool mine = false;
-        if (first + lane < sequences) {
-            int64_t a, b;
-            token_range(starts, first + lane, tokens, sequences, &a, &b);
-            mine = i >= a && i < b;
-        }
-        const uint64_t found = __ballot(mine);
+        int64_t a = 0, b = 0;
+        const bool ok = first + lane >= sequences || token_range(starts, first + lane, tokens, sequences, &a, &b);
+        apart.cut(ok, &a, &b);
+        const uint64_t found = __ballot(i >= a && i < b);
         if (found) return first + __builtin_ctzll(found);
     }
     return -1;

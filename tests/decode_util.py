@@ -104,3 +104,24 @@ def slots_of(table, page, sequence, first, last):
 
 def starts(counts):
     return torch.tensor([0] + list(torch.tensor(counts).cumsum(0)), dtype=torch.int32)
+
+
+def live_sequences(starts, tokens):
+    """(sequence, first token, end) of those that have tokens: starts in order and in range, not before the end of an earlier one."""
+    live, upto = [], 0
+    for s, (a, b) in enumerate(zip(starts, starts[1:])):
+        if 0 <= a < b <= tokens:
+            if a >= upto:
+                live.append((s, a, b))
+            upto = max(upto, b)
+    return live
+
+
+def senseless_starts(seed, sequences, tokens):
+    """Starts of which some descend, leave the tokens or lie inside earlier sequences."""
+    g = torch.Generator().manual_seed(seed)
+    draw = lambda n: int(torch.randint(0, n, (1,), generator=g))  # noqa: E731
+    starts = sorted(draw(tokens + 1) for _ in range(sequences + 1))
+    for _ in range((1, 2, 6, 20)[seed % 4]):
+        starts[draw(sequences + 1)] = (draw(tokens + 1), 0, tokens, -3, tokens + 5, 2 ** 31 - 1, -2 ** 31)[draw(7)]
+    return starts

@@ -776,3 +776,62 @@ def test_calls_in_a_graph(B):
         B.ap_cache_append(cache, k, v, old)
         for a, b in zip(got, step()):
             assert torch.equal(a, b)
+
+
+# ------------------------------------------------------------------------------------------------ sequences that begin in an earlier one
+
+
+def int32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.parametrize("width", [3, 40])                       # one launch, and ranges that are joined
+@pytest.mark.parametrize("seed", range(8))
+def test_cached_tokens_have_one_sequence(B, width, seed):
+    S, T, H, G, D, page = (70, 6)[seed % 2], 90, 8, 2, 64, 16
+    cache = full_cache(B, 64, G, D, page)
+    B.ap_cache_append(cache, normal(1, 1024, G, D), normal(2, 1024, G, D), torch.arange(1024).cuda())
+    g = torch.Generator().manual_seed(seed)
+    tables = torch.randint(0, 64, (S, width), generator=g).int().cuda()
+    lengths = torch.randint(0, width * page + 1, (S,), generator=g).int().cuda()
+    q, starts = normal(3, T, H, D), U.senseless_starts(seed, S, T)
+    work = torch.full((64 << 20,), 255, dtype=torch.uint8, device="cuda")      # sums that nobody has written are NaN
+    out = B.ap_attention_cached(cache, q, tables, lengths, q_starts=int32(starts), out=torch.full_like(q, 7.0), work=work)
+    live = U.live_sequences(starts, T)
+    rows = [i for _, a, b in live for i in range(a, b)]
+    rest = [i for i in range(T) if i not in rows]
+    assert (out[rest] == 7).all()
+    if live:
+        of = [s for s, _, _ in live]
+        want = B.ap_attention_cached(cache, q[rows].contiguous(), tables[of].contiguous(), lengths[of].contiguous(), q_starts=U.starts([b - a for _, a, b in live]).cuda())
+        assert torch.isfinite(out).all() and (out[rows].float() - want.float()).abs().max() <= 2.0 ** -9 * want.abs().max()
+
+
+@pytest.mark.parametrize("starts,same", [([0, 40, 0, 60], [0, 40, 40, 40]), ([0, 40, 10, 60], [0, 40, 40, 40]), ([70, 5, 40, 60], [5, 5, 40, 60])])
+def test_cached_sequences_in_an_earlier_one_have_no_tokens(B, starts, same):
+    cache = full_cache(B, 64, 2, 128, 16)
+    B.ap_cache_append(cache, normal(1, 1024, 2, 128), normal(2, 1024, 2, 128), torch.arange(1024).cuda())
+    q, tables = normal(3, 60, 4, 128), torch.arange(64, dtype=torch.int32).cuda().expand(3, -1).contiguous()
+    for lengths in ([64, 64, 64], [1000, 900, 800]):
+        call = lambda st: B.ap_attention_cached(cache, q, tables, int32(lengths), q_starts=int32(st), max_length=max(lengths), out=torch.full_like(q, 7.0),  # noqa: E731
+                                                work=torch.full((64 << 20,), 255, dtype=torch.uint8, device="cuda"))
+        assert torch.equal(call(starts), call(same))
+
+
+@pytest.mark.parametrize("keys", [60, 4000])
+@pytest.mark.parametrize("seed", range(8))
+def test_prompt_tokens_have_one_sequence(B, keys, seed):
+    S, T, H, G, D = (70, 6)[seed % 2], 90, 4, 2, 64
+    q, k, v = normal(3, T, H, D), normal(1, keys, G, D), normal(2, keys, G, D)
+    starts = U.senseless_starts(seed, S, T)
+    cuts = sorted(torch.randint(0, keys + 1, (S + 1,), generator=torch.Generator().manual_seed(seed)).tolist())
+    work = torch.full((64 << 20,), 255, dtype=torch.uint8, device="cuda")
+    out = B.ap_attention_prompt(q, k, v, int32(starts), int32(cuts), out=torch.full_like(q, 7.0), work=work)
+    live = U.live_sequences(starts, T)
+    rows = [i for _, a, b in live for i in range(a, b)]
+    rest = [i for i in range(T) if i not in rows]
+    assert (out[rest] == 7).all()
+    for s, a, b in live:
+        mine = slice(cuts[s], cuts[s + 1])
+        want = B.ap_attention_prompt(q[a:b].contiguous(), k[mine].contiguous(), v[mine].contiguous(), int32([0, b - a]), int32([0, cuts[s + 1] - cuts[s]]))
+        assert (out[a:b].float() - want.float()).abs().max() <= 2.0 ** -9 * max(float(want.abs().max()), 2.0 ** -9), s

@@ -399,3 +399,29 @@ def test_many_overlapping_prefixes(B, heads):
     same = owners[:60] + [owners[59]] * (P + 1 - 60)             # from there on starts descend, or begin at 0
     got, want = call(starts), call(same)
     assert torch.equal(got, want) and torch.isfinite(got).all()
+
+
+@pytest.mark.parametrize("heads", [8, 40])                       # prefixes of few rows on average, and of many
+@pytest.mark.parametrize("seed", range(8))
+def test_tokens_have_one_sequence(B, heads, seed):
+    # sequences and prefixes whose starts make no sense: each token's result is that of its sequence and prefix by themselves
+    S, T, P = (70, 9)[seed % 2], 90, 7
+    cache, prefix_table, table, k, v = filled(B, [300, 20, 700, 90, 400, 1, 33], [1 + (i * 37) % 200 for i in range(S)], 1, 64, 16, 5)
+    lengths, own = int32([300, 20, 700, 90, 400, 1, 33]), int32([1 + (i * 37) % 200 for i in range(S)])
+    q, starts, prefix_starts = normal(1, T, heads, 64), U.senseless_starts(seed, S, T), U.senseless_starts(seed + 50, P, S)
+    work = torch.full((64 << 20,), 255, dtype=torch.uint8, device="cuda")
+    out = B.ap_attention_shared(cache, q, prefix_table, lengths, table, own, prefix_starts=int32(prefix_starts), q_starts=int32(starts), work=work, out=torch.full_like(q, 7.0))
+    live, upto, prefixes = U.live_sequences(starts, T), 0, []
+    for p, (a, b) in enumerate(zip(prefix_starts, prefix_starts[1:])):
+        if 0 <= a < b <= S and 0 <= starts[a] < starts[b] <= T:
+            if starts[a] >= upto:
+                prefixes.append((p, a, b, starts[a], starts[b]))
+            upto = max(upto, starts[b])
+    rows = [i for _, a, b in live for i in range(a, b)]
+    assert (out[[i for i in range(T) if i not in rows]] == 7).all()
+    for s, a, b in live:
+        for i in range(a, b):
+            of = [p for p, s0, s1, t0, t1 in prefixes if s0 <= s < s1 and t0 <= i < t1]
+            sees = int(own[s]) - (b - 1 - i)
+            want = B.ap_attention_shared(cache, q[i:i + 1].contiguous(), prefix_table[of].contiguous(), lengths[of].contiguous(), table[s:s + 1].contiguous(), int32([sees]))
+            assert (out[i].float() - want[0].float()).abs().max() <= 2.0 ** -9 * max(float(want.abs().max()), 2.0 ** -9), (i, s, of)
