@@ -96,7 +96,7 @@ template <int WAVES> __device__ __forceinline__ double block_sum(double x, doubl
     return from_lane(x, WAVES - 1);
 }
 
-// The square of a sum's range: sums of squares beyond it are taken again of values times 2^-64 or 2^64
+// Sums of squares outside these are taken again of values times 2^-70 or 2^100: a thread's 32 then add up to 2^121 at most, or are 2^-98 each at least, subnormal values' too
 constexpr float kLeastSum = 0x1p-80f, kMostSum = 0x1p120f;
 
 // TAIL: the last chunk of a row is not whole
@@ -154,15 +154,15 @@ template <class R, int THREADS, int PER, bool TAIL> __global__ __launch_bounds__
 #pragma unroll
                 for (int i = 0; i < kEach; ++i) s = __builtin_fmaf(v[p][i], v[p][i], s);
             double mean = sum((double)s);
-            if (mean > (double)kMostSum) mean = squares(0x1p-64f) * 0x1p128;
-            else if (mean < (double)kLeastSum) mean = squares(0x1p64f) * 0x1p-128;
+            if (mean > (double)kMostSum) mean = squares(0x1p-70f) * 0x1p140;
+            else if (mean < (double)kLeastSum) mean = squares(0x1p100f) * 0x1p-200;
             mean = mean * a.each + (double)a.eps;
-            // 1 / sqrt as two factors, an inverse root of 1/4 .. 1 (to 1 ulp) and a power of two, of which neither leaves binary32.  Of a row with an infinity both are 0
-            // and its finite values become 0.
+            // 1 / sqrt as two factors, an inverse root of 1/4 .. 1 (to 1 ulp) and a power of two, which comes first, as a change of the exponent: no value leaves binary32, and the power
+            // may (subnormal values without eps have 2^127 and more).  Of a row with an infinity the root is taken as 0 and its finite values become 0.
             const int power = (__builtin_amdgcn_frexp_exp(mean) + 1) >> 1;
             const bool finite = mean < (double)INFINITY;
-            const float f = finite ? __builtin_amdgcn_rsqf((float)__builtin_ldexp(mean, -2 * power)) : mean == (double)INFINITY ? 0.0f : NAN,
-                        g = finite ? __builtin_ldexpf(1.0f, -power) : f;
+            const float f = finite ? __builtin_amdgcn_rsqf((float)__builtin_ldexp(mean, -2 * power)) : mean == (double)INFINITY ? 0.0f : NAN;
+            const int down = finite ? -power : 0;
 #pragma unroll
             for (int p = 0; p < PER; ++p) {
                 const int c = first + p * step;
@@ -174,7 +174,7 @@ template <class R, int THREADS, int PER, bool TAIL> __global__ __launch_bounds__
                     if (weight) w = load<TAIL>(weight, c, columns);
                     if (bias) b = load<TAIL>(bias, c, columns);
 #pragma unroll
-                    for (int i = 0; i < kEach; ++i) v[p][i] = __builtin_fmaf(v[p][i] * f * g, w[i], b[i]);
+                    for (int i = 0; i < kEach; ++i) v[p][i] = __builtin_fmaf(__builtin_ldexpf(v[p][i], down) * f, w[i], b[i]);
                 }
             }
         };

@@ -221,3 +221,38 @@ def test_rows_that_are_written_lie_apart(B):
         with pytest.raises(B.ApError):
             B.ap_norm(x, r, **bad)
     assert B.ap_norm(x[:1], r[:1], out=torch.empty_like(x)[:1].expand(1, -1))[0].shape == (1, 64)
+
+
+def ends_of_binary32(columns):
+    """Rows of binary32 values at the ends of their range, none of them infinite."""
+    g = torch.Generator().manual_seed(columns)
+    most, least = torch.finfo(torch.float32).max, 2.0 ** -149
+    rows = torch.zeros((9, columns), dtype=torch.float64)
+    x = torch.randn((9, columns), generator=g, dtype=torch.float64)
+    rows[0] = 1.0
+    rows[0, columns // 2] = 3e38
+    rows[1] = most
+    rows[2] = most * x[2].sign()
+    rows[3] = (x[3] * 1e38).clamp(-most, most)
+    rows[4] = x[4] * 1e-37
+    rows[5] = (x[5] * 2 ** 20).round() * least
+    rows[6, columns // 3] = least
+    rows[7] = x[7] * 1e-44
+    rows[8] = x[8] * 2.0 ** 63
+    return rows.float()
+
+
+def check_ends(B, r, w, eps, centred, x=None):
+    out, kept = B.ap_norm(x, r.cuda(), w, eps=eps, centred=centred)
+    given = r if x is None else kept.cpu()
+    want, bound = S.norm(given, w.cpu(), None, eps, centred)
+    check(out.cpu(), want, rounded(want, bound, torch.float16), "norm")
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-6])
+@pytest.mark.parametrize("columns", [1, 3, 8, 200, 1000, 5121, 8192, 20000, 32768])
+def test_rows_at_the_ends_of_binary32(B, columns, eps):
+    r, w = ends_of_binary32(columns), normal(3, columns, size=0.2) + 0.5
+    rows = [i for i in range(9) if eps > 0 or bool(r[i].any())]
+    check_ends(B, r[rows], w, eps, False)
+    check_ends(B, r[rows], w, eps, False, x=normal(4, len(rows), columns))
