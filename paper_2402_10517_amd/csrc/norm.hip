@@ -7,6 +7,8 @@
 // with no post norm, binary16, 101 us (537 MB, 5.3 TB/s).  Smaller ones are bound by what a row does one after the other, of which a CU has two or three at a time: loads
 // from HBM, two sums over the workgroup for a centred norm and one for another, weights from the L2, stores.  1531 x 5121 centred with a post norm 26 us (63 MB, 2.4 TB/s), 30 with
 // inputs from HBM, of which the rows' odd starts are 5.  One row of 4096: 4.4 us, a launch that does nothing 3.5.
+#include <type_traits>
+
 #include "decode_device.h"
 
 namespace apgemv {
@@ -99,8 +101,9 @@ template <int WAVES> __device__ __forceinline__ double block_sum(double x, doubl
 // Sums of squares outside these are taken again of values times 2^-70 or 2^100: a thread's 32 then add up to 2^121 at most, or are 2^-98 each at least, subnormal values' too
 constexpr float kLeastSum = 0x1p-80f, kMostSum = 0x1p120f;
 
-// TAIL: the last chunk of a row is not whole
-template <class R, int THREADS, int PER, bool TAIL> __global__ __launch_bounds__(THREADS) void norm_kernel(const NormArgs a)
+// TAIL: the last chunk of a row is not whole.  CENTRED by itself, as what large rows of it need costs the others registers (two workgroups of 1024 threads on a CU leave each 62
+// vector and 80 scalar ones): 8192 x 8192, binary32 residual, post norm 152 us, 166 with a branch.
+template <class R, int THREADS, int PER, bool TAIL, bool CENTRED> __global__ __launch_bounds__(THREADS) void norm_kernel(const NormArgs a)
 {
     __shared__ double places[2][16];
     constexpr bool LATE = THREADS * PER > 2048; // registers do not hold all of a wide row's inputs
@@ -124,19 +127,32 @@ template <class R, int THREADS, int PER, bool TAIL> __global__ __launch_bounds__
             for (int i = 0; i < kEach; ++i) v[p][i] = TAIL && i < n ? v[p][i] : 0.0f;
         };
         // normalises v: sums of up to 8 (the mean) or 32 values in binary32, of those in binary64.  The mean may be far above the differences from it: 48 bits.
-        const auto norm = [&](const _Float16 *weight, const _Float16 *bias) {
+        // large: values may be of any size; else they have been rounded to binary16
+        const auto norm = [&](const _Float16 *weight, const _Float16 *bias, auto large) {
             asm("" : "+s"(weight), "+s"(bias)); // not in registers for the next row
-            if (a.centred) {
-                double s = 0;
+            float part = 1.0f;
+            if constexpr (CENTRED) {
+                const auto values = [&](float by) {
+                    double s = 0;
 #pragma unroll
-                for (int p = 0; p < PER; ++p)
-                    s += (double)(((v[p][0] + v[p][1]) + (v[p][2] + v[p][3])) + ((v[p][4] + v[p][5]) + (v[p][6] + v[p][7])));
-                const double mean = sum(s) * a.each;
-                const float high = (float)mean, low = (float)(mean - (double)high);
+                    for (int p = 0; p < PER; ++p) {
+                        const auto x = [&](int i) { return v[p][i] * by; };
+                        s += (double)(((x(0) + x(1)) + (x(2) + x(3))) + ((x(4) + x(5)) + (x(6) + x(7))));
+                    }
+                    return sum(s);
+                };
+                double mean = values(1.0f);
+                if (large() && !(__builtin_fabs(mean) < (double)INFINITY)) mean = values(0x1p-8f) * 0x1p8; // eight values may add up to more than binary32 holds
+                mean *= a.each;
+                float high = (float)mean, low = (float)(mean - (double)high);
+                if (large()) { // and a difference may be more where the mean is not below the greatest's last place: a quarter of all of them then
+                    part = __builtin_fabsf(high) < 0x1p100f ? 1.0f : 0.25f;
+                    high *= part, low *= part;
+                }
 #pragma unroll
                 for (int p = 0; p < PER; ++p) {
 #pragma unroll
-                    for (int i = 0; i < kEach; ++i) v[p][i] = (v[p][i] - high) - low;
+                    for (int i = 0; i < kEach; ++i) v[p][i] = (large() ? __builtin_fmaf(v[p][i], part, -high) : v[p][i] - high) - low;
                     cut(p);
                 }
             }
@@ -156,13 +172,13 @@ template <class R, int THREADS, int PER, bool TAIL> __global__ __launch_bounds__
             double mean = sum((double)s);
             if (mean > (double)kMostSum) mean = squares(0x1p-70f) * 0x1p140;
             else if (mean < (double)kLeastSum) mean = squares(0x1p100f) * 0x1p-200;
-            mean = mean * a.each + (double)a.eps;
-            // 1 / sqrt as two factors, an inverse root of 1/4 .. 1 (to 1 ulp) and a power of two, which comes first, as a change of the exponent: no value leaves binary32, and the power
-            // may (subnormal values without eps have 2^127 and more).  Of a row with an infinity the root is taken as 0 and its finite values become 0.
-            const int power = (__builtin_amdgcn_frexp_exp(mean) + 1) >> 1;
+            mean = mean * a.each + (double)(CENTRED && large() ? a.eps * part * part : a.eps);
+            // 1 / sqrt as two factors, an inverse root (to 1 ulp) and a power of two, which comes first: values times it are 2^8 at most.  The root is of 1/4 .. 1, or of less where
+            // the power would leave binary32 (rows of subnormal values, without eps).  Of a row with an infinity both are 0 and its finite values become 0.
+            const int half = (__builtin_amdgcn_frexp_exp(mean) + 1) >> 1, power = half > -126 ? half : -126;
             const bool finite = mean < (double)INFINITY;
             const float f = finite ? __builtin_amdgcn_rsqf((float)__builtin_ldexp(mean, -2 * power)) : mean == (double)INFINITY ? 0.0f : NAN;
-            const int down = finite ? -power : 0;
+            const float g = finite ? __builtin_ldexpf(1.0f, -power) : 0.0f;
 #pragma unroll
             for (int p = 0; p < PER; ++p) {
                 const int c = first + p * step;
@@ -174,7 +190,7 @@ template <class R, int THREADS, int PER, bool TAIL> __global__ __launch_bounds__
                     if (weight) w = load<TAIL>(weight, c, columns);
                     if (bias) b = load<TAIL>(bias, c, columns);
 #pragma unroll
-                    for (int i = 0; i < kEach; ++i) v[p][i] = __builtin_fmaf(__builtin_ldexpf(v[p][i], down) * f, w[i], b[i]);
+                    for (int i = 0; i < kEach; ++i) v[p][i] = __builtin_fmaf(v[p][i] * g * f, w[i], b[i]);
                 }
             }
         };
@@ -198,7 +214,7 @@ template <class R, int THREADS, int PER, bool TAIL> __global__ __launch_bounds__
 #pragma unroll
                 for (int i = 0; i < kEach; ++i) v[p][i] = there ? x[p][i] : 0.0f;
             }
-            if (a.post) norm(a.post_weight, a.post_bias);
+            if (a.post) norm(a.post_weight, a.post_bias, std::false_type{});
         }
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
@@ -219,7 +235,7 @@ template <class R, int THREADS, int PER, bool TAIL> __global__ __launch_bounds__
             cut(p);
         }
         if (!a.out) continue;
-        norm(a.weight, a.bias);
+        norm(a.weight, a.bias, std::bool_constant<sizeof(R) == 4>{});
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
             const int c = first + p * step;
@@ -233,7 +249,7 @@ template <class R, int THREADS, int PER, bool TAIL> __global__ __launch_bounds__
     }
 }
 
-template <class R, bool TAIL> void launch(const NormArgs &k, hipStream_t stream)
+template <class R, bool TAIL, bool CENTRED> void launch(const NormArgs &k, hipStream_t stream)
 {
     const int chunks = (k.columns + kEach - 1) / kEach;
     const dim3 grid((unsigned)(k.tokens < 1 << 20 ? k.tokens : 1 << 20));
@@ -241,17 +257,17 @@ template <class R, bool TAIL> void launch(const NormArgs &k, hipStream_t stream)
     // A chunk per thread up to 8192 columns, as a row's time is that of its loads, sums and stores one after the other; of more rows than CUs with a binary16 residual two
     // (three workgroups of 8192 columns on a CU instead of two).  us with one / two, binary16 residual, 8192 columns: 256 rows 6.1 / 6.6, 1024 19.5 / 17.1, 8192
     // 106 / 101, with a centred post norm 170 / 132; 4096 columns, 4096 rows 27.1 / 28.9; binary32 residual, 8192 x 8192 140 / 148, with a post norm and a gate 170 / 181.
-    if (chunks <= 256) norm_kernel<R, 256, 1, TAIL><<<grid, threads(1), 0, stream>>>(k);
-    else if (sizeof(R) == 2 && chunks > 512 && chunks <= 1024 && k.tokens > 256) norm_kernel<R, 512, 2, TAIL><<<grid, threads(2), 0, stream>>>(k);
-    else if (chunks <= 1024) norm_kernel<R, 1024, 1, TAIL><<<grid, threads(1), 0, stream>>>(k);
-    else if (chunks <= 2048) norm_kernel<R, 1024, 2, TAIL><<<grid, threads(2), 0, stream>>>(k);
-    else norm_kernel<R, 1024, 4, TAIL><<<grid, threads(4), 0, stream>>>(k);
+    if (chunks <= 256) norm_kernel<R, 256, 1, TAIL, CENTRED><<<grid, threads(1), 0, stream>>>(k);
+    else if (sizeof(R) == 2 && chunks > 512 && chunks <= 1024 && k.tokens > 256) norm_kernel<R, 512, 2, TAIL, CENTRED><<<grid, threads(2), 0, stream>>>(k);
+    else if (chunks <= 1024) norm_kernel<R, 1024, 1, TAIL, CENTRED><<<grid, threads(1), 0, stream>>>(k);
+    else if (chunks <= 2048) norm_kernel<R, 1024, 2, TAIL, CENTRED><<<grid, threads(2), 0, stream>>>(k);
+    else norm_kernel<R, 1024, 4, TAIL, CENTRED><<<grid, threads(4), 0, stream>>>(k);
 }
 
 template <class R> void launch(const NormArgs &k, hipStream_t stream)
 {
-    if (k.columns % kEach) launch<R, true>(k, stream);
-    else launch<R, false>(k, stream);
+    if (k.columns % kEach) k.centred ? launch<R, true, true>(k, stream) : launch<R, true, false>(k, stream);
+    else k.centred ? launch<R, false, true>(k, stream) : launch<R, false, false>(k, stream);
 }
 
 } // namespace

@@ -246,6 +246,13 @@ def check_ends(B, r, w, eps, centred, x=None):
     out, kept = B.ap_norm(x, r.cuda(), w, eps=eps, centred=centred)
     given = r if x is None else kept.cpu()
     want, bound = S.norm(given, w.cpu(), None, eps, centred)
+    if centred:
+        # The mean is a multiple of 2^-149, the least number of binary32: off by 2^-150, and the differences are exact from there on.  With s that share of their root mean
+        # square, and d one of them, (d + s r) / sqrt(r^2 + s^2 r^2) is within s + s^2 / 2 |d| / r of d / r, and s^2 / 2 <= 2 s up to s = 4: beyond the half of a step there is none.
+        d = given.double() - given.double().mean(1, keepdim=True)
+        spread = d.square().mean(1, keepdim=True).sqrt()
+        share = 2.0 ** -150 / torch.where(spread == 0, torch.ones_like(spread), spread)
+        bound = bound + share * w.cpu().double().abs() + 2 * share * want.abs()
     check(out.cpu(), want, rounded(want, bound, torch.float16), "norm")
 
 
@@ -256,3 +263,20 @@ def test_rows_at_the_ends_of_binary32(B, columns, eps):
     rows = [i for i in range(9) if eps > 0 or bool(r[i].any())]
     check_ends(B, r[rows], w, eps, False)
     check_ends(B, r[rows], w, eps, False, x=normal(4, len(rows), columns))
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-6])
+@pytest.mark.parametrize("columns", [2, 3, 8, 200, 1000, 5121, 8192, 20000, 32768])
+def test_centred_rows_at_the_ends_of_binary32(B, columns, eps):
+    r, w = ends_of_binary32(columns), normal(3, columns, size=0.2) + 0.5
+    most = torch.finfo(torch.float32).max
+    g = torch.Generator().manual_seed(columns)
+    r[1] = most * (1 - torch.rand(columns, generator=g) / 2)       # sums of eight beyond binary32
+    more = torch.full((2, columns), -most)                        # differences beyond it
+    more[0, columns // 2] = most
+    more[1] = torch.where(torch.rand(columns, generator=g) < 0.1, most, -most)
+    more[1, 0], more[1, 1] = most, -most
+    r = torch.cat([r, more])
+    rows = [i for i in range(len(r)) if eps > 0 or bool((r[i] != r[i, 0]).any())]
+    check_ends(B, r[rows], w, eps, True)
+    check_ends(B, r[rows], w, eps, True, x=normal(4, len(rows), columns))
