@@ -11,6 +11,7 @@
 // us, with top-p 0.9 28 to 30; 300 rows of 32003 28 and 53 to 57.  Few rows leave CUs idle: to divide a row among several, all would have to wait for each other
 // between passes, three times at least.
 #include <cfloat>
+#include <cstddef>
 #include <type_traits>
 
 #include "decode_device.h"
@@ -223,7 +224,7 @@ struct List {
 };
 
 struct Shared {
-    uint64_t bins[kBins];        // or the sums of tiles
+    alignas(16) uint64_t bins[kBins]; // or the sums of tiles; read and cleared by 16 bytes
     uint2 list[kList];           // (token, key)
     double table[kSteps];
     uint64_t wave_sum[kFinders];
@@ -232,6 +233,7 @@ struct Shared {
     uint32_t low, high;
     int count, place, kept, zeroed;
 };
+static_assert(offsetof(Shared, bins) % 16 == 0 && alignof(Shared) % 16 == 0, "16-byte accesses of the bins");
 
 // Where in the sum of kept weights a uniform number draws: the first token up to which they reach it.  At least 1, at most the sum.
 __device__ __forceinline__ uint64_t wanted_of(float u, uint64_t sum)
