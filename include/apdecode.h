@@ -233,7 +233,7 @@ ap_status ap_norm(const ap_normed *a, void *stream);
  *   uniform, temperature, top_p, min_p  device, rows binary32;  top_k  device, rows int32;  each but uniform may be NULL: 1, 1, 0 and 0
  *   tokens     device, rows
  *   probabilities device, rows x vocabulary contiguous binary32, or binary16 where half_probabilities != 0; not in the logits' memory; NULL = not wanted
- *   work       device, ap_sample_size bytes, 16-byte aligned; may be NULL where that is 0
+ *   work       not used: ap_sample_size gives 0 for every call
  * Weights are binary64 and their sums 64-bit fixed point, exact in any order: what is kept and which token is drawn does not depend on how the work is
  * divided.  A weight below 2^-42 of the greatest (2^-62 of it times the vocabulary) may count as nothing in the sums.
  */

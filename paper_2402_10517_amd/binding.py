@@ -461,8 +461,8 @@ def ap_norm(x, residual=None, weight=None, bias=None, post_weight=None, post_bia
             out=None, residual_out=None, stream=None):
     """r = residual + scale * gate * post_norm(x) and norm(r) of (tokens, columns); returns (norm(r) float16, r).
 
-    x: float16, a block's output, None = none; residual: float32 or float16, None = none; weight, bias, post_weight, post_bias: float16 (columns,), None = 1 and
-    0; post: whether x is normed, None = where post_weight or post_bias is given; gate: float16 (tokens, columns), or (1, columns) for all; centred: means are
+    x: float16, a block's output, None = none; residual: float32 or float16, None = none; weight, bias, post_weight, post_bias: float16, contiguous, of columns
+    values in any shape, (columns,) or (1, columns), None = 1 and 0; post: whether x is normed, None = where post_weight or post_bias is given; gate: float16 (tokens, columns), or (1, columns) for all; centred: means are
     taken away; normed: False = norm(r) is not wanted (None).  r is allocated where x and a residual are given, else written only to a given residual_out, and
     None otherwise; residual_out may be residual, out may be x.  `stream` as in ap_gemv."""
     if post is None:
@@ -479,7 +479,7 @@ def ap_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=N
 
     temperature, top_p, min_p: float32 (rows,), top_k: int32 (rows,), None = 1, 1, 0 and 0, which keep every token; a temperature of 0 takes the greatest.
     probabilities: torch.float32 or torch.float16 = those that the token was drawn from, 0 for tokens that were not kept (what ap_verify takes); a
-    tensor (rows, vocabulary) = written there (not the logits); None = not wanted.  `stream` and work as in ap_attention_cached."""
+    tensor (rows, vocabulary) = written there (not the logits); None = not wanted.  `stream` as in ap_attention_cached; work is not used."""
     if probabilities is None or isinstance(probabilities, torch.dtype):
         kinds = {None: 0, torch.float32: 1, torch.float16: 2}
         assert probabilities in kinds, "probabilities are float32 or float16"

@@ -47,7 +47,6 @@ hipError_t launch_verify(const ap_verification &a, hipStream_t stream);
 size_t attention_shared_work(const ap_cache &c, const ap_shared &a);
 hipError_t launch_attention_shared(const ap_cache &c, const ap_shared &a, hipStream_t stream);
 hipError_t launch_norm(const ap_normed &a, hipStream_t stream);
-size_t sample_work(const ap_sampling &a);
 hipError_t launch_sample(const ap_sampling &a, hipStream_t stream);
 
 inline CacheShape cache_shape(const ap_cache &c)

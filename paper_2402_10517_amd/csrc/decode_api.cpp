@@ -272,7 +272,7 @@ extern "C" ap_status ap_sample_size(const ap_sampling *a, size_t *bytes)
     const ap_status s = check_sample(a);
     if (s != AP_OK) return s;
     if (!bytes) return AP_ERR_INVALID_ARG;
-    *bytes = a->rows == 0 ? 0 : sample_work(*a);
+    *bytes = 0; // a workgroup has a row and keeps its sums in LDS
     return AP_OK;
 }
 
@@ -303,8 +303,5 @@ extern "C" ap_status ap_sample(const ap_sampling *a, void *stream)
         !aligned(a->temperature, 4) || !aligned(a->top_p, 4) || !aligned(a->min_p, 4) || !aligned(a->top_k, 4) ||
         !aligned(a->probabilities, a->half_probabilities ? 2 : 4) || overlaps(a))
         return AP_ERR_INVALID_ARG;
-    const size_t need = sample_work(*a);
-    if (need && (!a->work || !aligned(a->work, 16))) return AP_ERR_INVALID_ARG;
-    if (a->work_bytes < need) return AP_ERR_BUFFER_TOO_SMALL;
     return done(launch_sample(*a, static_cast<hipStream_t>(stream)));
 }

@@ -898,8 +898,6 @@ template <class T, class P> void launch(const SampleArgs &k, hipStream_t stream)
 
 } // namespace
 
-size_t sample_work(const ap_sampling &) { return 0; }
-
 hipError_t launch_sample(const ap_sampling &a, hipStream_t stream)
 {
     SampleArgs k;

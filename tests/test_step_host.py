@@ -151,3 +151,12 @@ def test_binding_refuses_tensors_that_do_not_fit():
         B.ap_norm(3.0, x)
     with pytest.raises(TypeError):
         B.ap_sample(None, u)
+
+
+def test_sampling_needs_no_workspace():
+    size = ctypes.c_size_t(7)
+    for rows_, vocabulary in ((0, 1), (1, 1), (1, 1 << 20), (64, 131071), (1 << 21, 1 << 20)):
+        size.value = 7
+        assert B.lib.ap_sample_size(ctypes.byref(sampling(rows=rows_, vocabulary=vocabulary)), ctypes.byref(size)) == 0 and size.value == 0
+    if not torch.cuda.is_available():                            # (asked for in earnest the addresses would be written)
+        assert of(B.lib.ap_sample, sampling(work=None, work_bytes=0)) not in (0, INVALID, SHAPE, SMALL)
