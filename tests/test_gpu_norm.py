@@ -280,3 +280,33 @@ def test_centred_rows_at_the_ends_of_binary32(B, columns, eps):
     rows = [i for i in range(len(r)) if eps > 0 or bool((r[i] != r[i, 0]).any())]
     check_ends(B, r[rows], w, eps, True)
     check_ends(B, r[rows], w, eps, True, x=normal(4, len(rows), columns))
+
+
+def test_vectors_of_one_row(B):
+    x, residual, w, b = normal(1, 4, 64), normal(2, 4, 64, dtype=torch.float32), normal(3, 64), normal(4, 64)
+    want = B.ap_norm(x, residual, w, b, w, b)
+    got = B.ap_norm(x, residual, w[None], b[None], w.view(8, 8), b[None])
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    for bad in (dict(bias=torch.stack([b, b])), dict(bias=torch.stack([b, b], dim=1)[:, 0]), dict(bias=b[:63]), dict(bias=b.float())):
+        with pytest.raises(AssertionError):
+            B.ap_norm(x, residual, w, **bad)
+
+
+@pytest.mark.parametrize("tokens,columns,centred", [(1, 4096, False), (33, 5121, True), (300, 8192, False)])
+def test_captured_and_replayed(B, tokens, columns, centred):
+    x, residual, w, b = normal(1, tokens, columns), normal(2, tokens, columns, dtype=torch.float32), normal(3, columns), normal(4, columns)
+    call = lambda: B.ap_norm(x, residual, w, b, post_weight=w, gate=w[None], scale=0.5, centred=centred)  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    graphs, outs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()], []
+    for graph in graphs:
+        with torch.cuda.graph(graph):
+            outs.append(call())
+    for seed in range(5, 9):
+        x.copy_(normal(seed, tokens, columns))
+        residual.copy_(normal(seed + 10, tokens, columns, dtype=torch.float32))
+        for graph in graphs:
+            graph.replay()
+        want = call()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, want[0]) and torch.equal(r, want[1]) for o, r in outs), seed
