@@ -3,8 +3,8 @@
 // r = residual + scale * gate * norm(x) (the norm of the block's output only with `post`), out = norm(r); norm(v) = weight * (v - mean) / sqrt(mean square + eps) + bias.
 //
 // A workgroup holds a row in registers, `PER` chunks of 8 columns per thread: each input is read and each output written once, and the norm after the
-// residual needs no second pass over memory.  Large ones are bound by HBM: 8192 x 8192 with a post norm, a gate per value and a binary32 residual 170 us (940 MB, 5.5 TB/s),
-// with no post norm, binary16, 101 us (537 MB, 5.3 TB/s).  Smaller ones are bound by what a row does one after the other, of which a CU has two or three at a time: loads
+// residual needs no second pass over memory.  Large ones are bound by HBM: 8192 x 8192 with a post norm, a gate per value and a binary32 residual 172 us (940 MB, 5.5 TB/s),
+// with no post norm, binary16, 95 us (537 MB, 5.7 TB/s).  Smaller ones are bound by what a row does one after the other, of which a CU has two or three at a time: loads
 // from HBM, two sums over the workgroup for a centred norm and one for another, weights from the L2, stores.  1531 x 5121 centred with a post norm 26 us (63 MB, 2.4 TB/s), 30 with
 // inputs from HBM, of which the rows' odd starts are 5.  One row of 4096: 4.4 us, a launch that does nothing 3.5.
 #include <type_traits>
@@ -255,10 +255,12 @@ template <class R, bool TAIL, bool CENTRED> void launch(const NormArgs &k, hipSt
     const dim3 grid((unsigned)(k.tokens < 1 << 20 ? k.tokens : 1 << 20));
     const auto threads = [&](int per) { return (chunks + 64 * per - 1) / (64 * per) * 64; };
     // A chunk per thread up to 8192 columns, as a row's time is that of its loads, sums and stores one after the other; of more rows than CUs with a binary16 residual two
-    // (three workgroups of 8192 columns on a CU instead of two).  us with one / two, binary16 residual, 8192 columns: 256 rows 6.1 / 6.6, 1024 19.5 / 17.1, 8192
-    // 106 / 101, with a centred post norm 170 / 132; 4096 columns, 4096 rows 27.1 / 28.9; binary32 residual, 8192 x 8192 140 / 148, with a post norm and a gate 170 / 181.
+    // (three workgroups of 8192 columns on a CU) where a row has more sums or its last chunk takes registers.  us with one / two, binary16 residual: 8192 x 8190 159 / 127,
+    // centred with a post norm 225 / 144, 300 x 6201 8.4 / 7.0; 8192 x 8192 centred with a post norm 123 / 119, centred 104 / 105, 2000 x 6144 centred with a post norm
+    // 24.7 / 23.8; where it stays one: 256 x 8192 5.3 / 5.4, 1024 x 8192 12.7 / 13.7, 8192 x 8192 95 / 100, with a post norm 105 / 111, 4096 x 4096 22.1 / 22.9; binary32
+    // residual, 8192 x 8192 141 / 148, with a post norm and a gate 171 / 179.
     if (chunks <= 256) norm_kernel<R, 256, 1, TAIL, CENTRED><<<grid, threads(1), 0, stream>>>(k);
-    else if (sizeof(R) == 2 && chunks > 512 && chunks <= 1024 && k.tokens > 256) norm_kernel<R, 512, 2, TAIL, CENTRED><<<grid, threads(2), 0, stream>>>(k);
+    else if (sizeof(R) == 2 && (TAIL || CENTRED) && chunks > 512 && chunks <= 1024 && k.tokens > 256) norm_kernel<R, 512, 2, TAIL, CENTRED><<<grid, threads(2), 0, stream>>>(k);
     else if (chunks <= 1024) norm_kernel<R, 1024, 1, TAIL, CENTRED><<<grid, threads(1), 0, stream>>>(k);
     else if (chunks <= 2048) norm_kernel<R, 1024, 2, TAIL, CENTRED><<<grid, threads(2), 0, stream>>>(k);
     else norm_kernel<R, 1024, 4, TAIL, CENTRED><<<grid, threads(4), 0, stream>>>(k);
