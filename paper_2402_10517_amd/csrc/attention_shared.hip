@@ -6,8 +6,8 @@
 //
 // A key of one head is D + 8 bytes and 4 D operations for each row: with hundreds of rows the matrix cores bound it, not HBM.  A tile of 128 rows takes 64 keys a turn,
 // prepared once for its four waves.  Two prefixes of up to 65536 keys, 48 sequences of up to 3 tokens, 64 heads and 8 key heads of 128: 272 us (153 GFLOP, 561
-// TFLOP/s; of the cycles matrix cores 43 %, a third of that for the second part of the weights, vector instructions 49 %, hardly overlapped), of which the join 10.
-// 64 sequences behind 8192 keys with up to 1023 of their own: 51 us, 7 of them the join; 24 sequences with up to 5 tokens behind 3001 keys 18.6, a chain of latencies (start,
+// TFLOP/s; of the cycles matrix cores 41 %, a third of that for the second part of the weights, vector instructions 49 %, hardly overlapped), of which the join 9.
+// 64 sequences behind 8192 keys with up to 1023 of their own: 51 us, 7 of them the join; 24 sequences with up to 5 tokens behind 3001 keys 18.4, a chain of latencies (start,
 // lengths, pages, a turn's 64 keys 1.8 us, sums) twice.
 #include "attention_ranges.h"
 
@@ -24,19 +24,21 @@ static_assert(kTileRows == kWaveRows * kWaves, "query rows of a workgroup");
 constexpr int kTileKeys = 64;                 // keys in LDS, 16 from each wave
 constexpr int kPageKeys = 64 * 16;            // keys whose pages a wave holds
 // The division of the prefixes among workgroups.  Steps (of 64 keys, for a tile of rows and a key head) of a workgroup, at least: us at 1 / 2 / 4, heads of 128,
-// 8 key heads: 96 rows over 2000 keys 22.1 / 19.1 / 20.4, 128 over 4096 25.7 / 25.7 / 23.5, over 8192 29.3 / 28.6 / 29.6.
+// 8 key heads: 96 rows over 2000 keys 22.2 / 19.2 / 21.0, 128 over 4096 24.9 / 25.0 / 24.5, over 8192 27.9 / 27.5 / 27.9; heads of 64, 4 key heads: 96 rows over 3000 keys
+// 15.5 / 15.4 / 17.6, 3 x 128 over 3000 19.6 each.  2 would be the better for the shortest; 4 halves what the join of these reads at most.
 constexpr int kLeastSteps = 4;
 // Steps per CU from which on two workgroups for each share it, one at work while the other waits, at the price of twice as many sums.  us with one / two, 16 steps
-// (64 prefix rows of 16 prefixes, 2048 keys) 81.8 / 87.0, (256 rows, 16384 keys) 48.1 / 49.7; 32 steps (256 rows, 32768 keys) 68.9 / 66.1, (512, 16384) 76.4 / 74.7;
-// 64 steps (512, 32768) 123.3 / 111.4, 128 steps (1024, 32768) 232.7 / 205.6.
+// (128 rows of 16 prefixes, 2048 keys) 76.1 / 83.2, (256 rows, 16384 keys) 47.7 / 51.0; 32 steps (256 rows, 32768 keys) 75.9 / 73.4, (512, 16384) 78.1 / 77.9;
+// 64 steps (512, 32768) 136.9 / 128.7, 128 steps (1024, 32768) 258 / 238.
 constexpr int kStepsForTwo = 32;
 constexpr int kTried = 16; // prefixes
-// Rows (token and head) from which on the join takes a wave for each instead of a workgroup.  us of the whole call with workgroups / waves: 64 rows 26.9 / 28.7 (36 ranges
-// each), 256 20.1 / 20.8, 512 18.7 / 18.5 and 42.2 / 41.7, 1024 23.8 / 21.2, 29.9 / 29.0 and 49.8 / 49.5, 1920 24.1 / 21.7, 4096 (the join alone) 11.2 / 7.4.
+// Rows (token and head) from which on the join takes a wave for each instead of a workgroup.  us of the whole call with workgroups / waves: 64 rows 18.4 / 20.7 (32768 keys),
+// 256 13.8 / 14.0, 512 14.5 / 15.5 and 28.4 / 29.9, 1024 20.7 / 20.2 (1000 keys), 24.9 / 25.0 (4096) and 35.5 / 33.2 (16384), 1920 22.2 / 20.6, 4096 55.2 / 50.3.
 constexpr int kRowsForWaves = 1024;
 // Weights are 2^7 e^(..): up to 2^15, and above the subnormal numbers of binary16 down to 2^-21 of the greatest.  They go in as two binary16 parts, at twice the products
 // for the values: what is left is the rounding of the values, low + step * code, to binary16.  One part, whose roundings are as large as the result's own: relative error
-// 3.4e-4 against 3.0e-4 with two and 2.1e-4 of the result's rounding alone; 1024 rows over 32768 keys, 8 key heads of 128, 214 us against 258.
+// 3.4e-4 against 2.9e-4 with two and 2.1e-4 of the result's rounding alone (64 sequences behind 8192 keys, heads of 128); 1024 rows over 32768 keys, 8 key heads of 128, 187 us
+// against 238.
 constexpr float kRaise = 7.0f;
 // instruction classes of the scheduler's groups
 constexpr int kProducts = 0x8, kLdsReads = 0x100;
@@ -496,8 +498,10 @@ Plan plan_of(const ap_cache &c, const ap_shared &a)
     const int64_t prefix_rows = a.prefixes > 0 ? (o.tokens + a.prefixes - 1) / a.prefixes * group : 0;
     const auto round_up = [](int64_t x, int64_t to) { return (int)((x + to - 1) / to * to); };
     // Tiles of 128 rows read and prepare a key once where the others do so for every 32 rows, and wait longer before their first.  us with tiles of 32 / 128, 8 key
-    // heads of 128: 48 rows over 2000 keys 14.7 / 19.5, over 32768 36.1 / 39.4, 64 over 8192 22.8 / 23.4, 128 over 8192 28.0 / 28.3, over 32768 58.1 / 45.1,
-    // 256 over 1000 20.5 / 22.9, over 32768 92.0 / 65.6, 1024 over 8192 170.6 / 136.1.
+    // heads of 128: 48 rows over 2000 keys 14.0 / 19.9, over 32768 33.2 / 45.2, 64 over 1000 13.6 / 19.3, over 8192 22.1 / 24.5, 128 over 8192 27.6 / 27.6, over 32768
+    // 56.7 / 47.1, 256 over 8192 36.8 / 34.6, over 32768 89.2 / 74.1, 1024 over 1000 43.0 / 36.1, over 8192 91.9 / 85.8; 4 key heads of 64: 3 x 96 over 3000 20.3 / 18.4, 256 over
+    // 8192 22.3 / 20.9, 1024 52.2 / 40.6.  The rule is by rows alone and does not meet the crossing, which depends on the keys too: above it tiles of 32 are ahead at 72 rows (over
+    // 1000 keys 14.0 / 19.7, over 8192 22.6 / 25.3), 96 over 2000 (15.4 / 21.0), 128 and 256 over 1000 (15.3 / 19.8, 17.5 / 21.6; heads of 64 13.0 / 17.4).
     p.wide = prefix_rows > 64;
     if (p.wide) {
         p.rows = each * group <= 16 && longest / kPiece * items_of(16) * c.kv_heads < 1 << 20 ? 1 : 2;

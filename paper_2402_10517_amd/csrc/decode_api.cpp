@@ -199,7 +199,7 @@ static ap_status check_shared(const ap_cache *c, const ap_shared *a)
     if (!a) return c ? AP_ERR_INVALID_ARG : check_cache_shape(c);
     const ap_status s = check_cached(c, &a->own);
     if (s != AP_OK) return s;
-    if (a->own.tokens * a->own.heads >= (int64_t)1 << 24) return AP_ERR_SHAPE; // a workgroup of 256 threads joins the ranges of a row
+    if (a->own.tokens * a->own.heads >= (int64_t)1 << 24) return AP_ERR_SHAPE; // a launch has no more workgroups, and one of the two joins takes one for each row
     if (a->prefixes < 0 || a->prefixes > (1 << 20)) return AP_ERR_SHAPE;
     if (!a->prefix_starts && a->prefixes > 0 && a->own.sequences % a->prefixes) return AP_ERR_SHAPE;
     // besides the row tiles' workgroups there are up to 512 for the prefixes

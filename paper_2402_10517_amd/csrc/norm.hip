@@ -5,7 +5,7 @@
 // A workgroup holds a row in registers, `PER` chunks of 8 columns per thread: each input is read and each output written once, and the norm after the
 // residual needs no second pass over memory.  Large ones are bound by HBM: 8192 x 8192 with a post norm, a gate per value and a binary32 residual 172 us (940 MB, 5.5 TB/s),
 // with no post norm, binary16, 95 us (537 MB, 5.7 TB/s).  Smaller ones are bound by what a row does one after the other, of which a CU has two or three at a time: loads
-// from HBM, two sums over the workgroup for a centred norm and one for another, weights from the L2, stores.  1531 x 5121 centred with a post norm 26 us (63 MB, 2.4 TB/s), 30 with
+// from HBM, two sums over the workgroup for a centred norm and one for another, weights from the L2, stores.  1531 x 5121 centred with a post norm 25.5 us (63 MB, 2.5 TB/s), 30 with
 // inputs from HBM, of which the rows' odd starts are 5.  One row of 4096: 4.4 us, a launch that does nothing 3.5.
 #include <type_traits>
 

@@ -35,9 +35,14 @@ constexpr int kEach = 8;          // adjacent tokens of a lane and tile
 constexpr int kTile = 64 * kEach; // tokens of a wave and step: up to 2^20 / kTile = kBins sums of tiles take the bins' place
 constexpr int kBins = 2048;
 constexpr int kList = 2048;       // tokens that are listed
-constexpr int kMostListed = 1024; // top-k up to which a row's candidates are listed,
-constexpr int kFew = 128;         // and ranked among each other,
-constexpr int kRanked = 256;      // so many at most
+// Top-k up to which a row's candidates are listed, found by groups of 8 tokens where there are four for each of the k (with fewer they give a limit that lists too many), or, up
+// to kFew and a quarter of the lanes, by the tokens of each lane.  us, binary16, top-p too, one row of 131071 by lanes / by groups: top-k 20 11.6 / 18.5, 100 18.1 / 21.9, 128
+// 22.0 / 24.6, 200 30.2 / 29.7, 256 45.4 / 29.6; by groups / without: 129 24.6 / 80, 500 31.7 / 100, 1000 35.7 / 108, 1500 39 / 111, 2000 140 / 117, as the list overflows.  300 rows
+// of 32000 by lanes / by groups: 100 21.4 / 21.8, 128 30.4 / 28.3.  Four groups for each are on the safe side, by groups / without: 8000 tokens 256 16.4 / 18.4, 400 16.9 / 20.1,
+// 1000 23.5 / 20.7; 32000 tokens 1024 22.6 / 39.1.
+constexpr int kMostListed = 1024;
+constexpr int kFew = 128;
+constexpr int kRanked = 256; // tokens that are ranked among each other, at most
 constexpr int kWaves = 16;        // of a workgroup, at most
 constexpr int kFinders = 4;       // waves that look for a place in the bins: all 16 take turns on the four SIMDs, and twice as long
 constexpr double kLog2e = 1.4426950408889634, kLn2 = 0.6931471805599453;
