@@ -50,8 +50,8 @@ __device__ __forceinline__ bool token_range(const int32_t *starts, int s, int64_
 }
 
 // Ranges of rows that begin before the end of an earlier one are none: no row has two owners, and all row tiles together are as many as the host has counted.  64 lanes call
-// together, for 64 adjacent ranges after the other; ok: the lane's is as its starts say, or there is none for the lane.  Starts that do not descend have no such ranges, and
-// cost a vote of the wave.
+// together, each with its range, for the first 64 ranges, the next 64 and so on.  ok: the range is as its starts say, or the lane has none.  Starts that do not descend have no
+// such ranges, and cost a vote of the wave.
 struct Apart {
     int upto = 0; // the greatest end so far
     bool ordered = true;
